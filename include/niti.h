@@ -268,7 +268,8 @@ niti_status niti_sgd_update(int8_t *w, const int32_t *g32, int64_t n, int mu,
                             niti_round_mode mode, niti_stats *stats, void *stream);
 
 /* Bytes of workspace an operation needs (0 when none).  d is used by the
- * convolution ops, (M, N) = (batch, classes) by the loss. */
+ * convolution ops, (M, N) = (batch, classes) by the loss, and (M, N, K) by the
+ * operators on int8 rows as their ids say. */
 size_t niti_workspace_bytes(int op, const niti_conv_desc *d, int64_t M, int64_t N, int64_t K);
 
 /* Human-readable name of a status code (static storage). */
@@ -311,6 +312,164 @@ niti_status niti_dropout_fwd(const int8_t *x, int8_t *y, uint8_t *keep, int64_t 
                              void *stream);
 /* Backward of niti_dropout_fwd: dx = dy where keep, 0 elsewhere. */
 niti_status niti_dropout_bwd(const int8_t *dy, const uint8_t *keep, int8_t *dx, int64_t n, void *stream);
+
+/* ---- Operators on int8 rows with a scale each ----
+ *
+ * The calls above give a tensor one exponent.  Layers whose rows differ in
+ * size (the tokens of a language model, the output channels of a weight
+ * matrix) are held here as int8 rows with one float scale each: row m of a
+ * matrix stands for q[m][.] * scale[m].  With top = max(max |x[m][.]|, 2^-100),
+ *     scale[m] = top / 127,   q = round(x * (127 / top)) in [-127, 127].
+ * A row with an infinity or a NaN gets the scale NaN and codes 0.
+ *
+ * Conventions, besides those at the top of this file:
+ *   Types       Matrices outside int8 are NITI_F32, NITI_BF16 or NITI_F16.
+ *               Sums, statistics and states are held in 32 bits; a result in
+ *               16 bits is rounded once, to nearest even, when it is stored.
+ *   Layout      Matrices are row-major with a row stride in elements (ld...);
+ *               columns are contiguous.  A stride of 0 repeats one row, for
+ *               operands that are only read.  Only the elements' own
+ *               alignment is required; int8 operands of niti_linear_fwd run
+ *               fastest where their addresses and strides are multiples of 16.
+ *   Sizes       No operand is limited to 2^31 bytes.  M == 0 (and N == 0) is
+ *               a call without work.  Row strides and widths are below 2^22
+ *               elements, and the number of rows below 2^31.
+ *   Rounding    Codes are formed with NITI_ROUND_RTN (to nearest, ties to
+ *               even) or NITI_ROUND_SR (floor(x * (127 / top) + u), u from
+ *               draw number call * 2^40 + i + 1 of the SplitMix64 stream of
+ *               seed, i = the element's index m * columns + n);
+ *               NITI_ROUND_PSR, which reads the fraction of an integer, gives
+ *               NITI_ERR_ARG.
+ *   Aliasing    An output may be one of the call's own inputs (same address,
+ *               type and stride) where that is said; otherwise they must not
+ *               overlap.
+ */
+typedef enum niti_type {
+    NITI_F32 = 0,
+    NITI_BF16 = 1,
+    NITI_F16 = 2
+} niti_type;
+
+typedef enum niti_act {
+    NITI_ACT_NONE = 0,
+    NITI_ACT_RELU = 1,
+    NITI_ACT_GELU = 2,   /* z (1 + erf(z / sqrt 2)) / 2 */
+    NITI_ACT_SILU = 3    /* z / (1 + exp(-z))           */
+} niti_act;
+
+/* Operation ids for niti_workspace_bytes, which takes M, N, K as below. */
+#define NITI_OP_RMSNORM_BWD 5   /* (M, D, -) */
+#define NITI_OP_LINEAR_FWD  6   /* (M, N, K) */
+#define NITI_OP_LINEAR_BWD  7   /* (M, N, K) */
+
+/* Root-mean-square norm with the residual's addition.  Per row of D elements
+ *     h = x + res,  rstd = 1 / sqrt(mean(h^2) + eps),  y = h * rstd * gain,
+ * with h held in 32 bits throughout.  Outputs, each optional (NULL):
+ *   h      the sum, in `type`;
+ *   q, scale (both or neither)   the codes and scales of the rows of y;
+ *   y      in `type`: the values that the codes stand for where q is given,
+ *          y itself otherwise;
+ *   rstd   [M], for the backward pass.
+ * res is optional; h and y may be x or res.  gain [D] has a type of its own.
+ * D >= 1, eps >= 0. */
+niti_status niti_rmsnorm_fwd(const void *x, int64_t ldx, const void *res, int64_t ldres, const void *gain,
+                             int gain_type, void *h, int64_t ldh, void *y, int64_t ldy, int8_t *q, int64_t ldq,
+                             float *scale, float *rstd, int64_t M, int64_t D, float eps, int type, void *stream);
+
+/* Its backward pass, for the gradient dy of y (the codes pass it straight
+ * through).  With xh = h * rstd and t = dy * gain,
+ *     dx = rstd * (t - xh * mean(t * xh)) + dh,   dgain = sum over rows of dy * xh,
+ * where h and rstd are those of the forward call (h = x when that had no
+ * residual) and dh, optional, is a gradient that reaches h another way.  dx is
+ * the gradient of x and of res alike, and may be dy or dh.  dgain [D] is float
+ * and overwritten; it is optional.  The order of its sums is fixed, so that
+ * results repeat.  Workspace: niti_workspace_bytes(NITI_OP_RMSNORM_BWD, NULL,
+ * M, D, 0), not needed without dgain. */
+niti_status niti_rmsnorm_bwd(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *gain,
+                             int gain_type, const float *rstd, const void *dh, int64_t lddh, void *dx, int64_t lddx,
+                             float *dgain, int64_t M, int64_t D, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Codes and scales of the rows of x [M][D]; y, optional, receives the values
+ * that they stand for, in `type`, and may be x.  D >= 1. */
+niti_status niti_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ldq, float *scale, void *y,
+                               int64_t ldy, int64_t M, int64_t D, niti_round_mode mode, uint64_t seed, uint32_t call,
+                               int type, void *stream);
+
+/* Product of int8 rows with its epilogue: a [M][K], b [N][K],
+ *     z = s_a[m] * s_b[n] * sum_k a[m][k] b[n][k] + bias[n],   out = act(z) + res,
+ * the sum exact in 32-bit integers.  s_a holds M scales, or one for all rows
+ * (s_a_n = 1), as a tensor with an exponent has it; s_b likewise N or 1.  bias
+ * [N] (its own type), res [M][N] and z [M][N] (the value before the
+ * activation, for the backward pass) are optional; res and z have out's type,
+ * and out may be res.  K in 0..131071 (longer sums could leave 32 bits:
+ * NITI_ERR_UNSUPPORTED).  Workspace: niti_workspace_bytes(NITI_OP_LINEAR_FWD,
+ * NULL, M, N, K); it may be NULL with 0 bytes, and such a call takes longer
+ * where the products are few and the sum is long. */
+niti_status niti_linear_fwd(const int8_t *a, int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b,
+                            int64_t ldb, const float *s_b, int64_t s_b_n, const void *bias, int bias_type, int act,
+                            const void *res, int64_t ldres, void *z, int64_t ldz, void *out, int64_t ldout, int64_t M,
+                            int64_t N, int64_t K, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Its backward pass, for the gradient dy of out (which is res's gradient as
+ * well).  With dz = dy * act'(z), formed in 32 bits,
+ *     dbias[n] = sum_m dz[m][n],
+ *     da[m][k] = r[m] * sum_n p[m][n] b[n][k],   p, r: codes and scales of the rows    of dz[m][n] * s_b[n],
+ *     db[n][k] = c[n] * sum_m q[m][n] a[m][k],   q, c: codes and scales of the columns of dz[m][n] * s_a[m]:
+ * the gradients of the values that a and b stand for, by two int8 products
+ * whose sums are exact.  Stochastic codes take their draws from index m * N + n, the
+ * rows' from the top 24 bits and the columns' from bits 8 to 31.  z is the
+ * forward call's and may be NULL when act is NITI_ACT_NONE.  da, db (in
+ * `type`) and dbias (float) are optional and overwritten.  M and N up to
+ * 131071.  Workspace: niti_workspace_bytes(NITI_OP_LINEAR_BWD, NULL, M, N, K). */
+niti_status niti_linear_bwd(const void *dy, int64_t lddy, const void *z, int64_t ldz, int act, const int8_t *a,
+                            int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b, int64_t ldb,
+                            const float *s_b, int64_t s_b_n, void *da, int64_t ldda, void *db, int64_t lddb,
+                            float *dbias, int64_t M, int64_t N, int64_t K, niti_round_mode mode, uint64_t seed,
+                            uint32_t call, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* One tensor of an optimiser's step: n elements, all arrays contiguous.  p is
+ * the parameter, g its gradient.  32-bit states: m and v are float, m_scale
+ * and v_scale are NULL.  8-bit states: m is int8 and v uint8, with one float
+ * scale per 256 consecutive elements in m_scale and v_scale (ceil(n / 256)
+ * each); a code c stands for m = sign(c) c^2 m_scale and v = c^4 v_scale, finer
+ * the smaller the value, down to 6e-5 of its block's largest in m and 2e-10 in
+ * v.  m_read and v_read are niti_adamw_read's outputs and otherwise unused. */
+typedef struct niti_adamw_tensor {
+    void *p;
+    const void *g;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+    void *m_read;
+    void *v_read;
+    int64_t n;
+} niti_adamw_tensor;
+
+/* One AdamW step over `count` tensors (a host array, read during the call):
+ *     g' = g * *grad_scale,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *     p = p - lr * weight_decay * p - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps).
+ * grad_scale is a device scalar (loss scale, clipping) or NULL for 1.  p and g
+ * have one type each for all tensors; m and v are used before they are
+ * rounded to codes.  state_bits is 32 or 8.  With 8: m_scale = max |m| / 127^2
+ * and v_scale = max v / 255^4 over a block, 0 with codes 0 where that maximum
+ * is below 2^-100; codes round sqrt(|m| / m_scale) and (v / v_scale)^(1/4) to
+ * nearest (NITI_ROUND_RTN) or as floor(. + u) (NITI_ROUND_SR), and a v above 0
+ * has at least code 1, so that no step divides by a state that was rounded
+ * away.  With blocks of all tensors counted through in order, element i of
+ * block k has draw number step * 2^40 + (256 k + i) / 2 + 1 of the stream of
+ * seed; its u is bits 0-15 (m) and 16-31 (v) of the draw where i is even,
+ * 32-47 and 48-63 where it is odd.  A block of m or v with
+ * a value that is not finite gets the scale NaN, and its parameters are NaN
+ * from the next step on (with 32-bit states only that element's is).  step >= 1,
+ * 0 <= beta < 1, eps >= 0. */
+niti_status niti_adamw_step(const niti_adamw_tensor *tensors, int64_t count, int p_type, int g_type, int state_bits,
+                            int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
+                            const float *grad_scale, niti_round_mode mode, uint64_t seed, void *stream);
+
+/* The values of 8-bit states, into each tensor's m_read and v_read (either
+ * may be NULL) of type `type`: for checkpoints and inspection. */
+niti_status niti_adamw_read(const niti_adamw_tensor *tensors, int64_t count, int type, void *stream);
 
 /* Size of niti_stats (128), for bindings. */
 size_t niti_stats_bytes(void);

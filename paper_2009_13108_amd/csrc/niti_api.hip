@@ -5,6 +5,7 @@
 
 #include <mutex>
 
+#include "linear.h"
 #include "niti_internal.h"
 
 // Temporary memory of niti_conv_bwd_weight_noalloc: one fixed array per GPU
@@ -174,7 +175,6 @@ WgradSetup wgrad_setup(const niti_conv_desc* d, int64_t P, int64_t Q) {
 }
 
 size_t niti_workspace_bytes(int op, const niti_conv_desc* d, int64_t M, int64_t N, int64_t K) {
-    (void)K;
     int64_t P = 0, Q = 0;
     if ((op == NITI_OP_CONV_FWD || op == NITI_OP_CONV_BWD_DATA || op == NITI_OP_CONV_BWD_WEIGHT) &&
         (!d || check_conv(d, &P, &Q) != NITI_OK))
@@ -196,6 +196,12 @@ size_t niti_workspace_bytes(int op, const niti_conv_desc* d, int64_t M, int64_t 
         }
         case NITI_OP_INT_CE_LOSS:
             return (M > 0 && N > 0) ? (size_t)round_up(M * N * 16, 256) : 0;
+        case NITI_OP_RMSNORM_BWD:
+            return rmsnorm_bwd_workspace(M, N);
+        case NITI_OP_LINEAR_FWD:
+            return linear_fwd_workspace(M, N, K);
+        case NITI_OP_LINEAR_BWD:
+            return linear_bwd_workspace(M, N, K);
         default:
             return 0;
     }

@@ -1,0 +1,181 @@
+// Shared pieces of the operators on int8 rows with one scale each: element
+// types, int8 codes of a float row, stochastic draws, activations.
+//
+// A row x is held as codes q and a scale: x ~ q * scale with
+//   top = max(max |x|, 2^-100), scale = top / 127, q = round(x * (127 / top)),
+// so that a row of zeros has a scale like any other and nothing divides by
+// zero.  A row with an infinity or a NaN has the scale NaN and codes 0: what
+// is computed from it is NaN, as it would be without the codes.
+#pragma once
+
+#include "niti_internal.h"
+
+namespace niti {
+
+typedef _Float16 f16;
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr float kTopMin = 0x1p-100f;
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+struct bf16 {
+    uint16_t bits;
+};
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(f16 v) { return (float)v; }
+__device__ __forceinline__ float to_f(bf16 v) { return __uint_as_float((uint32_t)v.bits << 16); }
+
+// Results are held in 32 bits up to the store, which rounds once, to nearest even.
+template <typename T>
+__device__ __forceinline__ T from_f(float v);
+template <>
+__device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ f16 from_f<f16>(float v) { return (f16)v; }
+template <>
+__device__ __forceinline__ bf16 from_f<bf16>(float v) {
+    return __builtin_bit_cast(bf16, (__bf16)v);
+}
+
+// N consecutive elements from any address (see load16_any).
+template <typename T, int N>
+__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+    T t[N];
+    __builtin_memcpy(t, p, sizeof(t));
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = to_f(t[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+    T t[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) t[i] = from_f<T>(v[i]);
+    __builtin_memcpy(p, t, sizeof(t));
+}
+// The first n of them (n >= N: all), zero for the others.
+template <typename T, int N>
+__device__ __forceinline__ void load_some(const T* p, int n, float (&v)[N]) {
+    if (n >= N) {
+        load_n(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = i < n ? to_f(p[i]) : 0.f;
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N]) {
+    if (n >= N) {
+        store_n(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (i < n) p[i] = from_f<T>(v[i]);
+}
+
+// Elements i .. i+N-1 of a vector of a type known at run time (gains and
+// biases, which are small; uniform).
+template <int N>
+__device__ __forceinline__ void load_typed(const void* p, int type, int64_t i, int n, float (&v)[N]) {
+    if (type == NITI_F32)
+        load_some((const float*)p + i, n, v);
+    else if (type == NITI_BF16)
+        load_some((const bf16*)p + i, n, v);
+    else
+        load_some((const f16*)p + i, n, v);
+}
+
+inline size_t type_size(int type) { return type == NITI_F32 ? 4 : 2; }
+inline bool valid_type(int type) { return type == NITI_F32 || type == NITI_BF16 || type == NITI_F16; }
+
+// |v| as an integer of the same order; every NaN is above infinity, so that a
+// maximum of these keeps what a floating maximum drops.
+__device__ __forceinline__ uint32_t mag_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Codes of one row (or column): the scale, and the factor that forms them.
+struct RowScale {
+    float scale;   // NaN for a row that is not finite
+    float inv;     // 0 for such a row
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t top_bits) {
+    RowScale r;
+    const bool bad = top_bits >= kInfBits;
+    const float top = fmaxf(__uint_as_float(top_bits), kTopMin);
+    r.scale = bad ? __uint_as_float(0x7FC00000u) : top / 127.f;
+    r.inv = bad ? 0.f : 127.f / top;
+    return r;
+}
+
+// Code of v, as a float in [-127, 127]; bad rows (inv 0) give 0 whatever v is.
+__device__ __forceinline__ float code_rtn(float v, float inv) {
+    const float r = rintf(v * inv);
+    return fminf(fmaxf(inv > 0.f ? r : 0.f, -127.f), 127.f);
+}
+// Stochastically: floor(v + u) is v on average over u in [0, 1).
+__device__ __forceinline__ float code_sr(float v, float inv, float u) {
+    const float r = floorf(v * inv + u);
+    return fminf(fmaxf(inv > 0.f ? r : 0.f, -127.f), 127.f);
+}
+// Uniform fractions of 24 bits from a draw.
+__device__ __forceinline__ float draw_hi(uint64_t r) { return (float)(uint32_t)(r >> 40) * 0x1p-24f; }
+__device__ __forceinline__ float draw_lo(uint64_t r) { return (float)((uint32_t)(r >> 8) & 0xFFFFFFu) * 0x1p-24f; }
+
+// Four codes in a word, lowest first.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    return ((uint32_t)(int)a & 0xFFu) | (((uint32_t)(int)b & 0xFFu) << 8) | (((uint32_t)(int)c & 0xFFu) << 16) |
+           ((uint32_t)(int)d << 24);
+}
+
+__device__ __forceinline__ float wave_sum_f32(float v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+    return v;
+}
+
+// Activations and their derivatives.  Below -80 a sigmoid is under 2^-115 and
+// its argument is held there, so that an infinity gives the limit and no NaN.
+__device__ __forceinline__ float act_value(int act, float z) {
+    if (act == NITI_ACT_RELU) return z < 0.f ? 0.f : z;
+    if (act == NITI_ACT_GELU) {
+        const float c = z < -40.f ? -40.f : z;
+        return 0.5f * c * (1.f + erff(c * 0.70710678118654752f));
+    }
+    if (act == NITI_ACT_SILU) {
+        const float c = z < -80.f ? -80.f : z;
+        return c / (1.f + expf(-c));
+    }
+    return z;
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+    if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+    if (act == NITI_ACT_GELU) {
+        const float c = z < -40.f ? -40.f : (z > 40.f ? 40.f : z);
+        return 0.5f * (1.f + erff(c * 0.70710678118654752f)) + c * expf(-0.5f * c * c) * 0.39894228040143268f;
+    }
+    if (act == NITI_ACT_SILU) {
+        const float c = z < -80.f ? -80.f : (z > 80.f ? 80.f : z);
+        const float s = 1.f / (1.f + expf(-c));
+        return s * (1.f + c * (1.f - s));
+    }
+    return 1.f;
+}
+
+constexpr int64_t kMaxLd = (int64_t)1 << 22;   // row strides are below this
+constexpr int64_t kMaxDim = (int64_t)1 << 31;
+constexpr int64_t kMaxSum = (int64_t)1 << 17;   // shorter sums of int8 products stay in int32
+
+// A row stride: 0 only for operands that are read.
+inline bool bad_ld(int64_t ld, int64_t cols, bool out) {
+    return ld >= kMaxLd || ld < 0 || (ld < cols && (out || ld != 0));
+}
+
+// Calls f(T()) with the element type.
+template <typename F>
+inline hipError_t by_type(int type, F f) {
+    if (type == NITI_F32) return f(float());
+    if (type == NITI_BF16) return f(bf16());
+    return f(f16());
+}
+
+}  // namespace niti

@@ -31,6 +31,18 @@ OP_CONV_FWD = 1
 OP_CONV_BWD_DATA = 2
 OP_CONV_BWD_WEIGHT = 3
 OP_INT_CE_LOSS = 4
+OP_RMSNORM_BWD = 5
+OP_LINEAR_FWD = 6
+OP_LINEAR_BWD = 7
+
+F32 = 0
+BF16 = 1
+F16 = 2
+
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU = 2
+ACT_SILU = 3
 
 STATS_BYTES = 128
 STATS_DTYPE = np.dtype([
@@ -87,7 +99,8 @@ EXPORTS = [
     "niti_round_psr", "niti_int_ce_loss_grad", "niti_sgd_update", "niti_workspace_bytes",
     "niti_status_str", "niti_quantize_u8", "niti_maxpool2_fwd", "niti_maxpool2_bwd",
     "niti_relu_mask", "niti_dropout_fwd", "niti_dropout_bwd", "niti_stats_bytes", "niti_timing_enable", "niti_timing_read", "niti_timing_record",
-    "niti_mfma_loop",
+    "niti_mfma_loop", "niti_rmsnorm_fwd", "niti_rmsnorm_bwd", "niti_quantize_rows", "niti_linear_fwd",
+    "niti_linear_bwd", "niti_adamw_step", "niti_adamw_read",
 ]
 
 TIMING_IGEMM = 0
@@ -106,7 +119,7 @@ def lib():
             if not os.path.exists(LIB_PATH):
                 raise RuntimeError("libniti.so is not built (%s); run __graft_entry__.build()" % LIB_PATH)
             L = ctypes.CDLL(LIB_PATH)
-            P, I64, I, Z = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+            P, I64, I, Z, D = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_double
             sig = {
                 "niti_gemm_fwd": [P, P, P, I64, I64, I64, P, P, P, I, I, I, P, P],
                 "niti_conv_fwd": [P, P, P, P, P, P, P, I, I, P, P, Z, P],
@@ -128,6 +141,15 @@ def lib():
                 "niti_timing_read": [I, P, P],
                 "niti_timing_record": [I64, P, P, P],
                 "niti_mfma_loop": [I64, I64, P, P],
+                "niti_rmsnorm_fwd": [P, I64, P, I64, P, I, P, I64, P, I64, P, I64, P, P, I64, I64, ctypes.c_float, I, P],
+                "niti_rmsnorm_bwd": [P, I64, P, I64, P, I, P, P, I64, P, I64, P, I64, I64, I, P, Z, P],
+                "niti_quantize_rows": [P, I64, P, I64, P, P, I64, I64, I64, I, ctypes.c_uint64, ctypes.c_uint32, I, P],
+                "niti_linear_fwd": [P, I64, P, I64, P, I64, P, I64, P, I, I, P, I64, P, I64, P, I64, I64, I64, I64, I, P, Z,
+                                    P],
+                "niti_linear_bwd": [P, I64, P, I64, I, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I,
+                                    ctypes.c_uint64, ctypes.c_uint32, I, P, Z, P],
+                "niti_adamw_step": [P, I64, I, I, I, I64, D, D, D, D, D, P, I, ctypes.c_uint64, P],
+                "niti_adamw_read": [P, I64, I, P],
             }
             for name, args in sig.items():
                 f = getattr(L, name)
@@ -556,3 +578,239 @@ def dropout_bwd(dy, keep, dx, stream=None):
     if not (dy.numel() == dx.numel() == keep.numel()):
         raise ValueError("dropout_bwd: sizes differ")
     _run("niti_dropout_bwd", _ptr(dy), _ptr(keep), _ptr(dx), dy.numel(), _stream(stream))
+
+
+# ------------------------------------------------------------------ operators on int8 rows with a scale each
+# Matrices may have any row stride (columns contiguous).  A call of one token
+# takes a few microseconds on the GPU, so the checks are as short as those above.
+_types = {}
+
+
+def _type_of(dtype, what):
+    if not _types:
+        torch = _torch()
+        _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    t = _types.get(dtype)
+    if t is None:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (what, dtype))
+    return t
+
+
+def _mat(t, dtype, rows, cols, what, out=False):
+    """(address, row stride) of a matrix of the given type and shape; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a device tensor" % what)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if t.shape != (rows, cols):
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), (rows, cols)))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s must have contiguous columns" % what)
+    if rows < 2 or cols == 0:
+        ld = cols
+    elif ld < cols and (out or ld != 0):
+        raise ValueError("%s has overlapping rows" % what)
+    return t.data_ptr(), ld
+
+
+def _vec(t, n, what, dtype=None, one=False):
+    """Address of a contiguous vector of n elements (or one, where that is allowed); None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a device tensor" % what)
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    k = t.numel()
+    if (k != n and not (one and k == 1)) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous with %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def _same_device(x, *others):
+    """All tensors of a call on the device of its first and on the current one, whose stream it uses."""
+    dev = x.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors on %s and %s in one call" % (dev, t.device))
+
+
+def _matrix(x, what):
+    """Shape of a call's first operand."""
+    _torch()
+    if not isinstance(x, _Tensor) or not x.is_cuda:
+        raise TypeError("%s must be a device tensor" % what)
+    if x.dim() != 2:
+        raise ValueError("%s must be a matrix" % what)
+    return x.shape
+
+
+def _ws_args(ws):
+    if ws is None:
+        return None, 0
+    _dev(ws, _torch_mod.uint8, "ws")
+    return ws.data_ptr(), ws.numel()
+
+
+def rmsnorm_fwd(x, gain, res=None, h=None, y=None, q=None, scale=None, rstd=None, eps=1e-6, stream=None):
+    """h = x + res; y = h / sqrt(mean(h^2) + eps) * gain by rows; q, scale: y as
+    int8 rows, and y then the values that they stand for (niti_rmsnorm_fwd)."""
+    M, D = _matrix(x, "x")
+    f32, dt = _torch_mod.float32, x.dtype
+    px, ldx = _mat(x, dt, M, D, "x")
+    pr, ldr = _mat(res, dt, M, D, "res")
+    ph, ldh = _mat(h, dt, M, D, "h", True)
+    py, ldy = _mat(y, dt, M, D, "y", True)
+    pq, ldq = _mat(q, _torch_mod.int8, M, D, "q", True)
+    _same_device(x, res, gain, h, y, q, scale, rstd)
+    _run("niti_rmsnorm_fwd", px, ldx, pr, ldr, _vec(gain, D, "gain"), _type_of(gain.dtype, "gain"), ph, ldh, py, ldy, pq, ldq,
+         _vec(scale, M, "scale", f32), _vec(rstd, M, "rstd", f32), M, D, float(eps), _type_of(dt, "x"), _stream(stream))
+
+
+def rmsnorm_bwd(dy, h, gain, rstd, dx, dgain=None, ws=None, dh=None, stream=None):
+    """Gradients of rmsnorm_fwd's input (dx, plus dh that reaches h another
+    way) and gain; ws as workspace_bytes(OP_RMSNORM_BWD, None, M, D) when dgain is wanted."""
+    M, D = _matrix(dy, "dy")
+    f32, dt = _torch_mod.float32, dy.dtype
+    pdy, lddy = _mat(dy, dt, M, D, "dy")
+    ph, ldh = _mat(h, dt, M, D, "h")
+    pdh, lddh = _mat(dh, dt, M, D, "dh")
+    pdx, lddx = _mat(dx, dt, M, D, "dx", True)
+    pws, nws = _ws_args(ws)
+    _same_device(dy, h, gain, rstd, dx, dgain, ws, dh)
+    _run("niti_rmsnorm_bwd", pdy, lddy, ph, ldh, _vec(gain, D, "gain"), _type_of(gain.dtype, "gain"), _vec(rstd, M, "rstd", f32),
+         pdh, lddh, pdx, lddx, _vec(dgain, D, "dgain", f32), M, D, _type_of(dt, "dy"), pws, nws, _stream(stream))
+
+
+def quantize_rows(x, q, scale, y=None, mode=RTN, seed=0, call=0, stream=None):
+    """x as int8 rows with a scale each; y: the values that they stand for (niti_quantize_rows)."""
+    M, D = _matrix(x, "x")
+    px, ldx = _mat(x, x.dtype, M, D, "x")
+    pq, ldq = _mat(q, _torch_mod.int8, M, D, "q", True)
+    py, ldy = _mat(y, x.dtype, M, D, "y", True)
+    _same_device(x, q, scale, y)
+    _run("niti_quantize_rows", px, ldx, pq, ldq, _vec(scale, M, "scale", _torch_mod.float32), py, ldy, M, D, int(mode),
+         int(seed) & 0xFFFFFFFFFFFFFFFF, int(call) & 0xFFFFFFFF, _type_of(x.dtype, "x"), _stream(stream))
+
+
+def linear_fwd(a, b, out, s_a, s_b, bias=None, act=ACT_NONE, res=None, z=None, ws=None, stream=None):
+    """out = act(s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n]) + res; z: the
+    value before the activation; ws as workspace_bytes(OP_LINEAR_FWD, None, M, N, K), or None (niti_linear_fwd)."""
+    M, K = _matrix(a, "a")
+    N = b.shape[0] if isinstance(b, _Tensor) and b.dim() == 2 else -1
+    i8, f32, dt = _torch_mod.int8, _torch_mod.float32, out.dtype
+    pa, lda = _mat(a, i8, M, K, "a")
+    pb, ldb = _mat(b, i8, N, K, "b")
+    po, ldo = _mat(out, dt, M, N, "out", True)
+    pr, ldr = _mat(res, dt, M, N, "res")
+    pz, ldz = _mat(z, dt, M, N, "z", True)
+    pws, nws = _ws_args(ws)
+    _same_device(a, b, out, s_a, s_b, bias, res, z, ws)
+    _run("niti_linear_fwd", pa, lda, _vec(s_a, M, "s_a", f32, True), s_a.numel(), pb, ldb, _vec(s_b, N, "s_b", f32, True),
+         s_b.numel(), _vec(bias, N, "bias"), F32 if bias is None else _type_of(bias.dtype, "bias"), int(act), pr, ldr, pz, ldz,
+         po, ldo, M, N, K, _type_of(dt, "out"), pws, nws, _stream(stream))
+
+
+def linear_bwd(dy, a, b, s_a, s_b, ws, z=None, act=ACT_NONE, da=None, db=None, dbias=None, mode=RTN, seed=0, call=0,
+               stream=None):
+    """Gradients of the values that a and b stand for and of the bias, by int8
+    products; ws as workspace_bytes(OP_LINEAR_BWD, None, M, N, K) (niti_linear_bwd)."""
+    M, N = _matrix(dy, "dy")
+    K = a.shape[1] if isinstance(a, _Tensor) and a.dim() == 2 else -1
+    i8, f32, dt = _torch_mod.int8, _torch_mod.float32, dy.dtype
+    pdy, lddy = _mat(dy, dt, M, N, "dy")
+    pz, ldz = _mat(z, dt, M, N, "z")
+    pa, lda = _mat(a, i8, M, K, "a")
+    pb, ldb = _mat(b, i8, N, K, "b")
+    pda, ldda = _mat(da, dt, M, K, "da", True)
+    pdb, lddb = _mat(db, dt, N, K, "db", True)
+    pws, nws = _ws_args(ws)
+    _same_device(dy, a, b, s_a, s_b, ws, z, da, db, dbias)
+    _run("niti_linear_bwd", pdy, lddy, pz, ldz, int(act), pa, lda, _vec(s_a, M, "s_a", f32, True), s_a.numel(), pb, ldb,
+         _vec(s_b, N, "s_b", f32, True), s_b.numel(), pda, ldda, pdb, lddb, _vec(dbias, N, "dbias", f32), M, N, K, int(mode),
+         int(seed) & 0xFFFFFFFFFFFFFFFF, int(call) & 0xFFFFFFFF, _type_of(dt, "dy"), pws, nws, _stream(stream))
+
+
+ADAMW_BLOCK = 256   # consecutive elements that share a scale in an 8-bit state
+
+
+class AdamWTensor(ctypes.Structure):
+    """niti_adamw_tensor."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "m_read", "v_read")] + \
+               [("n", ctypes.c_int64)]
+
+
+class AdamWPlan:
+    """The tensors of an optimiser, checked and marshalled once (adamw_plan)."""
+    __slots__ = ("table", "count", "p_type", "g_type", "read_type", "bits", "tensors")
+
+
+def _flat(t, n, dtype, what):
+    _dev(t, dtype, what)
+    if t.numel() != n:
+        raise ValueError("%s has %d elements, expected %d" % (what, t.numel(), n))
+    return t.data_ptr()
+
+
+def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, m_read=None, v_read=None):
+    """The tensors that adamw_step updates: lists of parameters, gradients and
+    states, kept by the plan.  States are float32, or int8 (m) and uint8 (v)
+    with one float32 scale per 256 elements in m_scale and v_scale; m_read and
+    v_read are then what adamw_read fills.  Calls use the tensors' memory as it
+    is at the call: gradients are written into the same tensors every step."""
+    torch = _torch()
+    count = len(params)
+    plan = AdamWPlan()
+    plan.bits = 32 if m_scale is None else 8
+    if (m_scale is None) != (v_scale is None):
+        raise ValueError("adamw_plan: give both scales or neither")
+    if plan.bits == 32 and (m_read is not None or v_read is not None):
+        raise ValueError("adamw_plan: 32-bit states are read as they are")
+    lists = {"grads": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "m_read": m_read, "v_read": v_read}
+    for name, x in lists.items():
+        if x is not None and len(x) != count:
+            raise ValueError("adamw_plan: %d params and %d %s" % (count, len(x), name))
+    p_dt = params[0].dtype if count else torch.float32
+    g_dt = grads[0].dtype if count else torch.float32
+    r_dt = next((x[0].dtype for x in (m_read, v_read) if x), torch.float32)
+    m_dt, v_dt = (torch.float32, torch.float32) if plan.bits == 32 else (torch.int8, torch.uint8)
+    plan.p_type, plan.g_type, plan.read_type = (_type_of(d, w) for d, w in ((p_dt, "params"), (g_dt, "grads"), (r_dt, "m_read")))
+    plan.table = (AdamWTensor * max(count, 1))()
+    plan.count = count
+    plan.tensors = [list(params)] + [list(x) for x in lists.values() if x is not None]   # keeps their memory
+    for i in range(count):
+        n = params[i].numel()
+        blocks = -(-n // ADAMW_BLOCK)
+        row = plan.table[i]
+        row.n = n
+        _same_device(params[0], params[i], *(x[i] for x in lists.values() if x is not None))
+        row.p = _flat(params[i], n, p_dt, "params")
+        row.g = _flat(grads[i], n, g_dt, "grads")
+        row.m = _flat(m[i], n, m_dt, "m")
+        row.v = _flat(v[i], n, v_dt, "v")
+        if plan.bits == 8:
+            row.m_scale = _flat(m_scale[i], blocks, torch.float32, "m_scale")
+            row.v_scale = _flat(v_scale[i], blocks, torch.float32, "v_scale")
+            row.m_read = None if m_read is None else _flat(m_read[i], n, r_dt, "m_read")
+            row.v_read = None if v_read is None else _flat(v_read[i], n, r_dt, "v_read")
+    return plan
+
+
+def adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, mode=RTN, seed=0,
+               stream=None):
+    """One AdamW step (number `step`, from 1 on) of all tensors of a plan;
+    grad_scale: a float32 device scalar that multiplies the gradients."""
+    _run("niti_adamw_step", plan.table, plan.count, plan.p_type, plan.g_type, plan.bits, int(step), float(lr), float(beta1),
+         float(beta2), float(eps), float(weight_decay), _vec(grad_scale, 1, "grad_scale", _torch().float32), int(mode),
+         int(seed) & 0xFFFFFFFFFFFFFFFF, _stream(stream))
+
+
+def adamw_read(plan, stream=None):
+    """The values of a plan's 8-bit states, into its m_read and v_read."""
+    _torch()
+    if plan.bits != 8:
+        raise ValueError("adamw_read: 32-bit states are read as they are")
+    _run("niti_adamw_read", plan.table, plan.count, plan.read_type, _stream(stream))

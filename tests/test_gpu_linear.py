@@ -1,0 +1,323 @@
+"""Product of int8 rows with its epilogue, and its gradients, against 64-bit
+forms (tests/scaled_ref.py has the bounds)."""
+import pytest
+import torch
+
+import scaled_ref as R
+from helpers import say
+from paper_2009_13108_amd import niti
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+ACTS = {"none": niti.ACT_NONE, "relu": niti.ACT_RELU, "gelu": niti.ACT_GELU, "silu": niti.ACT_SILU}
+
+
+def codes(m, k, seed, pad=0):
+    """Int8 codes in rows of stride k + pad."""
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-127, 128, (m, k + pad), generator=g, dtype=torch.int8).cuda()[:, :k]
+
+
+def floats(*shape, seed, dtype=F32, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * scale).to(dtype).cuda()
+
+
+def row_scales(n, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    return ((0.5 + torch.rand(n, generator=g)) / (73 * max(k, 1) ** 0.5)).cuda()   # sums of order one (codes of deviation 73)
+
+
+def forward64(a, b, s_a, s_b, bias, act, res):
+    acc = a.double().cpu() @ b.double().cpu().t()
+    s = acc * (s_a.double().cpu().view(-1, 1) * s_b.double().cpu().view(1, -1))
+    z = s + (bias.double().cpu() if bias is not None else 0)
+    mag = s.abs() + (bias.double().cpu().abs() if bias is not None else 0)
+    zb = 5 * R.U32 * mag                      # int to float, two products, one sum
+    out = R.act(act, z) + (res.double().cpu() if res is not None else 0)
+    # slopes are at most 1.13; an activation's own evaluation is good to 8 U32 of |z|
+    ob = 1.2 * zb + 8 * R.U32 * z.abs() + R.U32 * out.abs()
+    return z, zb, out, ob
+
+
+def run_forward(m, n, k, dtype, act="none", bias=True, res=True, pad=(0, 0), one=(False, False), ws=True, seed=1):
+    a, b = codes(m, k, seed, pad[0]), codes(n, k, seed + 1, pad[1])
+    s_a, s_b = row_scales(1 if one[0] else m, k, seed + 2) * 4, row_scales(1 if one[1] else n, 1, seed + 3) * 18
+    bi = floats(n, seed=seed + 4, dtype=dtype) if bias else None
+    re = floats(m, n, seed=seed + 5, dtype=dtype) if res else None
+    out, io = R.guarded(m, n, dtype)
+    z, iz = R.guarded(m, n, dtype, pad=7)
+    space = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_FWD, None, m, n, k)) if ws else None
+    niti.linear_fwd(a, b, out, s_a, s_b, bias=bi, act=ACTS[act], res=re, z=z, ws=space)
+    z64, zb, o64, ob = forward64(a, b, s_a, s_b, bi, act, re)
+    R.close(z, z64, zb, dtype, "z")
+    R.close(out, o64, ob, dtype, "out")
+    io(), iz()
+
+
+# one token to many, sums from nothing on, around the tiles' edges (16, 32, 64, 128, 256) and their steps
+SIZES = [(1, 1, 1), (1, 1, 0), (5, 3, 15), (1, 4096, 4096), (1, 1000, 784), (2, 33, 16), (3, 17, 4099), (8, 128, 64), (16, 16, 64),
+         (17, 31, 63), (31, 40, 129), (32, 256, 9216), (33, 64, 1111), (64, 64, 64), (65, 129, 65), (100, 84, 120), (127, 255, 48),
+         (128, 128, 128), (129, 513, 4096), (200, 10, 8192), (256, 256, 80), (257, 300, 272), (500, 1000, 304), (1000, 1500, 1111),
+         (1031, 768, 512), (2048, 1024, 640)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_forward(m, n, k, dtype):
+    say("linear_fwd", m, n, k, dtype)
+    run_forward(m, n, k, dtype, act="gelu" if dtype is F32 else "silu")
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("m,n,k", [(1, 200, 256), (40, 72, 96), (300, 260, 128)])
+def test_forward_epilogues(m, n, k, dtype, act):
+    say("linear_fwd", m, n, k, dtype, act)
+    for bias in (False, True):
+        for res in (False, True):
+            run_forward(m, n, k, dtype, act, bias, res)
+
+
+@pytest.mark.parametrize("pad", [(0, 3), (1, 0), (5, 7), (16, 48), (16, 1)])
+@pytest.mark.parametrize("m,n,k", [(1, 130, 144), (7, 96, 100), (70, 130, 256), (300, 256, 512), (520, 520, 1000)])
+def test_forward_strides(m, n, k, pad):
+    say("linear_fwd strides", m, n, k, pad)
+    run_forward(m, n, k, BF16, pad=pad)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 64, 64), (50, 70, 80), (300, 300, 256)])
+def test_forward_one_scale(m, n, k):
+    for one in ((True, False), (False, True), (True, True)):
+        run_forward(m, n, k, F32, one=one)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 16, 65536), (4, 10, 40000), (60, 30, 20000), (130, 200, 8192), (1, 1, 131071)])
+def test_forward_long_sums(m, n, k):
+    """Few products and a long sum, with a workspace and without one."""
+    say("linear_fwd long", m, n, k)
+    run_forward(m, n, k, F32, ws=True)
+    run_forward(m, n, k, F32, ws=False)
+
+
+@pytest.mark.parametrize("m,n", [(1, 3), (20, 40), (140, 130)])
+def test_forward_largest_sum(m, n):
+    """131071 products of -128 * -128 and -128 * 127: the ends of what int32 holds, exactly."""
+    k = 131071
+    a = torch.full((m, k), -128, dtype=torch.int8, device="cuda")
+    b = torch.full((n, k), -128, dtype=torch.int8, device="cuda")
+    b[1:2] = 127
+    one = torch.ones(1, device="cuda")
+    out = torch.empty(m, n, device="cuda")
+    niti.linear_fwd(a, b, out, one, one)
+    want = torch.full((m, n), float(k * 16384))
+    want[:, 1] = -float(k * 128 * 127)
+    assert torch.equal(out.cpu(), want)   # 2^14 (2^17 - 1) rounds to 2^31 in 32 bits on both sides
+
+
+def test_forward_special_values():
+    m, n, k = 70, 90, 100
+    a, b = codes(m, k, 1), codes(n, k, 2)
+    s_a, s_b = row_scales(m, k, 3), row_scales(n, 1, 4)
+    s_a[5] = float("nan")                                   # a row that was not finite
+    a[6] = 0                                                # an empty row
+    bias, res = floats(n, seed=5), floats(m, n, seed=6)
+    bias[3], res[7, 8], res[9, 9] = float("-inf"), float("nan"), float("inf")
+    out = torch.empty(m, n, device="cuda")
+    for act in ACTS:
+        niti.linear_fwd(a, b, out, s_a, s_b, bias=bias, act=ACTS[act], res=res)
+        o = out.cpu()
+        assert torch.isnan(o[5]).all() and torch.isnan(o[7, 8])
+        rest = torch.ones(m, n, dtype=torch.bool)
+        rest[5] = False
+        rest[7, 8] = rest[9, 9] = False
+        rest[:, 3] = False
+        assert torch.isfinite(o[rest]).all()
+        col = torch.tensor([i for i in range(m) if i != 5])
+        if act == "none":
+            assert (o[col, 3] == float("-inf")).all()
+        else:                                                # act(-inf) is 0
+            assert torch.allclose(o[col, 3], res.cpu()[col, 3], atol=1e-30)
+        assert float(o[9, 9]) == float("inf")
+
+
+def test_out_over_res_and_no_work():
+    a, b = codes(33, 64, 1), codes(48, 64, 2)
+    s_a, s_b = row_scales(33, 64, 3), row_scales(48, 1, 4)
+    res = floats(33, 48, seed=5, dtype=BF16)
+    out = torch.empty_like(res)
+    niti.linear_fwd(a, b, out, s_a, s_b, res=res)
+    niti.linear_fwd(a, b, res, s_a, s_b, res=res)
+    assert torch.equal(out, res)
+    row = floats(1, 48, seed=6, dtype=BF16)
+    o2 = torch.empty_like(out)
+    niti.linear_fwd(a, b, out, s_a, s_b, res=row.expand(33, 48))       # stride 0
+    niti.linear_fwd(a, b, o2, s_a, s_b, res=row.repeat(33, 1))
+    assert torch.equal(out, o2)
+    niti.linear_fwd(a[:0], b, out[:0], s_a[:0], s_b)
+    niti.linear_fwd(a, b[:0], out[:, :0], s_a, s_b[:0])
+
+
+def test_product_past_32_bit_offsets():
+    """Output and operand offsets beyond 2^31 bytes: rows far apart in a large buffer."""
+    m, n, k = 600, 64, 64
+    ld = (1 << 22) - 16
+    big = torch.empty(m * ld, dtype=torch.int8, device="cuda")          # 2.5 GB
+    a = big.as_strided((m, k), (ld, 1))
+    small = codes(m, k, 1)
+    a.copy_(small)
+    b, s_a, s_b = codes(n, k, 2), row_scales(m, k, 3), row_scales(n, 1, 4)
+    want, out = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+    niti.linear_fwd(small, b, want, s_a, s_b)
+    niti.linear_fwd(a, b, out, s_a, s_b)
+    assert torch.equal(out, want)
+    wide = big.view(F32)[: m * (ld // 4)].as_strided((m, n), (ld // 4, 1))
+    niti.linear_fwd(small, b, wide, s_a, s_b)
+    assert torch.equal(wide.contiguous(), want)
+
+
+# ------------------------------------------------------------------ gradients
+def codes64(x, scale, u):
+    """Codes in 64 bits, and where a code's argument is too near a tie to tell."""
+    r = x / scale[:, None]
+    if u is None:
+        return torch.round(r).clamp(-127, 127), ((r - torch.floor(r)) - 0.5).abs() < R.CODE_SLACK
+    f = r + u
+    return torch.floor(f).clamp(-127, 127), (f - torch.round(f)).abs() < R.CODE_SLACK
+
+
+def backward64(dy, z, act, a, b, s_a, s_b, u=None, v=None):
+    dy, a, b = (t.double().cpu() for t in (dy, a, b))
+    s_a, s_b = s_a.double().cpu().expand(a.shape[0]), s_b.double().cpu().expand(b.shape[0])
+    dz = dy * R.slope(act, z.double().cpu()) if act != "none" else dy
+    x = dz * s_b
+    r = R.scales(x)
+    p, near = codes64(x, r, u)
+    da = r[:, None] * (p @ b)
+    # the scale's error (40 U32, and 8 U32 of dy: a slope near its zero is a
+    # difference of terms of order one), and one step for each code that a tie leaves open
+    dab = 40 * R.U32 * da.abs() + r[:, None] * (near.double() @ b.abs()) + 8 * R.U32 * R.scales(dy * s_b)[:, None] * (p @ b).abs()
+    x = (dz * s_a[:, None]).t()
+    c = R.scales(x)
+    q, near = codes64(x, c, v)
+    db = c[:, None] * (q @ a)
+    dbb = 40 * R.U32 * db.abs() + c[:, None] * (near.double() @ a.abs()) + \
+        8 * R.U32 * R.scales((dy * s_a[:, None]).t())[:, None] * (q @ a).abs()
+    return da, dab, db, dbb, dz.sum(dim=0), 80 * R.U32 * dz.abs().sum(dim=0) + 8 * R.U32 * dy.abs().sum(dim=0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("m,n,k,act,mode", [
+    (1, 1, 1, "none", "rtn"), (1, 300, 200, "silu", "sr"), (5, 33, 17, "gelu", "rtn"), (64, 64, 64, "relu", "sr"),
+    (100, 257, 130, "silu", "rtn"), (129, 1000, 784, "gelu", "sr"), (700, 128, 256, "none", "sr"), (1100, 600, 96, "silu", "rtn"),
+    (31, 2050, 64, "relu", "rtn"), (40, 4100, 48, "none", "rtn"), (20, 17000, 40, "silu", "sr"), (513, 512, 512, "gelu", "rtn")])
+def test_backward(m, n, k, act, mode, dtype):
+    say("linear_bwd", m, n, k, act, mode, dtype)
+    a, b = codes(m, k, 1, pad=k % 3), codes(n, k, 2)
+    s_a, s_b = row_scales(m, k, 3), row_scales(n, 1, 4)
+    dy, z = floats(m, n, seed=5, dtype=dtype), floats(m, n, seed=6, dtype=dtype, scale=1.5)
+    da, ia = R.guarded(m, k, dtype)
+    db, ib = R.guarded(n, k, dtype)
+    dbias = torch.empty(n, device="cuda")
+    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, m, n, k))
+    kw = dict(z=z if act != "none" else None, act=ACTS[act], mode=niti.SR if mode == "sr" else niti.RTN, seed=77, call=5)
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, da=da, db=db, dbias=dbias, **kw)
+    u = v = None
+    if mode == "sr":
+        r = R.draws(77, 5, m * n)
+        u, v = R.field(r, 40, 24).view(m, n), R.field(r, 8, 24).view(m, n).t()
+    wa, ba, wb, bb, wd, bd = backward64(dy, z, act, a, b, s_a, s_b, u, v)
+    R.close(da, wa, ba, dtype, "da")
+    R.close(db, wb, bb, dtype, "db")
+    R.close(dbias, wd, bd, what="dbias")
+    ia(), ib()
+    # each alone gives the same
+    ws.random_(0, 256)
+    one, two, three = torch.empty(m, k, dtype=dtype, device="cuda"), torch.empty(n, k, dtype=dtype, device="cuda"), torch.empty_like(dbias)
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, da=one, **kw)
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, db=two, **kw)
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, dbias=three, **kw)
+    assert torch.equal(one, da) and torch.equal(two, db) and torch.equal(three, dbias)
+
+
+def test_backward_against_differences():
+    """Directional differences of the 64-bit forward pass; the int8 products are
+    off by at most half a step of the error's codes."""
+    m, n, k = 24, 40, 56
+    a, b = codes(m, k, 1), codes(n, k, 2)
+    s_a, s_b = row_scales(m, k, 3), row_scales(n, 1, 4)
+    dy, bias = floats(m, n, seed=5), floats(n, seed=6)
+    z, out = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+    da, db, dbias = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda")
+    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, m, n, k))
+    for act in ACTS:
+        niti.linear_fwd(a, b, out, s_a, s_b, bias=bias, act=ACTS[act], z=z)
+        niti.linear_bwd(dy, a, b, s_a, s_b, ws, z=z, act=ACTS[act], da=da, db=db, dbias=dbias)
+        av, bv = a.double().cpu() * s_a.double().cpu()[:, None], b.double().cpu() * s_b.double().cpu()[:, None]
+        bias64, dy64 = bias.double().cpu(), dy.double().cpu()
+
+        def loss(x, w, c):
+            return (R.act(act, x @ w.t() + c) * dy64).sum()
+        dz = dy64 * R.slope(act, z.double().cpu())
+        half_a = 0.5 * R.scales(dz * s_b.double().cpu())[:, None] * b.double().cpu().abs().sum(dim=0)
+        half_b = 0.5 * R.scales((dz * s_a.double().cpu()[:, None]).t())[:, None] * a.double().cpu().abs().sum(dim=0)
+        for seed in range(3):
+            g = torch.Generator().manual_seed(seed)
+            va, vb = (torch.randn(t.shape, generator=g, dtype=torch.float64) for t in (av, bv))
+            vc = torch.randn(n, generator=g, dtype=torch.float64)
+            e = 1e-6
+            for got, v, room, want in (
+                    (da, va, half_a, (loss(av + e * va, bv, bias64) - loss(av - e * va, bv, bias64)) / (2 * e)),
+                    (db, vb, half_b, (loss(av, bv + e * vb, bias64) - loss(av, bv - e * vb, bias64)) / (2 * e)),
+                    (dbias, vc, torch.zeros(n, dtype=torch.float64),
+                     (loss(av, bv, bias64 + e * vc) - loss(av, bv, bias64 - e * vc)) / (2 * e))):
+                off = abs(float((got.double().cpu() * v).sum() - want))
+                # (a ReLU's kink inside the difference: none of these z is that near to zero)
+                assert off <= float((room * v.abs()).sum()) * 1.01 + 1e-4 * max(1.0, abs(float(want))), (act, off)
+
+
+def test_backward_special_rows():
+    """Empty rows and columns of the error, a row that is not finite, no rows at all."""
+    m, n, k = 50, 70, 32
+    a, b = codes(m, k, 1), codes(n, k, 2)
+    s_a, s_b = row_scales(m, k, 3), row_scales(n, 1, 4)
+    dy = floats(m, n, seed=5)
+    dy[3], dy[:, 4] = 0, 0
+    da, db, dbias = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda")
+    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, m, n, k))
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, da=da, db=db, dbias=dbias)
+    assert (da[3] == 0).all() and (db[4] == 0).all() and float(dbias[4]) == 0
+    assert torch.isfinite(da).all() and torch.isfinite(db).all()
+    dy[7, 9] = float("inf")
+    niti.linear_bwd(dy, a, b, s_a, s_b, ws, da=da, db=db, dbias=dbias)
+    assert torch.isnan(da[7]).all() and torch.isnan(db[9]).all() and not torch.isfinite(dbias[9])
+    ok_m, ok_n = [i for i in range(m) if i != 7], [i for i in range(n) if i != 9]
+    assert torch.isfinite(da[ok_m]).all() and torch.isfinite(db[ok_n]).all() and torch.isfinite(dbias[ok_n]).all()
+    db.fill_(5), dbias.fill_(5)
+    niti.linear_bwd(dy[:0], a[:0], b, s_a[:0], s_b, ws, da=da[:0], db=db, dbias=dbias)
+    assert (db == 0).all() and (dbias == 0).all()
+
+
+def test_refusals():
+    a, b, out = codes(4, 16, 1), codes(6, 16, 2), torch.empty(4, 6, device="cuda")
+    s_a, s_b = torch.ones(4, device="cuda"), torch.ones(6, device="cuda")
+    with pytest.raises(ValueError):
+        niti.linear_fwd(a, codes(6, 17, 2), out, s_a, s_b)
+    with pytest.raises(ValueError):
+        niti.linear_fwd(a, b, out, s_a[:3], s_b)
+    with pytest.raises(TypeError):
+        niti.linear_fwd(a.float(), b, out, s_a, s_b)
+    with pytest.raises(TypeError):
+        niti.linear_fwd(a, b, out, s_a.half(), s_b)
+    with pytest.raises(ValueError):
+        niti.linear_fwd(a, b, out.t().contiguous().t(), s_a, s_b)
+    with pytest.raises(niti.NitiError):
+        niti.linear_fwd(a, b, out, s_a, s_b, act=9)
+    da, ws = torch.empty(4, 16, device="cuda"), niti.new_workspace(256)
+    with pytest.raises(niti.NitiError):
+        niti.linear_bwd(out, a, b, s_a, s_b, ws, da=da)                       # workspace too small
+    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, 4, 6, 16))
+    with pytest.raises(niti.NitiError):
+        niti.linear_bwd(out, a, b, s_a, s_b, ws, act=niti.ACT_SILU, da=da)    # no z
+    with pytest.raises(niti.NitiError):
+        niti.linear_bwd(out, a, b, s_a, s_b, ws, da=da, mode=niti.PSR)
