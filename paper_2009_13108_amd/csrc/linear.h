@@ -19,6 +19,7 @@ struct LinArgs {
     int64_t M, N, K;
     int32_t a_step, b_step;   // 1, or 0 for one scale
     int32_t bias_type, act;
+    int32_t res_dma;          // set by linear_run
 };
 
 hipError_t linear_run(const LinArgs& a, int type, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -7,99 +7,171 @@
 // forms the sum: z, the activation and the residual cost no pass of their own.
 #include "linear.h"
 
+#include <math.h>
+
+#include <utility>
+
 namespace niti {
 
 namespace {
 
 // ---------------------------------------------------------------- epilogue
-// A wave's accumulators leave through a strip of LDS, 32 rows at a time, so
-// that each lane then holds 8 consecutive columns of a row: whole cache lines
-// are loaded (residual) and stored.  WTN: columns of the wave's tile.
-template <int WTN>
-struct Strip {
-    static constexpr int PITCH = WTN + 4;          // ints; lanes of a column hit distinct banks
-    static constexpr int INTS = 32 * PITCH;
-    static constexpr int LPR = WTN / 8;            // lanes of a row
-    static constexpr int RPP = 64 / LPR;           // rows of a pass
+// Accumulators are 32 x 32 tiles acc[a][b] (channels a, rows b): element 4 j + i
+// of a lane is channel 32 a + 8 j + 4 (lane / 32) + i of row 32 b + lane % 32.  The
+// epilogue works on them where they are (a lane has one row scale per b, and
+// four channels at a time), rounds, and turns the tile through LDS, so that
+// whole 16-byte pieces of rows are stored.  The residual comes the other way:
+// its tile is loaded into the same LDS places, by direct-to-LDS loads all in
+// flight at once where its rows are aligned, and each lane adds its four values
+// and puts the sums back.
+//
+// All tiles of a wave share one copy of this code (the accumulators are picked
+// by uniform branches): with the loops unrolled, the activations' code outgrew
+// the instruction cache and a 256 x 256 tile's epilogue took 16 us alone.
+template <typename T, int BM, int BN, int WGM, int WGN, int ROOM>
+struct Stage {
+    static constexpr int NT = 64 * WGM * WGN;
+    static constexpr int WTM = BM / WGM, WTN = BN / WGN, FM = WTM / 32, FN = WTN / 32;
+    static constexpr int PPR = BN * (int)sizeof(T) / 16;     // pieces of a row
+    static constexpr int EPP = 16 / (int)sizeof(T);          // elements of a piece
+    // row tiles b of a wave that are turned at a time: what ROOM bytes hold
+    static constexpr int BG = BM * BN * (int)sizeof(T) <= ROOM ? FM : (BM * BN * (int)sizeof(T) <= 2 * ROOM ? FM / 2 : FM / 4);
+    static_assert(BG >= 1 && BG * FN >= 1, "room for one row tile of each wave");
+    static constexpr int ROWS = 32 * BG * WGM;
+    static constexpr int PIECES = ROWS * PPR;
+    static_assert(PIECES % (64 * WGM * WGN) == 0, "whole load instructions");
+    // LDS piece of piece p of row r: rows that a lane group takes one column of hit distinct banks
+    static __device__ __forceinline__ int at(int r, int p) { return r * PPR + (p ^ (r & (PPR < 32 ? PPR - 1 : 31))); }
+    // row of the tile that row r of the turned rows is, for the group from b0 on
+    static __device__ __forceinline__ int tile_row(int r, int b0) { return r / (32 * BG) * WTM + b0 * 32 + r % (32 * BG); }
 };
 
-// What a lane needs of its 8 columns, the same for every row.
-struct ColArgs {
-    float sb[8], bias[8];
-};
+// x = acc[want] by uniform branches over constant indices: the accumulators stay in registers.
+template <int FN, int FM, int... I>
+__device__ __forceinline__ void pick(v16i (&acc)[FN][FM], int want, v16i& x, std::integer_sequence<int, I...>) {
+    ((want == I ? (void)(x = acc[I / FM][I % FM]) : (void)0), ...);
+}
 
-template <int WTN>
-__device__ __forceinline__ void load_cols(const LinArgs& A, int64_t n0, ColArgs& c) {
-    const int64_t n = n0 + (threadIdx.x & 63) % Strip<WTN>::LPR * 8;
-    const int left = (int)min((int64_t)8, A.N - n);
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        c.sb[e] = A.s_b && left > 0 ? A.s_b[A.b_step ? n + min(e, left - 1) : 0] : 1.f;
-        c.bias[e] = 0.f;
+// Scales and biases of a tile's columns and scales of its rows, to LDS before
+// the sum begins: loaded in the epilogue they cost it two memory round trips.
+template <int BM, int BN, int NT>
+__device__ __forceinline__ void load_params(const LinArgs& A, float* par, int64_t m0, int64_t n0) {
+    for (int c = threadIdx.x; c < BN; c += NT) {
+        const bool in = n0 + c < A.N;
+        float bias[1] = {0.f};
+        if (A.bias && in) load_typed(A.bias, A.bias_type, n0 + c, 1, bias);
+        par[c] = in ? (A.s_b ? A.s_b[A.b_step ? n0 + c : 0] : 1.f) : 0.f;
+        par[BN + c] = bias[0];
     }
-    if (A.bias) load_typed(A.bias, A.bias_type, n, left, c.bias);
+    for (int r = threadIdx.x; r < BM; r += NT)
+        par[2 * BN + r] = m0 + r < A.M ? (A.s_a ? A.s_a[A.a_step ? m0 + r : 0] : 1.f) : 0.f;
 }
 
-// 32 rows from m0 on, 8 columns a lane, from the strip.
-template <typename T, int WTN>
-__device__ __forceinline__ void finish_strip(const LinArgs& A, const int32_t* strip, int64_t m0, int64_t n0, const ColArgs& c) {
-    using S = Strip<WTN>;
+// res_dma: the residual's rows are whole aligned pieces within 32-bit offsets.
+template <typename T, int BM, int BN, int WGM, int WGN, int ROOM>
+__device__ __forceinline__ void epilogue(const LinArgs& A, v16i (&acc)[BN / WGN / 32][BM / WGM / 32], int8_t* lds, const float* par,
+                                         int64_t m0, int64_t n0) {
+    using S = Stage<T, BM, BN, WGM, WGN, ROOM>;
+    constexpr int FM = S::FM, FN = S::FN, BG = S::BG;
     const int lane = threadIdx.x & 63;
-    const int col = lane % S::LPR * 8;
-    const int64_t n = n0 + col;
-    const int left = (int)min((int64_t)8, A.N - n);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WGM, wn = wave / WGM;
+    const int rows = (int)min((int64_t)BM, A.M - m0), ncol = (int)min((int64_t)BN, A.N - n0);
+#pragma unroll 1
+    for (int b0 = 0; b0 < FM; b0 += BG) {
+#pragma unroll 1
+        for (int kind = A.z ? 0 : 1; kind < 2; kind++) {   // z, then out
+            const bool add = kind == 1 && A.res;
+            if (add && A.res_dma) {
+                const u32x4 rs = raw_rsrc((const T*)A.res + m0 * A.ldres + n0,
+                                          (uint32_t)(((int64_t)(rows - 1) * A.ldres + ncol) * (int64_t)sizeof(T)));
+                const uint32_t base = lds_address(lds);
+#pragma unroll 4
+                for (int i = 0; i < S::PIECES / S::NT; i++) {
+                    const int slot = (i * (S::NT / 64) + wave) * 64 + lane;
+                    const int r = slot / S::PPR, p = S::at(r, slot % S::PPR) - r * S::PPR;
+                    lds_dma16(rs, base + (uint32_t)((i * (S::NT / 64) + wave) * 1024),
+                              (uint32_t)S::tile_row(r, b0) * (uint32_t)(A.ldres * (int64_t)sizeof(T)) + (uint32_t)(p * 16), 0);
+                }
+                __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt 0
+            } else if (add) {
+                for (int slot = threadIdx.x; slot < S::PIECES; slot += S::NT) {
+                    const int r = slot / S::PPR, p = slot % S::PPR;
+                    const int m = min(S::tile_row(r, b0), rows - 1), nv = ncol - p * S::EPP;
+                    const T* src = (const T*)A.res + (m0 + m) * A.ldres + n0 + p * S::EPP;
+                    T v[S::EPP] = {};
+                    if (nv >= S::EPP) {
+                        __builtin_memcpy(v, src, 16);
+                    } else {
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += S::RPP) {
-        const int row = r0 + lane / S::LPR;
-        const int64_t m = m0 + row;
-        if (m >= A.M || left <= 0) continue;
-        const v4i lo = *(const v4i*)(strip + row * S::PITCH + col);
-        const v4i hi = *(const v4i*)(strip + row * S::PITCH + col + 4);
-        const float sa = A.s_a ? A.s_a[A.a_step ? m : 0] : 1.f;
-        float v[8];
+                        for (int e = 0; e < S::EPP; e++)
+                            if (e < nv) v[e] = src[e];
+                    }
+                    __builtin_memcpy(lds + S::at(r, p) * 16, v, 16);
+                }
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int t = 0; t < FN * BG; t++) {
+                const int ta = t / BG, tb = t % BG;
+                v16i x = acc[0][0];
+                pick(acc, ta * FM + b0 + tb, x, std::make_integer_sequence<int, FN * FM>());
+                const int row = tb * 32 + (lane & 31);                    // of the wave's turned rows
+                const float sa = par[2 * BN + wm * S::WTM + b0 * 32 + row];
+                const int r = wm * 32 * BG + row;
+                const int c0 = wn * S::WTN + ta * 32 + 4 * (lane >> 5);   // this lane's columns: c0 + 8 j + e
+                v4f sb[4], bias[4];
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = (float)(e < 4 ? lo[e & 3] : hi[e & 3]) * (sa * c.sb[e]) + c.bias[e];
-        if (A.z) store_some((T*)A.z + m * A.ldz + n, left, v);
-        if (A.act != NITI_ACT_NONE) {
+                for (int j = 0; j < 4; j++) {
+                    sb[j] = *(const v4f*)(par + c0 + 8 * j);
+                    bias[j] = *(const v4f*)(par + BN + c0 + 8 * j);
+                }
+                float v[16];
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = act_value(A.act, v[e]);
+                for (int e = 0; e < 16; e++) v[e] = (float)x[e] * sb[e >> 2][e & 3] * sa + bias[e >> 2][e & 3];
+                if (kind == 1 && A.act != NITI_ACT_NONE) act_values(A.act, v);
+                T* at[4];
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const int c = c0 + 8 * j;
+                    at[j] = (T*)(lds + S::at(r, c / S::EPP) * 16) + c % S::EPP;
+                }
+                if (add) {
+                    float res[4][4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) load_n(at[j], res[j]);
+#pragma unroll
+                    for (int e = 0; e < 16; e++) v[e] += res[e >> 2][e & 3];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float w[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+                    store_n(at[j], w);
+                }
+            }
+            __syncthreads();
+            T* out = (T*)(kind ? A.out : A.z) + m0 * (kind ? A.ldout : A.ldz) + n0;
+            const int64_t ld = kind ? A.ldout : A.ldz;
+#pragma unroll 4
+            for (int i = 0; i < S::PIECES / S::NT; i++) {
+                const int slot = i * S::NT + threadIdx.x;
+                const int r = slot / S::PPR, p = slot % S::PPR;
+                const int m = S::tile_row(r, b0), nv = ncol - p * S::EPP;
+                const uint4 v = *(const uint4*)(lds + S::at(r, p) * 16);
+                if (m >= rows || nv <= 0) continue;
+                T* dst = out + m * ld + p * S::EPP;
+                if (nv >= S::EPP) {
+                    store16_any(dst, v);
+                } else {
+                    T e[S::EPP];
+                    __builtin_memcpy(e, &v, 16);
+#pragma unroll
+                    for (int k = 0; k < S::EPP; k++)
+                        if (k < nv) dst[k] = e[k];
+                }
+            }
+            if (kind == 0 || b0 + BG < FM) __syncthreads();
         }
-        if (A.res) {
-            float r[8];
-            load_some((const T*)A.res + m * A.ldres + n, left, r);
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[e] += r[e];
-        }
-        store_some((T*)A.out + m * A.ldout + n, left, v);
-    }
-}
-
-// Orders a wave's own LDS writes before its reads by other lanes.
-__device__ __forceinline__ void wave_lds_fence() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// Accumulators acc[a][b] (32 x 32 tiles: channels a, rows b; element 4 j + i is
-// channel 32 a + 8 j + 4 (lane / 32) + i of row 32 b + lane % 32) through the strip.
-template <typename T, int FN, int FM>
-__device__ __forceinline__ void epilogue(const LinArgs& A, v16i (&acc)[FN][FM], int32_t* strip, int64_t m0, int64_t n0) {
-    constexpr int WTN = 32 * FN;
-    using S = Strip<WTN>;
-    const int lane = threadIdx.x & 63;
-    ColArgs c;
-    load_cols<WTN>(A, n0, c);
-#pragma unroll
-    for (int b = 0; b < FM; b++) {
-#pragma unroll
-        for (int a = 0; a < FN; a++)
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-                *(v4i*)(strip + (lane & 31) * S::PITCH + 32 * a + 8 * j + 4 * (lane >> 5)) =
-                    v4i{acc[a][b][4 * j], acc[a][b][4 * j + 1], acc[a][b][4 * j + 2], acc[a][b][4 * j + 3]};
-        wave_lds_fence();
-        finish_strip<T, WTN>(A, strip, m0 + 32 * b, n0, c);
-        wave_lds_fence();
     }
 }
 
@@ -128,7 +200,7 @@ __device__ __forceinline__ int gswz(int row) { return ((row >> 1) ^ (row >> 2)) 
 template <typename T>
 __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n) {
     __shared__ __attribute__((aligned(16))) int8_t lds[2][2 * GT * GK];
-    __shared__ __attribute__((aligned(16))) int32_t strips[4][Strip<32>::INTS];
+    __shared__ __attribute__((aligned(16))) float par[3 * GT];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * GT, n0 = (int64_t)(blockIdx.x % tiles_n) * GT;
@@ -138,6 +210,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
     const int8_t* rb = A.b + (n0 + row < A.N ? (n0 + row) * A.ldb : 0);
     const int K = (int)A.K, nk = (K + GK - 1) / GK;
     const int put = row * GK + ((pc ^ gswz(row)) << 4);
+    load_params<GT, GT, 256>(A, par, m0, n0);
     v16i acc[1][1];
     acc[0][0] = v16i{};
     const int wm = wave & 1, wn = wave >> 1;
@@ -161,7 +234,8 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
             acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb, fa, acc[0][0], 0, 0, 0);
         }
     }
-    epilogue<T, 1, 1>(A, acc, strips[wave], m0 + wm * 32, n0 + wn * 32);
+    __syncthreads();
+    epilogue<T, GT, GT, 2, 2, sizeof(lds)>(A, acc, lds[0], par, m0, n0);
 }
 
 template <typename T>
@@ -171,9 +245,333 @@ hipError_t run_any(const LinArgs& A, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- few products
+// Tiles of 16 FM rows x 16 FN channels; the workgroup's eight waves split the
+// sum, so that a tile's operands are in flight all at once, straight from
+// memory into MFMA registers, and join through LDS.  A step of a wave is 128
+// bytes of each row (two 16 x 16 x 64 MFMAs): whole cache lines.  Any strides and
+// addresses.  One token by 4096 x 4096 is 256 such tiles: every CU streams 64 KB
+// of weights.
+constexpr int SW = 8;
+
+template <typename T, int FM, int FN>
+__global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int tiles_n) {
+    constexpr int TM = 16 * FM, TN = 16 * FN, PITCH = TN + 4;
+    constexpr int KB = FM + FN <= 2 ? 4 : (FM + FN <= 3 ? 2 : 1);   // steps in flight of a wave
+    __shared__ __attribute__((aligned(16))) int32_t red[SW * TM * PITCH];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * TM, n0 = (int64_t)(blockIdx.x % tiles_n) * TN;
+    // the epilogue's operands of the threads that end a row's four channels, ahead of the sum
+    const int row = threadIdx.x / (4 * FN), col = threadIdx.x % (4 * FN) * 4;
+    const int64_t m = m0 + row, n = n0 + col;
+    const int left = row < TM && m < A.M && n < A.N ? (int)min((int64_t)4, A.N - n) : 0;
+    float sa = 0.f, sb[4], bias[4] = {0.f, 0.f, 0.f, 0.f}, res[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+        sa = A.s_a ? A.s_a[A.a_step ? m : 0] : 1.f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) sb[e] = A.s_b ? A.s_b[A.b_step ? n + min(e, left - 1) : 0] : 1.f;
+        if (A.bias) load_typed(A.bias, A.bias_type, n, left, bias);
+        if (A.res) load_some((const T*)A.res + m * A.ldres + n, left, res);
+    }
+    // rows past the edge read row 0: what they give is not stored
+    const int r16 = lane & 15, kq = (lane >> 4) * 16;
+    const int8_t *ra[FM], *rb[FN];
+#pragma unroll
+    for (int i = 0; i < FM; i++) ra[i] = A.a + (m0 + 16 * i + r16 < A.M ? (m0 + 16 * i + r16) * A.lda : 0);
+#pragma unroll
+    for (int i = 0; i < FN; i++) rb[i] = A.b + (n0 + 16 * i + r16 < A.N ? (n0 + 16 * i + r16) * A.ldb : 0);
+    const int K = (int)A.K;
+    v4i acc[FN][FM];
+#pragma unroll
+    for (int a = 0; a < FN; a++)
+#pragma unroll
+        for (int b = 0; b < FM; b++) acc[a][b] = v4i{0, 0, 0, 0};
+    auto mma = [&](v4i (&w)[FN], v4i (&x)[FM]) {
+#pragma unroll
+        for (int a = 0; a < FN; a++)
+#pragma unroll
+            for (int b = 0; b < FM; b++) acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[a], x[b], acc[a][b], 0, 0, 0);
+    };
+    const int whole = K >> 7;   // steps without a check
+    int s = wave;
+    for (; s + (KB - 1) * SW < whole; s += KB * SW) {
+        v4i w[2 * KB][FN], x[2 * KB][FM];
+#pragma unroll
+        for (int j = 0; j < 2 * KB; j++) {
+            const int k = (s + (j >> 1) * SW) * 128 + (j & 1) * 64 + kq;
+#pragma unroll
+            for (int i = 0; i < FN; i++) w[j][i] = __builtin_bit_cast(v4i, load16_any(rb[i] + k));
+#pragma unroll
+            for (int i = 0; i < FM; i++) x[j][i] = __builtin_bit_cast(v4i, load16_any(ra[i] + k));
+        }
+#pragma unroll
+        for (int j = 0; j < 2 * KB; j++) mma(w[j], x[j]);
+    }
+    for (; s * 128 < K; s += SW)
+#pragma unroll
+        for (int j = 0; j < 2; j++) {
+            const int k = s * 128 + j * 64 + kq;
+            v4i w[FN], x[FM];
+#pragma unroll
+            for (int i = 0; i < FN; i++) w[i] = row_piece(rb[i], k, K);
+#pragma unroll
+            for (int i = 0; i < FM; i++) x[i] = row_piece(ra[i], k, K);
+            mma(w, x);
+        }
+    // element i of acc[a][b]: channel 16 a + 4 (lane / 16) + i of row 16 b + lane % 16
+#pragma unroll
+    for (int a = 0; a < FN; a++)
+#pragma unroll
+        for (int b = 0; b < FM; b++)
+            *(v4i*)(red + (wave * TM + 16 * b + r16) * PITCH + 16 * a + 4 * (lane >> 4)) = acc[a][b];
+    __syncthreads();
+    if (left <= 0) return;
+    v4i sum = *(const v4i*)(red + row * PITCH + col);
+#pragma unroll
+    for (int i = 1; i < SW; i++) sum += *(const v4i*)(red + (i * TM + row) * PITCH + col);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (float)sum[e] * sb[e] * sa + bias[e];
+    if (A.z) store_some((T*)A.z + m * A.ldz + n, left, v);
+    act_values(A.act, v);
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] += res[e];
+    store_some((T*)A.out + m * A.ldout + n, left, v);
+}
+
+template <typename T, int FM, int FN>
+hipError_t run_small(const LinArgs& A, hipStream_t stream) {
+    const int64_t tm = (A.M + 16 * FM - 1) / (16 * FM), tn = (A.N + 16 * FN - 1) / (16 * FN);
+    hipLaunchKernelGGL((linear_small_kernel<T, FM, FN>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- ring
+// Tiles of BM x BN from an LDS ring of NS stages of KS bytes a row, filled by
+// direct-to-LDS loads.  Needs K, strides and addresses in whole 16 bytes.
+constexpr uint32_t kOut = 0x80000000u;   // an offset past any tile: loads zeros
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {   // vmcnt <= N and this wave's LDS reads done
+    static_assert(N < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0070);
+}
+
+template <int BM, int BN, int NS, int WGM, int WGN, int KS>
+struct Ring {
+    static constexpr int NW = WGM * WGN, NT = 64 * NW;
+    static constexpr int RPB = 1024 / KS;          // rows of a 1 KiB block (one load instruction)
+    static constexpr int LPR = KS / 16;            // lanes of a row
+    static constexpr int ND = KS / 32;             // MFMA depths of a step
+    static constexpr int WTM = BM / WGM, WTN = BN / WGN;
+    static constexpr int FM = WTM / 32, FN = WTN / 32;
+    static constexpr int LA = BM / RPB / NW, LB = BN / RPB / NW;   // loads of a wave and stage
+    static_assert(LA * RPB * NW == BM && LB * RPB * NW == BN, "loads split over the waves");
+    static_assert(NW % 2 == 0, "one swizzle parity per wave");
+    static constexpr int STAGE = (BM + BN) * KS;
+    static constexpr int LDS = NS * STAGE + (2 * BN + BM) * 4;   // the ring, and the tile's scales and biases
+    // 16-byte piece c of row r is stored at piece c ^ swz(r): the 32 rows that a
+    // fragment read takes one piece of then hit distinct banks
+    static __device__ __forceinline__ int swz(int row) { return KS == 64 ? ((row >> 1) ^ (row >> 2)) & 3 : (row >> 1) & 7; }
+};
+
+template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
+__global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_kernel(LinArgs A, int tiles_n) {
+    using R = Ring<BM, BN, NS, WGM, WGN, KS>;
+    extern __shared__ __attribute__((aligned(1024))) int8_t ring[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WGM, wn = wave / WGM;
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * BM, n0 = (int64_t)(blockIdx.x % tiles_n) * BN;
+    const int rows_a = (int)min((int64_t)BM, A.M - m0), rows_b = (int)min((int64_t)BN, A.N - n0);
+    const int K = (int)A.K, nk = (K + KS - 1) / KS;
+    // Offsets from the tile's first row; rows past the operand lie past the descriptor's end and load zeros.
+    const uint32_t lda = (uint32_t)A.lda, ldb = (uint32_t)A.ldb;
+    const u32x4 rs_a = raw_rsrc(A.a + m0 * A.lda, (uint32_t)(rows_a - 1) * lda + (uint32_t)K);
+    const u32x4 rs_b = raw_rsrc(A.b + n0 * A.ldb, (uint32_t)(rows_b - 1) * ldb + (uint32_t)K);
+    const int lrow = lane / R::LPR;
+    const uint32_t kpo = (uint32_t)(((lane % R::LPR) ^ R::swz((wave & 1) * R::RPB + lrow)) << 4);
+    const uint32_t lds0 = lds_address(ring);
+    uint32_t oa[R::LA], ob[R::LB], da[R::LA], db[R::LB];
+#pragma unroll
+    for (int i = 0; i < R::LA; i++) {
+        const int blk = wave + i * R::NW;
+        oa[i] = (uint32_t)(blk * R::RPB + lrow) * lda + kpo;
+        da[i] = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)blk * 1024u);
+    }
+#pragma unroll
+    for (int i = 0; i < R::LB; i++) {
+        const int blk = wave + i * R::NW;
+        ob[i] = (uint32_t)(blk * R::RPB + lrow) * ldb + kpo;
+        db[i] = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(BM * KS) + (uint32_t)blk * 1024u);
+    }
+    const uint32_t kend = (uint32_t)(K - (nk - 1) * KS);   // bytes of the last step
+    int left = nk - 1;                                     // whole steps to load
+    uint32_t koff = 0, slot = 0;
+    // Loads of the next step.  Past the last one they go on as zeros: the wait counts stay constant.
+    auto begin_step = [&]() {
+        if (left <= 0) {
+            const bool out = left < 0 || kpo >= kend;
+#pragma unroll
+            for (int i = 0; i < R::LA; i++) oa[i] = out ? kOut : oa[i];
+#pragma unroll
+            for (int i = 0; i < R::LB; i++) ob[i] = out ? kOut : ob[i];
+        }
+        left = __builtin_amdgcn_readfirstlane(left - 1);
+    };
+    auto end_step = [&]() {
+        koff += KS;
+        slot = slot + R::STAGE == (uint32_t)(NS * R::STAGE) ? 0u : slot + R::STAGE;
+    };
+    // load i of the step, of LA + LB
+    auto load = [&](int i) {
+        if (i < R::LA)
+            lds_dma16_at(rs_a, da[i], slot, oa[i], koff);
+        else
+            lds_dma16_at(rs_b, db[i - R::LA], slot, ob[i - R::LA], koff);
+    };
+
+    v16i acc[R::FN][R::FM];
+#pragma unroll
+    for (int a = 0; a < R::FN; a++)
+#pragma unroll
+        for (int b = 0; b < R::FM; b++) acc[a][b] = v16i{};
+    int a_at[R::FM], b_at[R::FN], a_sw[R::FM], b_sw[R::FN];
+#pragma unroll
+    for (int i = 0; i < R::FM; i++) {
+        const int row = wm * R::WTM + i * 32 + (lane & 31);
+        a_at[i] = row * KS;
+        a_sw[i] = R::swz(row & 15);
+    }
+#pragma unroll
+    for (int i = 0; i < R::FN; i++) {
+        const int row = wn * R::WTN + i * 32 + (lane & 31);
+        b_at[i] = BM * KS + row * KS;
+        b_sw[i] = R::swz(row & 15);
+    }
+    float* par = (float*)(ring + NS * R::STAGE);
+    load_params<BM, BN, R::NT>(A, par, m0, n0);
+#pragma unroll
+    for (int s = 0; s < NS - 1; s++) {
+        begin_step();
+#pragma unroll
+        for (int i = 0; i < R::LA + R::LB; i++) load(i);
+        end_step();
+    }
+    v4i fa[2][R::FM], fb[2][R::FN];
+    auto read = [&](const int8_t* st, int d, int i) {   // fragment i of FN + FM of a depth
+        const int kp = (lane >> 5) + 2 * d;
+        if (i < R::FN)
+            fb[d & 1][i] = *(const v4i*)(st + b_at[i] + ((kp ^ b_sw[i]) << 4));
+        else
+            fa[d & 1][i - R::FN] = *(const v4i*)(st + a_at[i - R::FN] + ((kp ^ a_sw[i - R::FN]) << 4));
+    };
+    // The MFMAs of depth d, with the reads of a next depth and loads from..to-1 spread between them: a wave
+    // that issues its loads and reads at once keeps its matrix core waiting meanwhile.
+    constexpr int NM = R::FN * R::FM, NR = R::FN + R::FM;
+    auto depth = [&](int d, const int8_t* rd_st, int rd, int from, int to) {
+#pragma unroll
+        for (int i = 0; i < NM; i++) {
+            const int a = i / R::FM, b = i % R::FM;
+            acc[a][b] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[d & 1][a], fa[d & 1][b], acc[a][b], 0, 0, 0);
+#pragma unroll
+            for (int r = i * NR / NM; r < (i + 1) * NR / NM; r++) read(rd_st, rd, r);
+#pragma unroll
+            for (int l = from + i * (to - from) / NM; l < from + (i + 1) * (to - from) / NM; l++) load(l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Fragments are double buffered over the depths: one depth's are read while the previous one's MFMAs run,
+    // the next stage's first right after the barrier.  Before a barrier a wave waits for its own fragment reads,
+    // so no read of the stage that the next loads overwrite is in flight behind it.
+    constexpr int NL = R::LA + R::LB;
+    constexpr int LD = NS > 2 || R::ND < 4 ? R::ND - 1 : R::ND - 2;   // depths that loads are issued in
+    wait_loads<(NS - 2) * NL>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int i = 0; i < NR; i++) read(ring, 0, i);
+    int cur = 0;
+    for (int kt = 0; kt < nk; kt++) {
+        const int8_t* st = ring + cur;
+        begin_step();
+#pragma unroll
+        for (int d = 0; d + 1 < R::ND; d++)
+            depth(d, st, d + 1, d < LD ? d * NL / LD : NL, d < LD ? (d + 1) * NL / LD : NL);
+        end_step();
+        wait_loads<(NS - 2) * NL>();
+        __builtin_amdgcn_s_barrier();
+        cur = cur + R::STAGE == NS * R::STAGE ? 0 : cur + R::STAGE;
+        depth(R::ND - 1, ring + cur, 0, NL, NL);   // (after the last step it reads zeros that no MFMA uses)
+    }
+    wait_loads<0>();   // the loads past the end, before the ring is reused
+    __builtin_amdgcn_s_barrier();
+    epilogue<T, BM, BN, WGM, WGN, NS * R::STAGE>(A, acc, ring, par, m0, n0);
+}
+
+template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
+hipError_t run_ring(const LinArgs& A, hipStream_t stream) {
+    using R = Ring<BM, BN, NS, WGM, WGN, KS>;
+    const auto kernel = linear_ring_kernel<T, BM, BN, NS, WGM, WGN, KS>;
+    static bool attr_done = false;
+    if (!attr_done) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, R::LDS);
+        if (e != hipSuccess) return e;
+        attr_done = true;
+    }
+    const int64_t tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(R::NT), R::LDS, stream, A, (int)tn);
+    return hipGetLastError();
+}
+
+bool ring_takes(const LinArgs& A) {
+    return A.K > 0 && A.K % 16 == 0 && A.lda % 16 == 0 && A.ldb % 16 == 0 && (((uintptr_t)A.a | (uintptr_t)A.b) & 15) == 0;
+}
+
+// The kernels, and what a product of `tiles` tiles and K takes in each (us):
+//   start + round * max(1, tiles / 256) + K / 1000 * (step + more * max(0, tiles / 256 - 1))
+// (256 x 256 tiles, one a CU at a time: whole rounds).  Small tiles give every
+// CU work and split the sum, large ones load less for each product.  Fitted to
+// 540 random products of 1..8192 x 32..9216 x 32..9216 timed with each kernel;
+// what the model picks takes 2.1% longer than the fastest in the mean, and
+// 64 x 64 tiles alone would take 29%.
+struct Cost {
+    int bm, bn;
+    float start, round, step, more;
+};
+constexpr Cost kSmall11{16, 16, 2.12f, 0.39f, 0.63f, 0.88f};
+constexpr Cost kSmall12{16, 32, 2.13f, 0.50f, 0.96f, 1.11f};
+constexpr Cost kSmall22{32, 32, 2.03f, 0.88f, 1.13f, 1.49f};
+constexpr Cost kRing64{64, 64, 2.00f, 1.47f, 2.01f, 2.17f};
+constexpr Cost kRing128{128, 128, 0.41f, 3.40f, 6.84f, 4.92f};
+constexpr Cost kRing256{256, 256, 0.f, 10.3f, 10.4f, 5.22f};
+
+float cost(const Cost& c, const LinArgs& A) {
+    const float tiles = (float)((A.M + c.bm - 1) / c.bm) * (float)((A.N + c.bn - 1) / c.bn) / 256.f, k = (float)A.K / 1000.f;
+    if (c.bm == 256) return c.start + ceilf(tiles) * (c.round + c.step * k) + fminf(tiles, 1.f) * c.more * k;
+    return c.start + c.round * fmaxf(1.f, tiles) + k * (c.step + c.more * fmaxf(0.f, tiles - 1.f));
+}
+
 template <typename T>
-hipError_t run_linear(const LinArgs& A, void*, size_t, hipStream_t stream) {
-    return run_any<T>(A, stream);
+hipError_t run_linear(LinArgs A, void*, size_t, hipStream_t stream) {
+    const int64_t ld = A.ldres * (int64_t)sizeof(T);
+    A.res_dma = A.res && ld % 16 == 0 && ((uintptr_t)A.res & 15) == 0 && ld < ((int64_t)1 << 22);
+    const float s11 = cost(kSmall11, A), s12 = cost(kSmall12, A), s22 = cost(kSmall22, A);
+    const float small = fminf(fminf(s11, s12), s22);
+    if (ring_takes(A)) {
+        const float r64 = cost(kRing64, A), r128 = cost(kRing128, A), r256 = cost(kRing256, A);
+        const float ring = fminf(fminf(r64, r128), r256);
+        if (ring < small) {
+            if (ring == r256) return run_ring<T, 256, 256, 4, 2, 4, 64>(A, stream);
+            if (ring == r128) return run_ring<T, 128, 128, 2, 4, 2, 128>(A, stream);
+            return run_ring<T, 64, 64, 4, 2, 2, 128>(A, stream);
+        }
+    } else if (cost(kRing64, A) < small) {
+        return run_any<T>(A, stream);
+    }
+    if (small == s11) return run_small<T, 1, 1>(A, stream);
+    if (small == s12) return run_small<T, 1, 2>(A, stream);
+    return run_small<T, 2, 2>(A, stream);
 }
 
 }  // namespace

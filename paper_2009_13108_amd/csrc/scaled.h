@@ -147,6 +147,20 @@ __device__ __forceinline__ float act_value(int act, float z) {
     }
     return z;
 }
+// The same of several values: the choice is made once.
+template <int N>
+__device__ __forceinline__ void act_values(int act, float (&v)[N]) {
+    if (act == NITI_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_value(NITI_ACT_RELU, v[e]);
+    } else if (act == NITI_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_value(NITI_ACT_GELU, v[e]);
+    } else if (act == NITI_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_value(NITI_ACT_SILU, v[e]);
+    }
+}
 __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
     if (act == NITI_ACT_GELU) {
