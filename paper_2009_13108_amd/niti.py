@@ -596,16 +596,30 @@ def _type_of(dtype, what):
     return t
 
 
-def _mat(t, dtype, rows, cols, what, out=False):
+def _bad(t, dev, dtype, what):
+    """Why a tensor is not one of a call on device dev."""
+    if not isinstance(t, _Tensor) or t.get_device() < 0:
+        raise TypeError("%s must be a device tensor" % what)
+    if t.get_device() != dev:
+        raise ValueError("%s is on device %d, the call's first operand on device %d" % (what, t.get_device(), dev))
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
+
+
+def _mat(t, dev, dtype, shape, what, out=False):
     """(address, row stride) of a matrix of the given type and shape; (None, 0) for None."""
     if t is None:
         return None, 0
-    if not isinstance(t, _Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a device tensor" % what)
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    if t.shape != (rows, cols):
-        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), (rows, cols)))
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+            return t.data_ptr(), shape[1]
+    except AttributeError:
+        pass
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev):
+        _bad(t, dev, dtype, what)
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+    rows, cols = shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous columns" % what)
@@ -616,122 +630,140 @@ def _mat(t, dtype, rows, cols, what, out=False):
     return t.data_ptr(), ld
 
 
-def _vec(t, n, what, dtype=None, one=False):
-    """Address of a contiguous vector of n elements (or one, where that is allowed); None for None."""
+def _vec(t, dev, n, what, dtype=None):
+    """Address of a contiguous vector of n elements; None for None."""
     if t is None:
         return None
-    if not isinstance(t, _Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a device tensor" % what)
-    if dtype is not None and t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    k = t.numel()
-    if (k != n and not (one and k == 1)) or not t.is_contiguous():
-        raise ValueError("%s must be contiguous with %d elements" % (what, n))
-    return t.data_ptr()
+    try:
+        if t.numel() == n and t.get_device() == dev and (dtype is None or t.dtype is dtype) and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _bad(t, dev, dtype, what)
+    raise ValueError("%s must be contiguous with %d elements" % (what, n))
 
 
-def _same_device(x, *others):
-    """All tensors of a call on the device of its first and on the current one, whose stream it uses."""
-    dev = x.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("tensors on %s and %s in one call" % (dev, t.device))
+def _scales(t, dev, n, what):
+    """(address, number) of a row scale for each of n rows, or one for all."""
+    try:
+        k = t.numel()
+        if (k == n or k == 1) and t.get_device() == dev and t.dtype is _torch_mod.float32 and t.is_contiguous():
+            return t.data_ptr(), k
+    except AttributeError:
+        pass
+    _bad(t, dev, _torch_mod.float32, what)
+    raise ValueError("%s must be contiguous with %d elements, or one" % (what, n))
 
 
 def _matrix(x, what):
-    """Shape of a call's first operand."""
-    _torch()
-    if not isinstance(x, _Tensor) or not x.is_cuda:
+    """Shape and device index of a call's first operand."""
+    if _Tensor is None:
+        _torch()
+    dev = x.get_device() if isinstance(x, _Tensor) else -1
+    if dev < 0:
         raise TypeError("%s must be a device tensor" % what)
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("%s must be a matrix" % what)
-    return x.shape
+    return shape, dev
 
 
-def _ws_args(ws):
+def _width(t, axis):
+    return t.shape[axis] if isinstance(t, _Tensor) and t.dim() == 2 else -1
+
+
+def _ws_args(ws, dev):
     if ws is None:
         return None, 0
-    _dev(ws, _torch_mod.uint8, "ws")
+    if not (isinstance(ws, _Tensor) and ws.dtype is _torch_mod.uint8 and ws.get_device() == dev and ws.is_contiguous()):
+        _bad(ws, dev, _torch_mod.uint8, "ws")
+        raise ValueError("ws must be contiguous")
     return ws.data_ptr(), ws.numel()
 
 
 def rmsnorm_fwd(x, gain, res=None, h=None, y=None, q=None, scale=None, rstd=None, eps=1e-6, stream=None):
     """h = x + res; y = h / sqrt(mean(h^2) + eps) * gain by rows; q, scale: y as
     int8 rows, and y then the values that they stand for (niti_rmsnorm_fwd)."""
-    M, D = _matrix(x, "x")
+    (M, D), dev = _matrix(x, "x")
     f32, dt = _torch_mod.float32, x.dtype
-    px, ldx = _mat(x, dt, M, D, "x")
-    pr, ldr = _mat(res, dt, M, D, "res")
-    ph, ldh = _mat(h, dt, M, D, "h", True)
-    py, ldy = _mat(y, dt, M, D, "y", True)
-    pq, ldq = _mat(q, _torch_mod.int8, M, D, "q", True)
-    _same_device(x, res, gain, h, y, q, scale, rstd)
-    _run("niti_rmsnorm_fwd", px, ldx, pr, ldr, _vec(gain, D, "gain"), _type_of(gain.dtype, "gain"), ph, ldh, py, ldy, pq, ldq,
-         _vec(scale, M, "scale", f32), _vec(rstd, M, "rstd", f32), M, D, float(eps), _type_of(dt, "x"), _stream(stream))
+    kind = _type_of(dt, "x")
+    px, ldx = _mat(x, dev, dt, (M, D), "x")
+    pr, ldr = _mat(res, dev, dt, (M, D), "res")
+    ph, ldh = _mat(h, dev, dt, (M, D), "h", True)
+    py, ldy = _mat(y, dev, dt, (M, D), "y", True)
+    pq, ldq = _mat(q, dev, _torch_mod.int8, (M, D), "q", True)
+    _run("niti_rmsnorm_fwd", px, ldx, pr, ldr, _vec(gain, dev, D, "gain"), _type_of(gain.dtype, "gain"), ph, ldh, py, ldy, pq,
+         ldq, _vec(scale, dev, M, "scale", f32), _vec(rstd, dev, M, "rstd", f32), M, D, eps, kind, _stream(stream))
 
 
 def rmsnorm_bwd(dy, h, gain, rstd, dx, dgain=None, ws=None, dh=None, stream=None):
     """Gradients of rmsnorm_fwd's input (dx, plus dh that reaches h another
     way) and gain; ws as workspace_bytes(OP_RMSNORM_BWD, None, M, D) when dgain is wanted."""
-    M, D = _matrix(dy, "dy")
+    (M, D), dev = _matrix(dy, "dy")
     f32, dt = _torch_mod.float32, dy.dtype
-    pdy, lddy = _mat(dy, dt, M, D, "dy")
-    ph, ldh = _mat(h, dt, M, D, "h")
-    pdh, lddh = _mat(dh, dt, M, D, "dh")
-    pdx, lddx = _mat(dx, dt, M, D, "dx", True)
-    pws, nws = _ws_args(ws)
-    _same_device(dy, h, gain, rstd, dx, dgain, ws, dh)
-    _run("niti_rmsnorm_bwd", pdy, lddy, ph, ldh, _vec(gain, D, "gain"), _type_of(gain.dtype, "gain"), _vec(rstd, M, "rstd", f32),
-         pdh, lddh, pdx, lddx, _vec(dgain, D, "dgain", f32), M, D, _type_of(dt, "dy"), pws, nws, _stream(stream))
+    kind = _type_of(dt, "dy")
+    pdy, lddy = _mat(dy, dev, dt, (M, D), "dy")
+    ph, ldh = _mat(h, dev, dt, (M, D), "h")
+    pdh, lddh = _mat(dh, dev, dt, (M, D), "dh")
+    pdx, lddx = _mat(dx, dev, dt, (M, D), "dx", True)
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_rmsnorm_bwd", pdy, lddy, ph, ldh, _vec(gain, dev, D, "gain"), _type_of(gain.dtype, "gain"),
+         _vec(rstd, dev, M, "rstd", f32), pdh, lddh, pdx, lddx, _vec(dgain, dev, D, "dgain", f32), M, D, kind, pws, nws,
+         _stream(stream))
 
 
 def quantize_rows(x, q, scale, y=None, mode=RTN, seed=0, call=0, stream=None):
     """x as int8 rows with a scale each; y: the values that they stand for (niti_quantize_rows)."""
-    M, D = _matrix(x, "x")
-    px, ldx = _mat(x, x.dtype, M, D, "x")
-    pq, ldq = _mat(q, _torch_mod.int8, M, D, "q", True)
-    py, ldy = _mat(y, x.dtype, M, D, "y", True)
-    _same_device(x, q, scale, y)
-    _run("niti_quantize_rows", px, ldx, pq, ldq, _vec(scale, M, "scale", _torch_mod.float32), py, ldy, M, D, int(mode),
-         int(seed) & 0xFFFFFFFFFFFFFFFF, int(call) & 0xFFFFFFFF, _type_of(x.dtype, "x"), _stream(stream))
+    (M, D), dev = _matrix(x, "x")
+    dt = x.dtype
+    kind = _type_of(dt, "x")
+    px, ldx = _mat(x, dev, dt, (M, D), "x")
+    pq, ldq = _mat(q, dev, _torch_mod.int8, (M, D), "q", True)
+    py, ldy = _mat(y, dev, dt, (M, D), "y", True)
+    _run("niti_quantize_rows", px, ldx, pq, ldq, _vec(scale, dev, M, "scale", _torch_mod.float32), py, ldy, M, D, mode,
+         seed & 0xFFFFFFFFFFFFFFFF, call & 0xFFFFFFFF, kind, _stream(stream))
 
 
 def linear_fwd(a, b, out, s_a, s_b, bias=None, act=ACT_NONE, res=None, z=None, ws=None, stream=None):
     """out = act(s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n]) + res; z: the
     value before the activation; ws as workspace_bytes(OP_LINEAR_FWD, None, M, N, K), or None (niti_linear_fwd)."""
-    M, K = _matrix(a, "a")
-    N = b.shape[0] if isinstance(b, _Tensor) and b.dim() == 2 else -1
-    i8, f32, dt = _torch_mod.int8, _torch_mod.float32, out.dtype
-    pa, lda = _mat(a, i8, M, K, "a")
-    pb, ldb = _mat(b, i8, N, K, "b")
-    po, ldo = _mat(out, dt, M, N, "out", True)
-    pr, ldr = _mat(res, dt, M, N, "res")
-    pz, ldz = _mat(z, dt, M, N, "z", True)
-    pws, nws = _ws_args(ws)
-    _same_device(a, b, out, s_a, s_b, bias, res, z, ws)
-    _run("niti_linear_fwd", pa, lda, _vec(s_a, M, "s_a", f32, True), s_a.numel(), pb, ldb, _vec(s_b, N, "s_b", f32, True),
-         s_b.numel(), _vec(bias, N, "bias"), F32 if bias is None else _type_of(bias.dtype, "bias"), int(act), pr, ldr, pz, ldz,
-         po, ldo, M, N, K, _type_of(dt, "out"), pws, nws, _stream(stream))
+    (M, K), dev = _matrix(a, "a")
+    N = _width(b, 0)
+    i8, dt = _torch_mod.int8, out.dtype
+    kind = _type_of(dt, "out")
+    pa, lda = _mat(a, dev, i8, (M, K), "a")
+    pb, ldb = _mat(b, dev, i8, (N, K), "b")
+    po, ldo = _mat(out, dev, dt, (M, N), "out", True)
+    pr, ldr = _mat(res, dev, dt, (M, N), "res")
+    pz, ldz = _mat(z, dev, dt, (M, N), "z", True)
+    psa, nsa = _scales(s_a, dev, M, "s_a")
+    psb, nsb = _scales(s_b, dev, N, "s_b")
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_linear_fwd", pa, lda, psa, nsa, pb, ldb, psb, nsb, _vec(bias, dev, N, "bias"),
+         F32 if bias is None else _type_of(bias.dtype, "bias"), act, pr, ldr, pz, ldz, po, ldo, M, N, K, kind, pws, nws,
+         _stream(stream))
 
 
 def linear_bwd(dy, a, b, s_a, s_b, ws, z=None, act=ACT_NONE, da=None, db=None, dbias=None, mode=RTN, seed=0, call=0,
                stream=None):
     """Gradients of the values that a and b stand for and of the bias, by int8
     products; ws as workspace_bytes(OP_LINEAR_BWD, None, M, N, K) (niti_linear_bwd)."""
-    M, N = _matrix(dy, "dy")
-    K = a.shape[1] if isinstance(a, _Tensor) and a.dim() == 2 else -1
+    (M, N), dev = _matrix(dy, "dy")
+    K = _width(a, 1)
     i8, f32, dt = _torch_mod.int8, _torch_mod.float32, dy.dtype
-    pdy, lddy = _mat(dy, dt, M, N, "dy")
-    pz, ldz = _mat(z, dt, M, N, "z")
-    pa, lda = _mat(a, i8, M, K, "a")
-    pb, ldb = _mat(b, i8, N, K, "b")
-    pda, ldda = _mat(da, dt, M, K, "da", True)
-    pdb, lddb = _mat(db, dt, N, K, "db", True)
-    pws, nws = _ws_args(ws)
-    _same_device(dy, a, b, s_a, s_b, ws, z, da, db, dbias)
-    _run("niti_linear_bwd", pdy, lddy, pz, ldz, int(act), pa, lda, _vec(s_a, M, "s_a", f32, True), s_a.numel(), pb, ldb,
-         _vec(s_b, N, "s_b", f32, True), s_b.numel(), pda, ldda, pdb, lddb, _vec(dbias, N, "dbias", f32), M, N, K, int(mode),
-         int(seed) & 0xFFFFFFFFFFFFFFFF, int(call) & 0xFFFFFFFF, _type_of(dt, "dy"), pws, nws, _stream(stream))
+    kind = _type_of(dt, "dy")
+    pdy, lddy = _mat(dy, dev, dt, (M, N), "dy")
+    pz, ldz = _mat(z, dev, dt, (M, N), "z")
+    pa, lda = _mat(a, dev, i8, (M, K), "a")
+    pb, ldb = _mat(b, dev, i8, (N, K), "b")
+    pda, ldda = _mat(da, dev, dt, (M, K), "da", True)
+    pdb, lddb = _mat(db, dev, dt, (N, K), "db", True)
+    psa, nsa = _scales(s_a, dev, M, "s_a")
+    psb, nsb = _scales(s_b, dev, N, "s_b")
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_linear_bwd", pdy, lddy, pz, ldz, act, pa, lda, psa, nsa, pb, ldb, psb, nsb, pda, ldda, pdb, lddb,
+         _vec(dbias, dev, N, "dbias", f32), M, N, K, mode, seed & 0xFFFFFFFFFFFFFFFF, call & 0xFFFFFFFF, kind, pws, nws,
+         _stream(stream))
 
 
 ADAMW_BLOCK = 256   # consecutive elements that share a scale in an 8-bit state
@@ -745,7 +777,7 @@ class AdamWTensor(ctypes.Structure):
 
 class AdamWPlan:
     """The tensors of an optimiser, checked and marshalled once (adamw_plan)."""
-    __slots__ = ("table", "count", "p_type", "g_type", "read_type", "bits", "tensors")
+    __slots__ = ("table", "count", "p_type", "g_type", "read_type", "bits", "tensors", "device")
 
 
 def _flat(t, n, dtype, what):
@@ -780,13 +812,15 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, m_read=None, v_r
     plan.p_type, plan.g_type, plan.read_type = (_type_of(d, w) for d, w in ((p_dt, "params"), (g_dt, "grads"), (r_dt, "m_read")))
     plan.table = (AdamWTensor * max(count, 1))()
     plan.count = count
+    plan.device = params[0].get_device() if count else -1
     plan.tensors = [list(params)] + [list(x) for x in lists.values() if x is not None]   # keeps their memory
     for i in range(count):
         n = params[i].numel()
         blocks = -(-n // ADAMW_BLOCK)
         row = plan.table[i]
         row.n = n
-        _same_device(params[0], params[i], *(x[i] for x in lists.values() if x is not None))
+        if any(t.get_device() != plan.device for t in [params[i]] + [x[i] for x in lists.values() if x is not None]):
+            raise ValueError("adamw_plan: tensors of one plan are on one device")
         row.p = _flat(params[i], n, p_dt, "params")
         row.g = _flat(grads[i], n, g_dt, "grads")
         row.m = _flat(m[i], n, m_dt, "m")
@@ -803,14 +837,13 @@ def adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.
                stream=None):
     """One AdamW step (number `step`, from 1 on) of all tensors of a plan;
     grad_scale: a float32 device scalar that multiplies the gradients."""
-    _run("niti_adamw_step", plan.table, plan.count, plan.p_type, plan.g_type, plan.bits, int(step), float(lr), float(beta1),
-         float(beta2), float(eps), float(weight_decay), _vec(grad_scale, 1, "grad_scale", _torch().float32), int(mode),
-         int(seed) & 0xFFFFFFFFFFFFFFFF, _stream(stream))
+    gs = None if grad_scale is None else _vec(grad_scale, plan.device, 1, "grad_scale", _torch_mod.float32)
+    _run("niti_adamw_step", plan.table, plan.count, plan.p_type, plan.g_type, plan.bits, step, lr, beta1, beta2, eps,
+         weight_decay, gs, mode, seed & 0xFFFFFFFFFFFFFFFF, _stream(stream))
 
 
 def adamw_read(plan, stream=None):
     """The values of a plan's 8-bit states, into its m_read and v_read."""
-    _torch()
     if plan.bits != 8:
         raise ValueError("adamw_read: 32-bit states are read as they are")
     _run("niti_adamw_read", plan.table, plan.count, plan.read_type, _stream(stream))
