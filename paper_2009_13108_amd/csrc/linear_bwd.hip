@@ -6,19 +6,24 @@
 // Folding b's scale into the rows (it varies along their sum) and a's into the
 // columns leaves both sums with integers only.
 //
-// Four steps.  (1) dy and z are read once for the rows' codes and for each
-// column's maximum and sum, which a workgroup keeps in registers over the rows
-// it takes and leaves as partial rows; (2) those are joined: c and dbias;
-// (3) the columns' codes, transposed, and transposed copies of a and b: the
-// products take rows along their sum; (4) the products, by the forward kernels.
+// Five launches.  (1) Tiles of 32 x 256 of dz leave the maxima of their rows and
+// the maxima and sums of their columns; (2) those are joined, in a fixed order:
+// r, c and dbias; (3) dz is formed again, in tiles of 128 x 128, for the codes of
+// rows and columns at once, the columns' transposed through LDS, and the same
+// launch transposes a and b: the products take rows along their sum; (4), (5) the
+// products, by the forward kernels.  dy and z are read twice, the second time
+// mostly from the last-level cache; holding dz for step 3 would round it or cost
+// four bytes an element each way.
 #include "linear.h"
 
 namespace niti {
 
 namespace {
 
-constexpr int CH = 8;
-constexpr int kParts = 512;      // partial rows of the column statistics
+constexpr int CH = 8;            // elements of a thread's piece of a row
+constexpr int SR = 32, SC = 256; // tile of step 1
+constexpr int CT = 128;          // tile of step 3
+constexpr int CP = CT + 4;       // its LDS pitch: lanes that write one row group hit distinct banks, two by two
 constexpr int64_t kPad = 16;     // sums are padded to whole 16-byte pieces
 
 inline int64_t up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
@@ -30,18 +35,19 @@ struct DzArgs {
     const float* s_b;
     int64_t lddy, ldz;
     int64_t M, N, Mp, Np;
+    int64_t tiles_m, tiles_n;   // of step 1
     int32_t a_step, b_step;
     int32_t act, sr;
     uint64_t seed;
     uint32_t call;
-    int8_t* p;       // [M][Np] codes of the rows, or NULL
-    float* r;        // [M]
-    int8_t* q;       // [N][Mp] codes of the columns, transposed, or NULL
-    float* c;        // [N]
-    float* dbias;    // [N] or NULL
-    uint32_t* pmax;  // [parts][N] partial maxima (magnitude bits)
-    float* psum;     // [parts][N]
-    int64_t parts;
+    int8_t* p;        // [M][Np] codes of the rows, or NULL
+    int8_t* q;        // [N][Mp] codes of the columns, transposed, or NULL
+    float* r;         // [2][M] scales, and the factors that form codes
+    float* c;         // [2][N]
+    float* dbias;     // [N] or NULL
+    uint32_t* rmax;   // [tiles_n][M] magnitude bits of the row maxima
+    uint32_t* cmax;   // [tiles_m][N]
+    float* csum;      // [tiles_m][N]
 };
 
 // dz of n consecutive elements from (m, c) on; zeros past them.
@@ -51,144 +57,88 @@ __device__ __forceinline__ void load_dz(const DzArgs& a, int64_t m, int64_t c, i
     if (a.act != NITI_ACT_NONE) {
         float z[CH];
         load_some((const T*)a.z + m * a.ldz + c, n, z);
+        act_slopes(a.act, z);
 #pragma unroll
-        for (int e = 0; e < CH; e++)
-            if (e < n) d[e] *= act_slope(a.act, z[e]);
+        for (int e = 0; e < CH; e++) d[e] = e < n ? d[e] * z[e] : 0.f;
     }
 }
 
-// Codes of a piece of a row; the row's padding up to a multiple of 16 is zero.
-__device__ __forceinline__ void put_codes(const DzArgs& a, int64_t m, int64_t c, int n, const float (&v)[CH], float inv) {
-    float code[CH];
+// b's scales of n columns from c on.
+__device__ __forceinline__ void load_sb(const DzArgs& a, int64_t c, int n, float (&v)[CH]) {
 #pragma unroll
-    for (int e = 0; e < CH; e++) {
-        const float u = a.sr ? draw_hi(sr_draw(a.seed, a.call, (uint64_t)(m * a.N + c + e))) : 0.f;
-        code[e] = e < n ? (a.sr ? code_sr(v[e], inv, u) : code_rtn(v[e], inv)) : 0.f;
-    }
-    const uint32_t w[2] = {pack4(code[0], code[1], code[2], code[3]), pack4(code[4], code[5], code[6], code[7])};
-    __builtin_memcpy(a.p + m * a.Np + c, w, CH);
+    for (int e = 0; e < CH; e++) v[e] = e < n ? a.s_b[a.b_step ? c + e : 0] : 0.f;
 }
 
-// Step 1 for up to 64 NW VPT 8 columns: NW waves a row.
-template <typename T, int NW, int VPT>
-__global__ __launch_bounds__(64 * NW) void dz_rows_kernel(DzArgs a) {
-    constexpr int NT = 64 * NW;
-    __shared__ uint32_t red[2][NW];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int N = (int)a.N;
-    float sb[VPT][CH], sum[VPT][CH];
-    uint32_t mx[VPT][CH];
-#pragma unroll
-    for (int i = 0; i < VPT; i++)
-#pragma unroll
-        for (int e = 0; e < CH; e++) {
-            const int c = (i * NT + (int)threadIdx.x) * CH + e;
-            sb[i][e] = c < N ? a.s_b[a.b_step ? c : 0] : 0.f;
-            sum[i][e] = 0.f;
-            mx[i][e] = 0;
-        }
-    int par = 0;
-    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x, par ^= 1) {
-        const float sa = a.s_a[a.a_step ? m : 0];
-        float d[VPT][CH];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < VPT; i++) {
-            const int c = (i * NT + (int)threadIdx.x) * CH;
-            load_dz<T>(a, m, c, N - c, d[i]);
-#pragma unroll
-            for (int e = 0; e < CH; e++) {
-                sum[i][e] += d[i][e];
-                mx[i][e] = max(mx[i][e], mag_bits(d[i][e] * sa));
-                d[i][e] *= sb[i][e];
-                if (c + e < N) top = max(top, mag_bits(d[i][e]));
-            }
-        }
-        if (a.p) {
-            top = wave_max_u32(top);
-            if ((threadIdx.x & 63) == 0) red[par][wave] = top;
-            __syncthreads();   // the halves of red alternate, see the norm's backward pass
-#pragma unroll
-            for (int i = 0; i < NW; i++) top = max(top, red[par][i]);
-            const RowScale rs = row_scale(top);
-            if (threadIdx.x == 0) a.r[m] = rs.scale;
-#pragma unroll
-            for (int i = 0; i < VPT; i++) {
-                const int c = (i * NT + (int)threadIdx.x) * CH;
-                if (c < (int)a.Np) put_codes(a, m, c, N - c, d[i], rs.inv);
-            }
-        }
-    }
-    if (!a.pmax) return;
-#pragma unroll
-    for (int i = 0; i < VPT; i++)
-#pragma unroll
-        for (int e = 0; e < CH; e++) {
-            const int c = (i * NT + (int)threadIdx.x) * CH + e;
-            if (c < N) {
-                a.pmax[(int64_t)blockIdx.x * N + c] = mx[i][e];
-                a.psum[(int64_t)blockIdx.x * N + c] = sum[i][e];
-            }
-        }
-}
-
-// Step 1 for more columns: each row twice, column statistics in the workspace.
+// Step 1.  A thread takes 8 columns of 4 rows; 32 lanes a row, 8 threads a column group.
 template <typename T>
-__global__ __launch_bounds__(1024) void dz_rows_long_kernel(DzArgs a) {
-    constexpr int NW = 16;
-    __shared__ uint32_t red[2][NW];
-    const int wave = threadIdx.x >> 6;
-    int par = 0;
-    for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x, par ^= 1) {
+__global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
+    __shared__ float ssum[8][SC + 8];
+    __shared__ uint32_t smax[8][SC + 8];
+    const int64_t tm = blockIdx.x / a.tiles_n, tn = blockIdx.x % a.tiles_n;
+    const int col = (threadIdx.x & 31) * CH, grp = threadIdx.x >> 5;
+    const int64_t c = tn * SC + col;
+    const int n = (int)max((int64_t)0, min((int64_t)CH, a.N - c));
+    float sb[CH], sum[CH];
+    uint32_t mx[CH];
+    load_sb(a, c, n, sb);
+#pragma unroll
+    for (int e = 0; e < CH; e++) sum[e] = 0.f, mx[e] = 0;
+#pragma unroll
+    for (int i = 0; i < SR / 8; i++) {
+        const int64_t m = tm * SR + i * 8 + grp;
+        if (m >= a.M) continue;   // the same for the row's lanes
         const float sa = a.s_a[a.a_step ? m : 0];
+        float d[CH];
+        load_dz<T>(a, m, c, n, d);
         uint32_t top = 0;
-        for (int64_t c = threadIdx.x * CH; c < a.N; c += 1024 * CH) {
-            const int n = (int)min((int64_t)CH, a.N - c);
-            float d[CH];
-            load_dz<T>(a, m, c, n, d);
 #pragma unroll
-            for (int e = 0; e < CH; e++) {
-                if (e >= n) continue;
-                if (a.pmax) {
-                    const int64_t at = (int64_t)blockIdx.x * a.N + c + e;
-                    const bool first = m == blockIdx.x;
-                    a.pmax[at] = max(first ? 0u : a.pmax[at], mag_bits(d[e] * sa));
-                    a.psum[at] = (first ? 0.f : a.psum[at]) + d[e];
-                }
-                top = max(top, mag_bits(d[e] * a.s_b[a.b_step ? c + e : 0]));
-            }
+        for (int e = 0; e < CH; e++) {
+            sum[e] += d[e];
+            mx[e] = max(mx[e], mag_bits(d[e] * sa));
+            top = max(top, mag_bits(d[e] * sb[e]));   // (zeros past the edge)
         }
-        if (!a.p) continue;
-        top = wave_max_u32(top);
-        if ((threadIdx.x & 63) == 0) red[par][wave] = top;
-        __syncthreads();
-        for (int i = 0; i < NW; i++) top = max(top, red[par][i]);
-        const RowScale rs = row_scale(top);
-        if (threadIdx.x == 0) a.r[m] = rs.scale;
-        for (int64_t c = threadIdx.x * CH; c < a.Np; c += 1024 * CH) {
-            const int n = (int)max((int64_t)0, min((int64_t)CH, a.N - c));
-            float d[CH];
-            load_dz<T>(a, m, c, n, d);
 #pragma unroll
-            for (int e = 0; e < CH; e++)
-                if (e < n) d[e] *= a.s_b[a.b_step ? c + e : 0];
-            put_codes(a, m, c, n, d, rs.inv);
+        for (int o = 16; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 32));
+        if ((threadIdx.x & 31) == 0) a.rmax[tn * a.M + m] = top;
+    }
+#pragma unroll
+    for (int e = 0; e < CH; e++) ssum[grp][col + e] = sum[e], smax[grp][col + e] = mx[e];
+    __syncthreads();
+    const int64_t cc = tn * SC + threadIdx.x;
+    if (cc < a.N) {
+        float s = ssum[0][threadIdx.x];
+        uint32_t m = smax[0][threadIdx.x];
+        for (int g = 1; g < 8; g++) {
+            s += ssum[g][threadIdx.x];
+            m = max(m, smax[g][threadIdx.x]);
         }
+        a.csum[tm * a.N + cc] = s;
+        a.cmax[tm * a.N + cc] = m;
     }
 }
 
-// Step 2: 64 columns a workgroup, partial rows shared by 16 groups and joined in order.
-__global__ __launch_bounds__(1024) void dz_cols_kernel(DzArgs a) {
+// Step 2.  Columns: 64 a workgroup, the tiles' values shared by 16 groups and joined in order.  Rows: 1024 a workgroup.
+__global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks) {
     __shared__ float ssum[16][64];
     __shared__ uint32_t smax[16][64];
+    if ((int)blockIdx.x >= col_blocks) {
+        const int64_t m = (int64_t)((int)blockIdx.x - col_blocks) * 1024 + threadIdx.x;
+        if (m >= a.M) return;
+        uint32_t mx = 0;
+        for (int64_t t = 0; t < a.tiles_n; t++) mx = max(mx, a.rmax[t * a.M + m]);
+        const RowScale rs = row_scale(mx);
+        a.r[m] = rs.scale;
+        a.r[a.M + m] = rs.inv;
+        return;
+    }
     const int col = threadIdx.x & 63, grp = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * 64 + col;
     float s = 0.f;
     uint32_t mx = 0;
     if (c < a.N)
-        for (int64_t i = grp; i < a.parts; i += 16) {
-            s += a.psum[i * a.N + c];
-            mx = max(mx, a.pmax[i * a.N + c]);
+        for (int64_t i = grp; i < a.tiles_m; i += 16) {
+            s += a.csum[i * a.N + c];
+            mx = max(mx, a.cmax[i * a.N + c]);
         }
     ssum[grp][col] = s;
     smax[grp][col] = mx;
@@ -199,108 +149,154 @@ __global__ __launch_bounds__(1024) void dz_cols_kernel(DzArgs a) {
             mx = max(mx, smax[i][col]);
         }
         if (a.dbias) a.dbias[c] = s;
-        a.c[c] = __uint_as_float(mx);   // step 3 forms the scale, and writes it here
+        const RowScale rs = row_scale(mx);
+        a.c[c] = rs.scale;
+        a.c[a.N + c] = rs.inv;
     }
 }
 
-// Step 3: a 64 x 64 tile of the columns' codes, transposed through LDS.  The
-// rows of a tile of column maxima are its last reader, so that the tiles of row 0
-// may not replace them with the scales: those go out by dz_scale_kernel.
-template <typename T>
-__global__ __launch_bounds__(256) void dz_cols_codes_kernel(DzArgs a, int tiles_n) {
-    __shared__ int8_t tile[64][64 + 4];
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 64, n0 = (int64_t)(blockIdx.x % tiles_n) * 64;
-    const int col = (threadIdx.x & 7) * CH;
+// A CT x CT tile of bytes in LDS, transposed, to rows from n0 on (`rows` of them) of stride ld, columns m0 .. cols - 1 (whole pieces).
+__device__ __forceinline__ void store_turned(const int8_t (*tile)[CP], int8_t* out, int64_t ld, int64_t n0, int64_t rows, int64_t m0,
+                                             int64_t cols) {
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int row = (threadIdx.x >> 3) + 32 * i;
-        const int64_t m = m0 + row;
-        const int n = m < a.M ? (int)max((int64_t)0, min((int64_t)CH, a.N - (n0 + col))) : 0;
-        float d[CH];
-        if (n > 0) load_dz<T>(a, m, n0 + col, n, d);
-        const float sa = n > 0 ? a.s_a[a.a_step ? m : 0] : 0.f;
-#pragma unroll
-        for (int e = 0; e < CH; e++) {
-            float code = 0.f;   // rows past M pad the sums with zeros
-            if (e < n) {
-                const float inv = row_scale(__float_as_uint(a.c[n0 + col + e])).inv;
-                const float v = d[e] * sa;
-                code = a.sr ? code_sr(v, inv, draw_lo(sr_draw(a.seed, a.call, (uint64_t)(m * a.N + n0 + col + e)))) : code_rtn(v, inv);
-            }
-            tile[col + e][row] = (int8_t)(int)code;
-        }
-    }
-    __syncthreads();
-    const int row = threadIdx.x >> 2, pc = (threadIdx.x & 3) * 16;
-    if (n0 + row < a.N && m0 + pc < a.Mp) {
+    for (int i = 0; i < CT * CT / 16 / 256; i++) {
+        const int idx = i * 256 + threadIdx.x, row = idx / (CT / 16), pc = idx % (CT / 16) * 16;
+        if (n0 + row >= rows || m0 + pc >= cols) continue;
         uint32_t w[4];
         __builtin_memcpy(w, &tile[row][pc], 16);
-        *(uint4*)(a.q + (n0 + row) * a.Mp + m0 + pc) = make_uint4(w[0], w[1], w[2], w[3]);
+        *(uint4*)(out + (n0 + row) * ld + m0 + pc) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
-__global__ void dz_scale_kernel(float* c, int64_t N) {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n < N) c[n] = row_scale(__float_as_uint(c[n])).scale;
+// 4 x 4 bytes: w[i] holds row i's four columns and then column i's four rows.
+__device__ __forceinline__ void turn4(uint32_t (&w)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
+    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
+    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
 }
 
-// t[k][r] = x[r][k] for r < R, zeros up to Rp (a multiple of 16).
-__global__ __launch_bounds__(256) void transpose_kernel(const int8_t* x, int64_t ldx, int8_t* t, int64_t R, int64_t Rp, int64_t K,
-                                                        int tiles_k) {
-    __shared__ int8_t tile[64][64 + 4];
-    const int64_t r0 = (int64_t)(blockIdx.x / tiles_k) * 64, k0 = (int64_t)(blockIdx.x % tiles_k) * 64;
-    const int row = threadIdx.x >> 2, pc = (threadIdx.x & 3) * 16;
-    int8_t v[16] = {};
-    if (r0 + row < R) {
-        const int8_t* src = x + (r0 + row) * ldx + k0 + pc;
-        const int n = (int)min((int64_t)16, K - (k0 + pc));
+// x [R][K] to be turned into t [K][Rp], zeros from column R to Rp (a multiple of 16).
+struct Turn {
+    const int8_t* x;
+    int8_t* t;
+    int64_t ldx, R, Rp, K;
+    int32_t blocks, tiles_k;
+};
+
+__device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*tile)[CP]) {
+    const int64_t r0 = (int64_t)(block / a.tiles_k) * CT, k0 = (int64_t)(block % a.tiles_k) * CT;
+    const int pc = (threadIdx.x & 7) * 16, row = (threadIdx.x >> 3) * 4;   // four rows of 16 bytes a thread
+    uint4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const int64_t r = r0 + row + i;
+        const int n = r < a.R ? (int)max((int64_t)0, min((int64_t)16, a.K - (k0 + pc))) : 0;
+        v[i] = make_uint4(0, 0, 0, 0);
         if (n == 16) {
-            __builtin_memcpy(v, src, 16);
-        } else {
-            for (int i = 0; i < n; i++) v[i] = src[i];
+            v[i] = load16_any(a.x + r * a.ldx + k0 + pc);
+        } else if (n > 0) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            for (int e = 0; e < n; e++) w[e >> 2] |= (uint32_t)(uint8_t)a.x[r * a.ldx + k0 + pc + e] << (8 * (e & 3));
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < 16; i++) tile[pc + i][row] = v[i];
-    __syncthreads();
-    if (k0 + row < K && r0 + pc < Rp) {
+    for (int g = 0; g < 4; g++) {
         uint32_t w[4];
-        __builtin_memcpy(w, &tile[row][pc], 16);
-        *(uint4*)(t + (k0 + row) * Rp + r0 + pc) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = g == 0 ? v[i].x : (g == 1 ? v[i].y : (g == 2 ? v[i].z : v[i].w));
+        turn4(w);
+#pragma unroll
+        for (int i = 0; i < 4; i++) *(uint32_t*)&tile[pc + 4 * g + i][row] = w[i];
     }
+    __syncthreads();
+    store_turned(tile, a.t, a.Rp, k0, a.K, r0, a.Rp);
 }
 
+// Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
 template <typename T>
-hipError_t run_rows(const DzArgs& a, hipStream_t stream) {
-    const unsigned grid = (unsigned)a.parts;
-    const int64_t pieces = (a.N + CH - 1) / CH;
-    if (pieces <= 256)
-        hipLaunchKernelGGL((dz_rows_kernel<T, 4, 1>), dim3(grid), dim3(256), 0, stream, a);
-    else if (pieces <= 512)
-        hipLaunchKernelGGL((dz_rows_kernel<T, 4, 2>), dim3(grid), dim3(256), 0, stream, a);
-    else if (pieces <= 2048)
-        hipLaunchKernelGGL((dz_rows_kernel<T, 16, 2>), dim3(grid), dim3(1024), 0, stream, a);
-    else
-        hipLaunchKernelGGL((dz_rows_long_kernel<T>), dim3(grid), dim3(1024), 0, stream, a);
-    return hipGetLastError();
-}
-
-hipError_t transpose(const int8_t* x, int64_t ldx, int8_t* t, int64_t R, int64_t Rp, int64_t K, hipStream_t stream) {
-    const int64_t tr = (R + 63) / 64, tk = (K + 63) / 64;
-    hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(tr * tk)), dim3(256), 0, stream, x, ldx, t, R, Rp, K, (int)tk);
-    return hipGetLastError();
+__global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int tiles_c) {
+    __shared__ __attribute__((aligned(16))) int8_t tile[CT][CP];
+    int block = blockIdx.x;
+    if (block < ta.blocks) {
+        turn_tile(ta, block, tile);
+        return;
+    }
+    block -= ta.blocks;
+    if (block < tb.blocks) {
+        turn_tile(tb, block, tile);
+        return;
+    }
+    block -= tb.blocks;
+    const int64_t m0 = (int64_t)(block / tiles_c) * CT, n0 = (int64_t)(block % tiles_c) * CT;
+    const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 8;   // 8 columns of 8 rows a thread
+    const int64_t c = n0 + col;
+    const int n = (int)max((int64_t)0, min((int64_t)CH, a.N - c));
+    float sb[CH], ci[CH];
+    load_sb(a, c, n, sb);
+#pragma unroll
+    for (int e = 0; e < CH; e++) ci[e] = a.q && e < n ? a.c[a.N + c + e] : 0.f;
+    uint32_t cmask[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < CH; e++) cmask[e >> 2] |= (code_mask(ci[e]) & 0xFFu) << (8 * (e & 3));
+#pragma unroll 1
+    for (int h = 0; h < 2; h++) {
+        uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int64_t m = m0 + row0 + 4 * h + i;
+            const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
+            float d[CH] = {}, pc[CH], cc[CH];
+            float ri = 0.f, sa = 0.f;
+            if (in) {
+                if (n > 0) load_dz<T>(a, m, c, n, d);
+                if (a.p) ri = a.r[a.M + m];
+                sa = a.s_a[a.a_step ? m : 0];
+            }
+            uint64_t r[CH];
+#pragma unroll
+            for (int e = 0; e < CH; e++) r[e] = a.sr ? sr_draw(a.seed, a.call, (uint64_t)(m * a.N + c + e)) : 0;
+#pragma unroll
+            for (int e = 0; e < CH; e++) {
+                // (past the edges dz is 0, and so are the codes: a draw is below 1)
+                pc[e] = a.sr ? code_sr(d[e] * sb[e], ri, draw_hi(r[e])) : code_rtn(d[e] * sb[e], ri);
+                cc[e] = a.sr ? code_sr(d[e] * sa, ci[e], draw_lo(r[e])) : code_rtn(d[e] * sa, ci[e]);
+            }
+            if (a.p && in && c < a.Np) {
+                const uint32_t mask = code_mask(ri);
+                const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
+                __builtin_memcpy(a.p + m * a.Np + c, w, CH);
+            }
+            qc[i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[0];
+            qc[i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[1];
+        }
+#pragma unroll
+        for (int g = 0; g < 2; g++) {
+            uint32_t w[4] = {qc[0][g], qc[1][g], qc[2][g], qc[3][g]};
+            turn4(w);
+#pragma unroll
+            for (int i = 0; i < 4; i++) *(uint32_t*)&tile[col + 4 * g + i][row0 + 4 * h] = w[i];
+        }
+    }
+    if (!a.q) return;
+    __syncthreads();
+    store_turned(tile, a.q, a.Mp, n0, a.N, m0, a.Mp);
 }
 
 struct BwdSpace {
-    int64_t Mp, Np, parts;
-    int64_t p, q, at, bt, r, c, pmax, psum, total;
+    int64_t Mp, Np, tiles_m, tiles_n;
+    int64_t p, q, at, bt, r, c, rmax, cmax, csum, total;
 };
 
 BwdSpace space(int64_t M, int64_t N, int64_t K) {
     BwdSpace s;
     s.Mp = up(M, kPad);
     s.Np = up(N, kPad);
-    s.parts = M < kParts ? M : kParts;
+    s.tiles_m = (M + SR - 1) / SR;
+    s.tiles_n = (N + SC - 1) / SC;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t o = at;
@@ -311,10 +307,11 @@ BwdSpace space(int64_t M, int64_t N, int64_t K) {
     s.q = take(N * s.Mp);
     s.at = take(K * s.Mp);
     s.bt = take(K * s.Np);
-    s.r = take(M * 4);
-    s.c = take(N * 4);
-    s.pmax = take(s.parts * N * 4);
-    s.psum = take(s.parts * N * 4);
+    s.r = take(M * 8);
+    s.c = take(N * 8);
+    s.rmax = take(s.tiles_n * M * 4);
+    s.cmax = take(s.tiles_m * N * 4);
+    s.csum = take(s.tiles_m * N * 4);
     s.total = at;
     return s;
 }
@@ -380,39 +377,39 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.M = M, d.N = N, d.Mp = w.Mp, d.Np = w.Np;
     d.a_step = s_a_n == 1 ? 0 : 1, d.b_step = s_b_n == 1 ? 0 : 1;
     d.act = act, d.sr = mode == NITI_ROUND_SR, d.seed = seed, d.call = call;
+    d.tiles_m = w.tiles_m, d.tiles_n = w.tiles_n;
     d.p = da ? (int8_t*)(base + w.p) : nullptr;
-    d.r = (float*)(base + w.r);
     d.q = db ? (int8_t*)(base + w.q) : nullptr;
+    d.r = (float*)(base + w.r);
     d.c = (float*)(base + w.c);
     d.dbias = dbias;
-    d.parts = w.parts;
-    if (db || dbias) {
-        d.pmax = (uint32_t*)(base + w.pmax);
-        d.psum = (float*)(base + w.psum);
-    }
-    if (by_type(type, [&](auto t) { return run_rows<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
-    if (db || dbias) {
-        hipLaunchKernelGGL(dz_cols_kernel, dim3((unsigned)((N + 63) / 64)), dim3(1024), 0, s, d);
-        if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
-    }
+    d.rmax = (uint32_t*)(base + w.rmax);
+    d.cmax = (uint32_t*)(base + w.cmax);
+    d.csum = (float*)(base + w.csum);
+    if (by_type(type, [&](auto t) {
+            hipLaunchKernelGGL((dz_stats_kernel<decltype(t)>), dim3((unsigned)(w.tiles_m * w.tiles_n)), dim3(256), 0, s, d);
+            return hipGetLastError();
+        }) != hipSuccess)
+        return NITI_ERR_HIP;
+    const int64_t cols = (N + 63) / 64;
+    hipLaunchKernelGGL(dz_join_kernel, dim3((unsigned)(cols + (M + 1023) / 1024)), dim3(1024), 0, s, d, (int)cols);
+    if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
+    if (!da && !db) return NITI_OK;
+    const int64_t tr = (M + CT - 1) / CT, tc = (N + CT - 1) / CT, tk = (K + CT - 1) / CT;
+    Turn ta{a, (int8_t*)(base + w.at), lda, M, w.Mp, K, db ? (int32_t)(tr * tk) : 0, (int32_t)tk};
+    Turn tb{b, (int8_t*)(base + w.bt), ldb, N, w.Np, K, da ? (int32_t)(tc * tk) : 0, (int32_t)tk};
+    if (by_type(type, [&](auto t) {
+            hipLaunchKernelGGL((dz_codes_kernel<decltype(t)>), dim3((unsigned)(ta.blocks + tb.blocks + tr * tc)), dim3(256), 0, s, d,
+                               ta, tb, (int)tc);
+            return hipGetLastError();
+        }) != hipSuccess)
+        return NITI_ERR_HIP;
     if (db) {
-        int8_t* at = (int8_t*)(base + w.at);
-        const int64_t tm = (M + 63) / 64, tn = (N + 63) / 64;
-        if (by_type(type, [&](auto t) {
-                hipLaunchKernelGGL((dz_cols_codes_kernel<decltype(t)>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, d, (int)tn);
-                return hipGetLastError();
-            }) != hipSuccess)
-            return NITI_ERR_HIP;
-        hipLaunchKernelGGL(dz_scale_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, s, d.c, N);
-        if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
-        if (transpose(a, lda, at, M, w.Mp, K, s) != hipSuccess) return NITI_ERR_HIP;
-        const LinArgs A{d.q, at, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE};
+        const LinArgs A{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0};
         if (linear_run(A, type, nullptr, 0, s) != hipSuccess) return NITI_ERR_HIP;
     }
     if (da) {
-        int8_t* bt = (int8_t*)(base + w.bt);
-        if (transpose(b, ldb, bt, N, w.Np, K, s) != hipSuccess) return NITI_ERR_HIP;
-        const LinArgs A{d.p, bt, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE};
+        const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0};
         if (linear_run(A, type, nullptr, 0, s) != hipSuccess) return NITI_ERR_HIP;
     }
     return NITI_OK;

@@ -71,8 +71,8 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* red, int wave)
 // summed again with its elements scaled down by 2^-80.
 constexpr float kDown = 0x1p-80f;
 
-__device__ __forceinline__ void store_codes(int8_t* q, int n, const float (&c)[CH]) {
-    uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]), pack4(c[4], c[5], c[6], c[7])};
+__device__ __forceinline__ void store_codes(int8_t* q, int n, const float (&c)[CH], uint32_t mask) {
+    uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]) & mask, pack4(c[4], c[5], c[6], c[7]) & mask};
     if (n >= CH) {
         __builtin_memcpy(q, w, CH);
         return;
@@ -91,9 +91,9 @@ __device__ __forceinline__ void put_piece(const RowArgs& a, int64_t m, int64_t c
         for (int e = 0; e < CH; e++) {
             const float u = a.sr ? draw_hi(sr_draw(a.seed, a.call, (uint64_t)((a.m0 + m) * a.D + c + e))) : 0.f;
             code[e] = a.sr ? code_sr(v[e], rs.inv, u) : code_rtn(v[e], rs.inv);
-            v[e] = code[e] * rs.scale;
+            v[e] = code_value(code[e]) * rs.scale;
         }
-        store_codes(a.q + m * a.ldq + c, n, code);
+        store_codes(a.q + m * a.ldq + c, n, code, code_mask(rs.inv));
     }
     if (a.y) store_some((T*)a.y + m * a.ldy + c, n, v);
 }

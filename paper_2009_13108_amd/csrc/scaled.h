@@ -107,31 +107,47 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top_bits) {
     return r;
 }
 
-// Code of v, as a float in [-127, 127]; bad rows (inv 0) give 0 whatever v is.
-__device__ __forceinline__ float code_rtn(float v, float inv) {
-    const float r = rintf(v * inv);
-    return fminf(fmaxf(inv > 0.f ? r : 0.f, -127.f), 127.f);
-}
-// Stochastically: floor(v + u) is v on average over u in [0, 1).
+// Codes as floats that begin at kCode = 1.5 * 2^23: there a step of a float is 1,
+// so that one multiply-add rounds v * inv to the nearest integer, ties to even, and
+// leaves the code as the float's lowest byte.  For a finite row |v * inv| is at most
+// 127 and a rounding error, which rounds to 127.  Rows that are not finite (inv 0)
+// may leave anything: their words are masked (see code_mask).
+constexpr float kCode = 12582912.f;
+__device__ __forceinline__ float code_rtn(float v, float inv) { return __builtin_fmaf(v, inv, kCode); }
+// Stochastically: floor(v * inv + u) is v * inv on average over u in [0, 1).
 __device__ __forceinline__ float code_sr(float v, float inv, float u) {
-    const float r = floorf(v * inv + u);
-    return fminf(fmaxf(inv > 0.f ? r : 0.f, -127.f), 127.f);
+    return __builtin_amdgcn_fmed3f(floorf(__builtin_fmaf(v, inv, u)), -127.f, 127.f) + kCode;
+}
+__device__ __forceinline__ float code_value(float c) { return c - kCode; }
+// All bits for a row with codes, none for one without.
+__device__ __forceinline__ uint32_t code_mask(float inv) { return inv > 0.f ? ~0u : 0u; }
+// Four codes in a word, lowest first.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0C);
+    return lo | hi;
 }
 // Uniform fractions of 24 bits from a draw.
 __device__ __forceinline__ float draw_hi(uint64_t r) { return (float)(uint32_t)(r >> 40) * 0x1p-24f; }
 __device__ __forceinline__ float draw_lo(uint64_t r) { return (float)((uint32_t)(r >> 8) & 0xFFFFFFu) * 0x1p-24f; }
-
-// Four codes in a word, lowest first.
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-    return ((uint32_t)(int)a & 0xFFu) | (((uint32_t)(int)b & 0xFFu) << 8) | (((uint32_t)(int)c & 0xFFu) << 16) |
-           ((uint32_t)(int)d << 24);
-}
 
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
     return v;
 }
+
+// exp(x) for |x| <= 80, within three units in the last place: x log2(e) in two parts, the
+// second as a first-order factor.  The library's expf, which also takes the ends
+// of the range, costs about twice that, and an IEEE division ten instructions:
+// the slopes bounded the passes over a gradient with both.
+__device__ __forceinline__ float exp_mid(float x) {
+    const float t = x * 1.44269502e+00f;                       // log2(e) rounded to 32 bits
+    const float r = __builtin_fmaf(x, 1.92596303e-08f, __builtin_fmaf(x, 1.44269502e+00f, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r * 6.93147182e-01f, e);
+}
+__device__ __forceinline__ float sigmoid_mid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_mid(-x)); }
 
 // Activations and their derivatives.  Below -80 a sigmoid is under 2^-115 and
 // its argument is held there, so that an infinity gives the limit and no NaN.
@@ -143,7 +159,7 @@ __device__ __forceinline__ float act_value(int act, float z) {
     }
     if (act == NITI_ACT_SILU) {
         const float c = z < -80.f ? -80.f : z;
-        return c / (1.f + expf(-c));
+        return c * sigmoid_mid(c > 80.f ? 80.f : c);
     }
     return z;
 }
@@ -165,11 +181,11 @@ __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
     if (act == NITI_ACT_GELU) {
         const float c = z < -40.f ? -40.f : (z > 40.f ? 40.f : z);
-        return 0.5f * (1.f + erff(c * 0.70710678118654752f)) + c * expf(-0.5f * c * c) * 0.39894228040143268f;
+        return 0.5f * (1.f + erff(c * 0.70710678118654752f)) + c * exp_mid(fmaxf(-0.5f * c * c, -80.f)) * 0.39894228040143268f;
     }
     if (act == NITI_ACT_SILU) {
         const float c = z < -80.f ? -80.f : (z > 80.f ? 80.f : z);
-        const float s = 1.f / (1.f + expf(-c));
+        const float s = sigmoid_mid(c);
         return s * (1.f + c * (1.f - s));
     }
     return 1.f;
@@ -182,6 +198,21 @@ constexpr int64_t kMaxSum = (int64_t)1 << 17;   // shorter sums of int8 products
 // A row stride: 0 only for operands that are read.
 inline bool bad_ld(int64_t ld, int64_t cols, bool out) {
     return ld >= kMaxLd || ld < 0 || (ld < cols && (out || ld != 0));
+}
+
+// The slopes of several values, in their place.
+template <int N>
+__device__ __forceinline__ void act_slopes(int act, float (&v)[N]) {
+    if (act == NITI_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_slope(NITI_ACT_RELU, v[e]);
+    } else if (act == NITI_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_slope(NITI_ACT_GELU, v[e]);
+    } else if (act == NITI_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; e++) v[e] = act_slope(NITI_ACT_SILU, v[e]);
+    }
 }
 
 // Calls f(T()) with the element type.

@@ -28,7 +28,9 @@ def close(got, want, bound, dtype=torch.float32, what=""):
     assert torch.equal(torch.isnan(got), torch.isnan(want)), what + ": NaNs differ"
     fine = torch.isfinite(want)
     assert torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)]), what
-    room = (torch.as_tensor(bound, dtype=torch.float64).cpu() + UNIT[dtype] * want.abs() * 1.01 + STEP[dtype]).expand(want.shape)
+    # the value before the store is x with |x - want| <= bound, and its rounding is off by UNIT |x| <= UNIT (|want| + bound)
+    bound = torch.as_tensor(bound, dtype=torch.float64).cpu()
+    room = (bound + UNIT[dtype] * (want.abs() + bound) * 1.01 + STEP[dtype]).expand(want.shape)
     off = (got - want).abs()
     bad = (off > room) & fine
     assert not bad.any(), "%s: %d of %d off, by up to %g (allowed there %g)" % (
