@@ -89,17 +89,18 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top_bits, float unit)
     return b;
 }
 
+// Square roots and reciprocals are the hardware's, good to one unit in the last
+// place; the IEEE sequences around them took as long as the memory traffic.
 constexpr float kUnitM = 1.f / 16129.f;                       // 1 / 127^2
 constexpr float kUnitV = 1.f / (255.f * 255.f * 255.f * 255.f);   // 1 / 255^4
 
-template <typename TP, typename TG, int BITS>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
-    const int k = find_tensor(tab.start, blockIdx.x);
-    const Entry& E = tab.e[k];
-    const Step& S = tab.s;
-    const int64_t i = (int64_t)((int)blockIdx.x - tab.start[k]) * kChunk + threadIdx.x * PT;
+// A thread's elements i .. i + PT - 1 of a tensor.  FULL: all of the chunk's are
+// there, and no load is in a branch, where it would be waited for.
+template <typename TP, typename TG, int BITS, bool FULL>
+__device__ __forceinline__ void adamw_elements(const Entry& E, const Step& S, int64_t i) {
     const int64_t left = E.n - i;
-    const int n = left >= PT ? PT : (left > 0 ? (int)left : 0);
+    const int n = FULL || left >= PT ? PT : (left > 0 ? (int)left : 0);
+    const float gs = S.gscale ? *S.gscale : 1.f;
     float p[PT], g[PT], m[PT], v[PT];
     load_some((const TP*)E.p + i, n, p);
     load_some((const TG*)E.g + i, n, g);
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
         int8_t cm[PT] = {};
         uint8_t cv[PT] = {};
         float ms = 0.f, vs = 0.f;
-        if (n == PT) {
+        if (FULL || n == PT) {
             __builtin_memcpy(cm, (const int8_t*)E.m + i, PT);
             __builtin_memcpy(cv, (const uint8_t*)E.v + i, PT);
         } else {
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
             for (int e = 0; e < PT; e++)
                 if (e < n) cm[e] = ((const int8_t*)E.m)[i + e], cv[e] = ((const uint8_t*)E.v)[i + e];
         }
-        if (n > 0) ms = E.ms[i / kBlock], vs = E.vs[i / kBlock];
+        if (FULL || n > 0) ms = E.ms[i / kBlock], vs = E.vs[i / kBlock];
 #pragma unroll
         for (int e = 0; e < PT; e++) {
             const float c = (float)cm[e], d = (float)cv[e];
@@ -126,13 +127,12 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
             v[e] = (d * d) * (d * d) * vs;
         }
     }
-    const float gs = S.gscale ? *S.gscale : 1.f;
 #pragma unroll
     for (int e = 0; e < PT; e++) {
         const float x = g[e] * gs;
         m[e] = S.b1 * m[e] + S.c1 * x;
         v[e] = S.b2 * v[e] + S.c2 * (x * x);
-        p[e] = p[e] * S.keep - S.lr * (m[e] / (sqrtf(v[e]) * S.root + S.eps));
+        p[e] = p[e] * S.keep - S.lr * (m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) * S.root + S.eps));
     }
     store_some((TP*)E.p + i, n, p);
     if constexpr (BITS == 32) {
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
             if (S.sr) r = sr_draw(S.seed, S.call, pair0 + e / 2);
 #pragma unroll
             for (int o = 0; o < 2; o++) {
-                float rm = 127.f * sqrtf(fabsf(m[e + o]) * bm.inv);
-                float rv = 255.f * sqrtf(sqrtf(v[e + o] * bv.inv));
+                float rm = 127.f * __builtin_amdgcn_sqrtf(fabsf(m[e + o]) * bm.inv);
+                float rv = 255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(v[e + o] * bv.inv));
                 if (S.sr) {
                     const uint32_t w = (uint32_t)(r >> (32 * o));
                     rm = floorf(rm + (float)(w & 0xFFFFu) * 0x1p-16f);
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
                 cv[e + o] = (uint8_t)(int)rv;
             }
         }
-        if (n == PT) {
+        if (FULL || n == PT) {
             __builtin_memcpy((int8_t*)E.m + i, cm, PT);
             __builtin_memcpy((uint8_t*)E.v + i, cv, PT);
         } else {
@@ -177,8 +177,19 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
             for (int e = 0; e < PT; e++)
                 if (e < n) ((int8_t*)E.m)[i + e] = cm[e], ((uint8_t*)E.v)[i + e] = cv[e];
         }
-        if ((threadIdx.x & 31) == 0 && n > 0) E.ms[i / kBlock] = bm.scale, E.vs[i / kBlock] = bv.scale;
+        if ((threadIdx.x & 31) == 0 && (FULL || n > 0)) E.ms[i / kBlock] = bm.scale, E.vs[i / kBlock] = bv.scale;
     }
+}
+
+template <typename TP, typename TG, int BITS>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
+    const int k = find_tensor(tab.start, blockIdx.x);
+    const Entry& E = tab.e[k];
+    const int64_t first = (int64_t)((int)blockIdx.x - tab.start[k]) * kChunk;
+    if (first + kChunk <= E.n)
+        adamw_elements<TP, TG, BITS, true>(E, tab.s, first + threadIdx.x * PT);
+    else
+        adamw_elements<TP, TG, BITS, false>(E, tab.s, first + threadIdx.x * PT);
 }
 
 // Values of 8-bit states: p and g are the outputs for m and v here.

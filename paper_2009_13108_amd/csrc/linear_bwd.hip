@@ -14,13 +14,14 @@
 // products, by the forward kernels.  dy and z are read twice, the second time
 // mostly from the last-level cache; holding dz for step 3 would round it or cost
 // four bytes an element each way.
+#include <type_traits>
+
 #include "linear.h"
 
 namespace niti {
 
 namespace {
 
-constexpr int CH = 8;            // elements of a thread's piece of a row
 constexpr int SR = 32, SC = 256; // tile of step 1
 constexpr int CT = 128;          // tile of step 3
 constexpr int CP = CT + 4;       // its LDS pitch: lanes that write one row group hit distinct banks, two by two
@@ -50,18 +51,43 @@ struct DzArgs {
     float* csum;      // [tiles_m][N]
 };
 
-// dz of n consecutive elements from (m, c) on; zeros past them.
-template <typename T>
-__device__ __forceinline__ void load_dz(const DzArgs& a, int64_t m, int64_t c, int n, float (&d)[CH]) {
-    load_some((const T*)a.dy + m * a.lddy + c, n, d);
-    if (a.act != NITI_ACT_NONE) {
-        float z[CH];
-        load_some((const T*)a.z + m * a.ldz + c, n, z);
-        act_slopes(a.act, z);
+// dz of 8 columns from c on of rows m, m + step, ...; zeros past the edges.  All
+// loads go out before the first is used (see load_piece).  KIND: the number of
+// columns is a multiple of 8 (2), is at least 8 (1), or neither (0).
+template <typename T, int KIND, int ROWS>
+struct DzRows {
+    Piece<T> y[KIND ? ROWS : 1], z[KIND ? ROWS : 1];
+    __device__ __forceinline__ void load(const DzArgs& a, int64_t m, int64_t step, int c) {
+        if constexpr (KIND > 0) {
 #pragma unroll
-        for (int e = 0; e < CH; e++) d[e] = e < n ? d[e] * z[e] : 0.f;
+            for (int i = 0; i < ROWS; i++) {
+                const int64_t r = min(m + i * step, a.M - 1);
+                const T* dy = (const T*)a.dy + r * a.lddy;
+                y[i] = load_piece<T, KIND == 2>(dy, c, (int)a.N);
+                z[i] = load_piece<T, KIND == 2>(a.act != NITI_ACT_NONE ? (const T*)a.z + r * a.ldz : dy, c, (int)a.N);
+            }
+        }
     }
-}
+    __device__ __forceinline__ void get(const DzArgs& a, int i, int64_t m, int c, float (&d)[CH]) {
+        const int N = (int)a.N;
+        float s[CH];
+        if constexpr (KIND > 0) {
+            piece_values<T, KIND == 2>(y[i], c, N, d);
+            piece_values<T, KIND == 2>(z[i], c, N, s);
+        } else {
+            const int64_t r = min(m, a.M - 1);
+            load_some((const T*)a.dy + r * a.lddy + c, N - c, d);
+            if (a.act != NITI_ACT_NONE) load_some((const T*)a.z + r * a.ldz + c, N - c, s);
+        }
+        if (a.act != NITI_ACT_NONE) {
+            act_slopes(a.act, s);
+#pragma unroll
+            for (int e = 0; e < CH; e++) d[e] *= s[e];
+        }
+#pragma unroll
+        for (int e = 0; e < CH; e++) d[e] = m < a.M ? d[e] : 0.f;
+    }
+};
 
 // b's scales of n columns from c on.
 __device__ __forceinline__ void load_sb(const DzArgs& a, int64_t c, int n, float (&v)[CH]) {
@@ -70,14 +96,16 @@ __device__ __forceinline__ void load_sb(const DzArgs& a, int64_t c, int n, float
 }
 
 // Step 1.  A thread takes 8 columns of 4 rows; 32 lanes a row, 8 threads a column group.
-template <typename T>
+template <typename T, int KIND>
 __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     __shared__ float ssum[8][SC + 8];
     __shared__ uint32_t smax[8][SC + 8];
     const int64_t tm = blockIdx.x / a.tiles_n, tn = blockIdx.x % a.tiles_n;
     const int col = (threadIdx.x & 31) * CH, grp = threadIdx.x >> 5;
-    const int64_t c = tn * SC + col;
-    const int n = (int)max((int64_t)0, min((int64_t)CH, a.N - c));
+    const int c = (int)(tn * SC + col);
+    const int n = max(0, min(CH, (int)a.N - c));
+    DzRows<T, KIND, SR / 8> rows;
+    rows.load(a, tm * SR + grp, 8, c);
     float sb[CH], sum[CH];
     uint32_t mx[CH];
     load_sb(a, c, n, sb);
@@ -86,20 +114,19 @@ __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
 #pragma unroll
     for (int i = 0; i < SR / 8; i++) {
         const int64_t m = tm * SR + i * 8 + grp;
-        if (m >= a.M) continue;   // the same for the row's lanes
-        const float sa = a.s_a[a.a_step ? m : 0];
+        const float sa = a.s_a[a.a_step ? min(m, a.M - 1) : 0];
         float d[CH];
-        load_dz<T>(a, m, c, n, d);
+        rows.get(a, i, m, c, d);
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < CH; e++) {
             sum[e] += d[e];
             mx[e] = max(mx[e], mag_bits(d[e] * sa));
-            top = max(top, mag_bits(d[e] * sb[e]));   // (zeros past the edge)
+            top = max(top, mag_bits(d[e] * sb[e]));   // (zeros past the edges)
         }
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 32));
-        if ((threadIdx.x & 31) == 0) a.rmax[tn * a.M + m] = top;
+        if ((threadIdx.x & 31) == 0 && m < a.M) a.rmax[tn * a.M + m] = top;
     }
 #pragma unroll
     for (int e = 0; e < CH; e++) ssum[grp][col + e] = sum[e], smax[grp][col + e] = mx[e];
@@ -217,7 +244,7 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
 }
 
 // Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
-template <typename T>
+template <typename T, int KIND>
 __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int tiles_c) {
     __shared__ __attribute__((aligned(16))) int8_t tile[CT][CP];
     int block = blockIdx.x;
@@ -233,8 +260,8 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
     block -= tb.blocks;
     const int64_t m0 = (int64_t)(block / tiles_c) * CT, n0 = (int64_t)(block % tiles_c) * CT;
     const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 8;   // 8 columns of 8 rows a thread
-    const int64_t c = n0 + col;
-    const int n = (int)max((int64_t)0, min((int64_t)CH, a.N - c));
+    const int c = (int)(n0 + col);
+    const int n = max(0, min(CH, (int)a.N - c));
     float sb[CH], ci[CH];
     load_sb(a, c, n, sb);
 #pragma unroll
@@ -245,17 +272,16 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
 #pragma unroll 1
     for (int h = 0; h < 2; h++) {
         uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
+        DzRows<T, KIND, 4> rows;
+        rows.load(a, m0 + row0 + 4 * h, 1, c);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int64_t m = m0 + row0 + 4 * h + i;
             const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
-            float d[CH] = {}, pc[CH], cc[CH];
-            float ri = 0.f, sa = 0.f;
-            if (in) {
-                if (n > 0) load_dz<T>(a, m, c, n, d);
-                if (a.p) ri = a.r[a.M + m];
-                sa = a.s_a[a.a_step ? m : 0];
-            }
+            float d[CH], pc[CH], cc[CH];
+            rows.get(a, i, m, c, d);
+            const int64_t mi = min(m, a.M - 1);
+            const float ri = a.p ? a.r[a.M + mi] : 0.f, sa = a.s_a[a.a_step ? mi : 0];
             uint64_t r[CH];
 #pragma unroll
             for (int e = 0; e < CH; e++) r[e] = a.sr ? sr_draw(a.seed, a.call, (uint64_t)(m * a.N + c + e)) : 0;
@@ -284,6 +310,31 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
     if (!a.q) return;
     __syncthreads();
     store_turned(tile, a.q, a.Mp, n0, a.N, m0, a.Mp);
+}
+
+// Calls f with the column count's KIND.
+template <typename F>
+hipError_t by_kind(int64_t N, F f) {
+    if (N % CH == 0) return f(std::integral_constant<int, 2>());
+    if (N > CH) return f(std::integral_constant<int, 1>());
+    return f(std::integral_constant<int, 0>());
+}
+
+template <typename T>
+hipError_t run_stats(const DzArgs& a, hipStream_t stream) {
+    return by_kind(a.N, [&](auto k) {
+        hipLaunchKernelGGL((dz_stats_kernel<T, decltype(k)::value>), dim3((unsigned)(a.tiles_m * a.tiles_n)), dim3(256), 0, stream, a);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t run_codes(const DzArgs& a, const Turn& ta, const Turn& tb, int64_t tiles, int tiles_c, hipStream_t stream) {
+    return by_kind(a.N, [&](auto k) {
+        hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(256), 0,
+                           stream, a, ta, tb, tiles_c);
+        return hipGetLastError();
+    });
 }
 
 struct BwdSpace {
@@ -386,11 +437,7 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.rmax = (uint32_t*)(base + w.rmax);
     d.cmax = (uint32_t*)(base + w.cmax);
     d.csum = (float*)(base + w.csum);
-    if (by_type(type, [&](auto t) {
-            hipLaunchKernelGGL((dz_stats_kernel<decltype(t)>), dim3((unsigned)(w.tiles_m * w.tiles_n)), dim3(256), 0, s, d);
-            return hipGetLastError();
-        }) != hipSuccess)
-        return NITI_ERR_HIP;
+    if (by_type(type, [&](auto t) { return run_stats<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
     const int64_t cols = (N + 63) / 64;
     hipLaunchKernelGGL(dz_join_kernel, dim3((unsigned)(cols + (M + 1023) / 1024)), dim3(1024), 0, s, d, (int)cols);
     if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
@@ -398,11 +445,7 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     const int64_t tr = (M + CT - 1) / CT, tc = (N + CT - 1) / CT, tk = (K + CT - 1) / CT;
     Turn ta{a, (int8_t*)(base + w.at), lda, M, w.Mp, K, db ? (int32_t)(tr * tk) : 0, (int32_t)tk};
     Turn tb{b, (int8_t*)(base + w.bt), ldb, N, w.Np, K, da ? (int32_t)(tc * tk) : 0, (int32_t)tk};
-    if (by_type(type, [&](auto t) {
-            hipLaunchKernelGGL((dz_codes_kernel<decltype(t)>), dim3((unsigned)(ta.blocks + tb.blocks + tr * tc)), dim3(256), 0, s, d,
-                               ta, tb, (int)tc);
-            return hipGetLastError();
-        }) != hipSuccess)
+    if (by_type(type, [&](auto t) { return run_codes<decltype(t)>(d, ta, tb, tr * tc, (int)tc, s); }) != hipSuccess)
         return NITI_ERR_HIP;
     if (db) {
         const LinArgs A{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0};

@@ -20,7 +20,6 @@ namespace niti {
 
 namespace {
 
-constexpr int CH = 8;          // elements of a thread's piece
 constexpr int NT_LONG = 1024;  // threads of the kernels for longer rows
 constexpr int kMaxParts = 512; // partial rows of dgain
 
@@ -99,7 +98,8 @@ __device__ __forceinline__ void put_piece(const RowArgs& a, int64_t m, int64_t c
 }
 
 // NW waves per row, VPT pieces per thread; NORM: the norm, otherwise codes of x.
-template <typename T, int NW, int VPT, bool NORM>
+// TG: type of the gain.  All loads of a row go out together.
+template <typename T, typename TG, int NW, int VPT, bool NORM, bool WHOLE>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_fwd_kernel(RowArgs a) {
     constexpr int NT = 64 * NW;
     __shared__ float red_s[NW], red_t[NW];
@@ -109,36 +109,39 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_fwd_kernel(RowArg
     if (m >= a.M) return;   // a whole wave of a workgroup that has no barrier
     const int t = NW == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     const int D = (int)a.D;
+    const T* x = (const T*)a.x + m * a.ldx;
+    const T* res = NORM && a.res ? (const T*)a.res + m * a.ldres : nullptr;
+    Piece<T> px[VPT], pr[VPT];
+    Piece<TG> pg[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; i++) px[i] = load_piece<T, WHOLE>(x, (i * NT + t) * CH, D);
+    if constexpr (NORM) {
+        // without a residual x again, which costs no traffic, in place of a branch
+#pragma unroll
+        for (int i = 0; i < VPT; i++) pr[i] = load_piece<T, WHOLE>(res ? res : x, (i * NT + t) * CH, D);
+#pragma unroll
+        for (int i = 0; i < VPT; i++) pg[i] = load_piece<TG, WHOLE>((const TG*)a.gain, (i * NT + t) * CH, D);
+    }
     float v[VPT][CH];
 #pragma unroll
-    for (int i = 0; i < VPT; i++) {
-        const int c = (i * NT + t) * CH;
-        load_some((const T*)a.x + m * a.ldx + c, D - c, v[i]);
-    }
-    uint32_t top = 0;
+    for (int i = 0; i < VPT; i++) piece_values<T, WHOLE>(px[i], (i * NT + t) * CH, D, v[i]);
     if constexpr (NORM) {
-        if (a.res) {
-            float r[VPT][CH];
-#pragma unroll
-            for (int i = 0; i < VPT; i++) {
-                const int c = (i * NT + t) * CH;
-                load_some((const T*)a.res + m * a.ldres + c, D - c, r[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < VPT; i++)
-#pragma unroll
-                for (int e = 0; e < CH; e++) v[i][e] += r[i][e];
-        }
         float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < VPT; i++)
+        for (int i = 0; i < VPT; i++) {
+            float r[CH];
+            piece_values<T, WHOLE>(pr[i], (i * NT + t) * CH, D, r);
 #pragma unroll
-            for (int e = 0; e < CH; e++) ss += v[i][e] * v[i][e];
+            for (int e = 0; e < CH; e++) {
+                v[i][e] = res ? v[i][e] + r[e] : v[i][e];
+                ss += v[i][e] * v[i][e];
+            }
+        }
         if (a.h) {
 #pragma unroll
             for (int i = 0; i < VPT; i++) {
                 const int c = (i * NT + t) * CH;
-                store_some((T*)a.h + m * a.ldh + c, D - c, v[i]);
+                if (c < D) store_some((T*)a.h + m * a.ldh + c, WHOLE ? CH : D - c, v[i]);
             }
         }
         ss = row_sum<NW>(ss, red_s, wave);
@@ -157,29 +160,26 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_fwd_kernel(RowArg
         if (a.rstd && t == 0) a.rstd[m] = rstd * down;
 #pragma unroll
         for (int i = 0; i < VPT; i++) {
-            const int c = (i * NT + t) * CH;
             float g[CH];
-            load_typed(a.gain, a.gain_type, c, D - c, g);
+            piece_values<TG, WHOLE>(pg[i], (i * NT + t) * CH, D, g);
 #pragma unroll
             for (int e = 0; e < CH; e++) v[i][e] = (v[i][e] * down) * rstd * g[e];
         }
     }
     RowScale rs{0.f, 0.f};
     if (a.q) {
+        uint32_t top = 0;   // (elements past the row are zeros)
 #pragma unroll
-        for (int i = 0; i < VPT; i++) {
-            const int n = D - (i * NT + t) * CH;   // elements past the row are not part of it
+        for (int i = 0; i < VPT; i++)
 #pragma unroll
-            for (int e = 0; e < CH; e++)
-                if (e < n) top = max(top, mag_bits(v[i][e]));
-        }
+            for (int e = 0; e < CH; e++) top = max(top, mag_bits(v[i][e]));
         rs = row_scale(row_max<NW>(top, red_m, wave));
         if (t == 0) a.scale[m] = rs.scale;
     }
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         const int c = (i * NT + t) * CH;
-        if (c < D) put_piece<T>(a, m, c, D - c, v[i], rs);
+        if (c < D) put_piece<T>(a, m, c, WHOLE ? CH : D - c, v[i], rs);
     }
 }
 
@@ -272,7 +272,7 @@ struct RowBwdArgs {
     int gain_type;
 };
 
-template <typename T, int NW, int VPT>
+template <typename T, typename TG, int NW, int VPT, bool WHOLE>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwdArgs a) {
     constexpr int NT = 64 * NW;
     constexpr int ROWS = NW == 1 ? 4 : 1;   // rows of a workgroup at a time
@@ -285,21 +285,43 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         const int c = (i * NT + t) * CH;
-        load_typed(a.gain, a.gain_type, c, D - c, g[i]);
+        piece_values<TG, WHOLE>(load_piece<TG, WHOLE>((const TG*)a.gain, c, D), c, D, g[i]);
 #pragma unroll
         for (int e = 0; e < CH; e++) dg[i][e] = 0.f;
     }
-    int par = 0;
-    for (int64_t m = (int64_t)blockIdx.x * ROWS + (NW == 1 ? wave : 0); m < a.M; m += (int64_t)gridDim.x * ROWS, par ^= 1) {
-        float dy[VPT][CH], xh[VPT][CH];
-        const float rstd = a.rstd[m];
+    // A row's loads go out while the row before it is worked on (past the last row, that one's again).
+    Piece<T> dyr[VPT], hr[VPT], er[VPT];
+    float rstd_r;
+    auto load = [&](int64_t m) {
+        m = min(m, a.M - 1);
+        rstd_r = a.rstd[m];
+        const T* dy = (const T*)a.dy + m * a.lddy;
+        const T* h = (const T*)a.h + m * a.ldh;
+        const T* dh = a.dh ? (const T*)a.dh + m * a.lddh : dy;
 #pragma unroll
         for (int i = 0; i < VPT; i++) {
             const int c = (i * NT + t) * CH;
-            load_some((const T*)a.dy + m * a.lddy + c, D - c, dy[i]);
-            load_some((const T*)a.h + m * a.ldh + c, D - c, xh[i]);
+            dyr[i] = load_piece<T, WHOLE>(dy, c, D);
+            hr[i] = load_piece<T, WHOLE>(h, c, D);
+            er[i] = load_piece<T, WHOLE>(dh, c, D);
         }
+    };
+    int par = 0;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t m = (int64_t)blockIdx.x * ROWS + (NW == 1 ? wave : 0);
+    load(m);
+    for (; m < a.M; m += step, par ^= 1) {
+        float dy[VPT][CH], xh[VPT][CH], r[VPT][CH];
+        const float rstd = rstd_r;
         float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < VPT; i++) {
+            const int c = (i * NT + t) * CH;
+            piece_values<T, WHOLE>(dyr[i], c, D, dy[i]);
+            piece_values<T, WHOLE>(hr[i], c, D, xh[i]);
+            piece_values<T, WHOLE>(er[i], c, D, r[i]);
+        }
+        load(m + step);
 #pragma unroll
         for (int i = 0; i < VPT; i++)
 #pragma unroll
@@ -315,14 +337,12 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
         for (int i = 0; i < VPT; i++) {
             const int c = (i * NT + t) * CH;
             if (c >= D) continue;
-            float r[CH];
-            if (a.dh) load_some((const T*)a.dh + m * a.lddh + c, D - c, r);
 #pragma unroll
             for (int e = 0; e < CH; e++) {
                 const float d = rstd * (dy[i][e] - xh[i][e] * mean);
-                r[e] = a.dh ? d + r[e] : d;
+                r[i][e] = a.dh ? d + r[i][e] : d;
             }
-            store_some((T*)a.dx + m * a.lddx + c, D - c, r);
+            store_some((T*)a.dx + m * a.lddx + c, WHOLE ? CH : D - c, r[i]);
         }
     }
     if (!a.part) return;
@@ -390,46 +410,70 @@ __global__ __launch_bounds__(NT_LONG) void row_bwd_long_kernel(RowBwdArgs a) {
     }
 }
 
-// dgain = the partial rows' sum: 64 columns a workgroup, the partial rows
-// shared by 16 groups of threads and joined in order.
+// dgain = the partial rows' sum: 32 columns a workgroup, the partial rows
+// shared by 32 groups of threads, eight loads of each in flight, and joined in order.
 __global__ __launch_bounds__(1024) void dgain_kernel(const float* part, float* dgain, int64_t parts, int64_t D) {
-    __shared__ float s[16][64];
-    const int col = threadIdx.x & 63, grp = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + col;
+    __shared__ float s[32][33];
+    const int col = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + col;
     float v = 0.f;
     if (c < D)
-        for (int64_t p = grp; p < parts; p += 16) v += part[p * D + c];
+        for (int64_t p = grp; p < parts; p += 256) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = p + 32 * i < parts ? part[(p + 32 * i) * D + c] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) v += x[i];
+        }
     s[grp][col] = v;
     __syncthreads();
+    // eight partial sums of four groups, then those
+    if (threadIdx.x < 256) {
+        const int o = threadIdx.x >> 5;
+        s[o][col] = (s[o][col] + s[o + 8][col]) + (s[o + 16][col] + s[o + 24][col]);
+    }
+    __syncthreads();
     if (grp == 0 && c < D) {
-        for (int i = 1; i < 16; i++) v += s[i][col];
+        v = s[0][col];
+        for (int i = 1; i < 8; i++) v += s[i][col];
         dgain[c] = v;
     }
 }
 
 inline int pieces(int64_t D) { return (int)((D + CH - 1) / CH); }
 
-template <typename T, int NW, int VPT, bool NORM>
+template <typename T, typename TG, int NW, int VPT, bool NORM>
 hipError_t launch_fwd(const RowArgs& a, hipStream_t stream) {
-    const int64_t grid = NW == 1 ? (a.M + 3) / 4 : a.M;
-    hipLaunchKernelGGL((row_fwd_kernel<T, NW, VPT, NORM>), dim3((unsigned)grid), dim3(NW == 1 ? 256 : 64 * NW), 0, stream, a);
+    const dim3 grid((unsigned)(NW == 1 ? (a.M + 3) / 4 : a.M)), block(NW == 1 ? 256 : 64 * NW);
+    if (a.D % CH == 0)
+        hipLaunchKernelGGL((row_fwd_kernel<T, TG, NW, VPT, NORM, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((row_fwd_kernel<T, TG, NW, VPT, NORM, false>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 
+template <typename T, typename TG, bool NORM>
+hipError_t run_short_rows(const RowArgs& a, hipStream_t stream) {
+    const int p = pieces(a.D);
+    if (p <= 64) return launch_fwd<T, TG, 1, 1, NORM>(a, stream);
+    if (p <= 128) return launch_fwd<T, TG, 1, 2, NORM>(a, stream);
+    if (p <= 256) return launch_fwd<T, TG, 1, 4, NORM>(a, stream);
+    if (p <= 512) return launch_fwd<T, TG, 4, 2, NORM>(a, stream);
+    if (p <= 1024) return launch_fwd<T, TG, 4, 4, NORM>(a, stream);
+    if (p <= 2048) return launch_fwd<T, TG, 16, 2, NORM>(a, stream);
+    return launch_fwd<T, TG, 16, 4, NORM>(a, stream);
+}
+
+// Rows below one piece, above 32768 elements, and a gain of another 16-bit type than x go by the kernel for rows of any length.
 template <typename T, bool NORM>
 hipError_t run_rows(const RowArgs& a, hipStream_t stream) {
-    const int p = pieces(a.D);
-    if (a.D > 32768) {
-        hipLaunchKernelGGL((row_fwd_long_kernel<T, NORM>), dim3((unsigned)a.M), dim3(NT_LONG), 0, stream, a);
-        return hipGetLastError();
+    if (a.D >= CH && a.D <= 32768) {
+        if (!NORM || a.gain_type == type_id<T>()) return run_short_rows<T, T, NORM>(a, stream);
+        if constexpr (NORM)
+            if (a.gain_type == NITI_F32) return run_short_rows<T, float, NORM>(a, stream);
     }
-    if (p <= 64) return launch_fwd<T, 1, 1, NORM>(a, stream);
-    if (p <= 128) return launch_fwd<T, 1, 2, NORM>(a, stream);
-    if (p <= 256) return launch_fwd<T, 1, 4, NORM>(a, stream);
-    if (p <= 512) return launch_fwd<T, 4, 2, NORM>(a, stream);
-    if (p <= 1024) return launch_fwd<T, 4, 4, NORM>(a, stream);
-    if (p <= 2048) return launch_fwd<T, 16, 2, NORM>(a, stream);
-    return launch_fwd<T, 16, 4, NORM>(a, stream);
+    hipLaunchKernelGGL((row_fwd_long_kernel<T, NORM>), dim3((unsigned)a.M), dim3(NT_LONG), 0, stream, a);
+    return hipGetLastError();
 }
 
 // A launch holds fewer than 2^32 threads: very many rows go in slabs.
@@ -452,28 +496,40 @@ hipError_t run_fwd(RowArgs a, hipStream_t stream) {
     }
 }
 
-template <typename T, int NW, int VPT>
+template <typename T, typename TG, int NW, int VPT>
 hipError_t launch_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
-    hipLaunchKernelGGL((row_bwd_kernel<T, NW, VPT>), dim3((unsigned)parts), dim3(NW == 1 ? 256 : 64 * NW), 0, stream, a);
+    const dim3 grid((unsigned)parts), block(NW == 1 ? 256 : 64 * NW);
+    if (a.D % CH == 0)
+        hipLaunchKernelGGL((row_bwd_kernel<T, TG, NW, VPT, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((row_bwd_kernel<T, TG, NW, VPT, false>), grid, block, 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename T, typename TG>
+hipError_t run_short_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
+    const int p = pieces(a.D);
+    if (p <= 64) return launch_bwd<T, TG, 1, 1>(a, parts, stream);
+    if (p <= 128) return launch_bwd<T, TG, 1, 2>(a, parts, stream);
+    if (p <= 256) return launch_bwd<T, TG, 4, 1>(a, parts, stream);
+    if (p <= 512) return launch_bwd<T, TG, 4, 2>(a, parts, stream);
+    if (p <= 1024) return launch_bwd<T, TG, 16, 1>(a, parts, stream);
+    return launch_bwd<T, TG, 16, 2>(a, parts, stream);
 }
 
 template <typename T>
 hipError_t run_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
-    const int p = pieces(a.D);
-    if (p <= 64) return launch_bwd<T, 1, 1>(a, parts, stream);
-    if (p <= 128) return launch_bwd<T, 1, 2>(a, parts, stream);
-    if (p <= 256) return launch_bwd<T, 1, 4>(a, parts, stream);
-    if (p <= 512) return launch_bwd<T, 4, 2>(a, parts, stream);
-    if (p <= 1024) return launch_bwd<T, 4, 4>(a, parts, stream);
-    if (p <= 2048) return launch_bwd<T, 16, 2>(a, parts, stream);
+    if (a.D >= CH && a.D <= 16384) {
+        if (a.gain_type == type_id<T>()) return run_short_bwd<T, T>(a, parts, stream);
+        if (a.gain_type == NITI_F32) return run_short_bwd<T, float>(a, parts, stream);
+    }
     hipLaunchKernelGGL((row_bwd_long_kernel<T>), dim3((unsigned)parts), dim3(NT_LONG), 0, stream, a);
     return hipGetLastError();
 }
 
 // Workgroups of the backward pass, which is also the number of partial rows.
 int64_t bwd_parts(int64_t M, int64_t D) {
-    const int64_t units = pieces(D) <= 256 ? (M + 3) / 4 : M;
+    const int64_t units = pieces(D) <= 128 ? (M + 3) / 4 : M;
     return units < kMaxParts ? units : kMaxParts;
 }
 
@@ -545,7 +601,7 @@ niti_status niti_rmsnorm_bwd(const void* dy, int64_t lddy, const void* h, int64_
         if (by_type(type, [&](auto t) { return run_bwd<decltype(t)>(a, parts, s); }) != hipSuccess) return NITI_ERR_HIP;
     }
     if (dgain) {   // no rows: zeros
-        hipLaunchKernelGGL(dgain_kernel, dim3((unsigned)((D + 63) / 64)), dim3(1024), 0, s, (const float*)ws, dgain, parts, D);
+        hipLaunchKernelGGL(dgain_kernel, dim3((unsigned)((D + 31) / 32)), dim3(1024), 0, s, (const float*)ws, dgain, parts, D);
         if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
     }
     return NITI_OK;

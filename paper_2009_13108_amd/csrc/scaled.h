@@ -74,6 +74,50 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N]) {
         if (i < n) p[i] = from_f<T>(v[i]);
 }
 
+// Eight elements as they are loaded.  A load inside a branch is waited for where the
+// branch ends, so a kernel that is to have many in flight has none of them in a
+// branch: a piece past the row's end is loaded from inside it and set to zeros,
+// a row's last, partial piece as the row's last eight elements, moved down.
+// WHOLE: the row's length is a multiple of 8, and there are no partial pieces.
+constexpr int CH = 8;
+template <typename T>
+struct Piece {
+    uint32_t w[CH * sizeof(T) / 4];
+};
+template <typename T, bool WHOLE>
+__device__ __forceinline__ Piece<T> load_piece(const T* row, int c, int D) {   // D >= 8
+    const int from = min(c, D - CH);
+    Piece<T> p;
+    __builtin_memcpy(p.w, row + from, sizeof(p.w));
+    return p;
+}
+// The piece's values once it is used: those of column c on, zeros past D.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void piece_values(Piece<T> p, int c, int D, float (&v)[CH]) {
+    constexpr int W = CH * sizeof(T) / 4, PER = 4 / sizeof(T);   // words, elements of a word
+    const bool out = c >= D;
+    if (!WHOLE) {
+        const int down = out ? 0 : c - min(c, D - CH);   // elements, 0..7
+        if (PER == 2) {
+            const bool odd = down & 1;
+#pragma unroll
+            for (int i = 0; i < W; i++) p.w[i] = odd ? p.w[i] >> 16 | (i + 1 < W ? p.w[i + 1 < W ? i + 1 : i] << 16 : 0u) : p.w[i];
+        }
+#pragma unroll
+        for (int b = 1; b < W; b *= 2) {
+            const bool move = (down / PER) & b;
+#pragma unroll
+            for (int i = 0; i < W; i++) p.w[i] = move ? (i + b < W ? p.w[i + b < W ? i + b : i] : 0u) : p.w[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < W; i++) p.w[i] = out ? 0u : p.w[i];
+    T t[CH];
+    __builtin_memcpy(t, p.w, sizeof(t));
+#pragma unroll
+    for (int i = 0; i < CH; i++) v[i] = to_f(t[i]);
+}
+
 // Elements i .. i+N-1 of a vector of a type known at run time (gains and
 // biases, which are small; uniform).
 template <int N>
@@ -87,6 +131,8 @@ __device__ __forceinline__ void load_typed(const void* p, int type, int64_t i, i
 }
 
 inline size_t type_size(int type) { return type == NITI_F32 ? 4 : 2; }
+template <typename T>
+constexpr int type_id() { return sizeof(T) == 4 ? NITI_F32 : (__is_same(T, bf16) ? NITI_BF16 : NITI_F16); }
 inline bool valid_type(int type) { return type == NITI_F32 || type == NITI_BF16 || type == NITI_F16; }
 
 // |v| as an integer of the same order; every NaN is above infinity, so that a
