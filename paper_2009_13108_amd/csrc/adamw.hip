@@ -193,21 +193,20 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Table tab) {
 }
 
 // Values of 8-bit states: p and g are the outputs for m and v here.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void adamw_read_kernel(Table tab) {
-    const int k = find_tensor(tab.start, blockIdx.x);
-    const Entry& E = tab.e[k];
-    const int64_t i = (int64_t)((int)blockIdx.x - tab.start[k]) * kChunk + threadIdx.x * PT;
-    if (i >= E.n) return;
-    const int n = (int)min((int64_t)PT, E.n - i);
+template <typename T, bool FULL>
+__device__ __forceinline__ void read_elements(const Entry& E, int64_t i) {
+    if (!FULL && i >= E.n) return;
+    const int n = FULL ? PT : (int)min((int64_t)PT, E.n - i);
     const float ms = E.ms[i / kBlock], vs = E.vs[i / kBlock];
     int8_t cm[PT] = {};
     uint8_t cv[PT] = {};
-    if (n == PT) {
+    if (FULL || n == PT) {
         __builtin_memcpy(cm, (const int8_t*)E.m + i, PT);
         __builtin_memcpy(cv, (const uint8_t*)E.v + i, PT);
     } else {
-        for (int e = 0; e < n; e++) cm[e] = ((const int8_t*)E.m)[i + e], cv[e] = ((const uint8_t*)E.v)[i + e];
+#pragma unroll
+        for (int e = 0; e < PT; e++)
+            if (e < n) cm[e] = ((const int8_t*)E.m)[i + e], cv[e] = ((const uint8_t*)E.v)[i + e];
     }
     float m[PT], v[PT];
 #pragma unroll
@@ -218,6 +217,17 @@ __global__ __launch_bounds__(kThreads) void adamw_read_kernel(Table tab) {
     }
     if (E.p) store_some((T*)E.p + i, n, m);
     if (E.g) store_some((T*)const_cast<void*>(E.g) + i, n, v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void adamw_read_kernel(Table tab) {
+    const int k = find_tensor(tab.start, blockIdx.x);
+    const Entry& E = tab.e[k];
+    const int64_t first = (int64_t)((int)blockIdx.x - tab.start[k]) * kChunk;
+    if (first + kChunk <= E.n)
+        read_elements<T, true>(E, first + threadIdx.x * PT);
+    else
+        read_elements<T, false>(E, first + threadIdx.x * PT);
 }
 
 // Fills tables with the tensors' pieces and calls launch(table, chunks) for each.

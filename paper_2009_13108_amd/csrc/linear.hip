@@ -191,11 +191,20 @@ __device__ __forceinline__ v4i row_piece(const int8_t* row, int k, int K) {
 }
 
 // 64 x 64 tiles, four waves of 32 x 32, K steps of 64 bytes through two LDS
-// stages; the next step's pieces are in registers while one is computed.  Takes
-// any strides and addresses.
-constexpr int GT = 64, GK = 64;
+// stages, a thread's pieces of four steps in registers: with those of one step a
+// step took a memory round trip (1000 x 1500 x 1111 18.8 us).  The loads are in no
+// branch, where each would be waited for: past a row's last whole piece they
+// read that one, and the last step sets right what they gave.
+constexpr int GT = 64, GK = 64, GA = 4;
 
 __device__ __forceinline__ int gswz(int row) { return ((row >> 1) ^ (row >> 2)) & 3; }
+
+// The piece at k of a row, as loaded from min(k, K - 16): zeros past K.
+__device__ __forceinline__ v4i cut_piece(v4i v, int k, int K) {
+    if (k + 16 <= K) return v;
+    if (k >= K) return v4i{0, 0, 0, 0};
+    return __builtin_bit_cast(v4i, __builtin_bit_cast(unsigned __int128, v) >> (8 * (k + 16 - K)));
+}
 
 template <typename T>
 __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n) {
@@ -210,21 +219,16 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
     const int8_t* rb = A.b + (n0 + row < A.N ? (n0 + row) * A.ldb : 0);
     const int K = (int)A.K, nk = (K + GK - 1) / GK;
     const int put = row * GK + ((pc ^ gswz(row)) << 4);
-    load_params<GT, GT, 256>(A, par, m0, n0);
     v16i acc[1][1];
     acc[0][0] = v16i{};
     const int wm = wave & 1, wn = wave >> 1;
-    v4i pa = row_piece(ra, pc * 16, K), pb = row_piece(rb, pc * 16, K);
-    for (int kt = 0; kt < nk; kt++) {
-        int8_t* st = lds[kt & 1];
+    auto step = [&](int8_t* st, v4i pa, v4i pb) {
         *(v4i*)(st + put) = pa;
         *(v4i*)(st + GT * GK + put) = pb;
         // one barrier a step: a wave writes this stage again two steps on, after the barrier in between
         __syncthreads();
-        if (kt + 1 < nk) {
-            pa = row_piece(ra, (kt + 1) * GK + pc * 16, K);
-            pb = row_piece(rb, (kt + 1) * GK + pc * 16, K);
-        }
+    };
+    auto products = [&](const int8_t* st) {
 #pragma unroll
         for (int ks = 0; ks < 2; ks++) {
             const int kp = (lane >> 5) + 2 * ks;
@@ -232,6 +236,39 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
             const v4i fa = *(const v4i*)(st + (wm * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
             const v4i fb = *(const v4i*)(st + GT * GK + (wn * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
             acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb, fa, acc[0][0], 0, 0, 0);
+        }
+    };
+    if (K >= 16) {
+        v4i pa[GA], pb[GA];
+        auto load = [&](int kt, int s) {
+            const int k = min(kt * GK + pc * 16, K - 16);
+            pa[s] = __builtin_bit_cast(v4i, load16_any(ra + k));
+            pb[s] = __builtin_bit_cast(v4i, load16_any(rb + k));
+        };
+#pragma unroll
+        for (int s = 0; s < GA; s++) load(s, s);
+        load_params<GT, GT, 256>(A, par, m0, n0);
+        for (int k0 = 0; k0 < nk; k0 += GA) {
+#pragma unroll
+            for (int s = 0; s < GA; s++) {
+                const int kt = k0 + s;
+                if (kt >= nk) break;
+                int8_t* st = lds[s & 1];
+                v4i a = pa[s], b = pb[s];
+                if (kt == nk - 1) {
+                    a = cut_piece(a, kt * GK + pc * 16, K);
+                    b = cut_piece(b, kt * GK + pc * 16, K);
+                }
+                step(st, a, b);
+                load(kt + GA, s);
+                products(st);
+            }
+        }
+    } else {
+        load_params<GT, GT, 256>(A, par, m0, n0);
+        if (K > 0) {
+            step(lds[0], row_piece(ra, pc * 16, K), row_piece(rb, pc * 16, K));
+            products(lds[0]);
         }
     }
     __syncthreads();

@@ -6,7 +6,7 @@
 // Folding b's scale into the rows (it varies along their sum) and a's into the
 // columns leaves both sums with integers only.
 //
-// Five launches.  (1) Tiles of 32 x 256 of dz leave the maxima of their rows and
+// Five launches.  (1) Tiles of 16 x 256 of dz leave the maxima of their rows and
 // the maxima and sums of their columns; (2) those are joined, in a fixed order:
 // r, c and dbias; (3) dz is formed again, in tiles of 128 x 128, for the codes of
 // rows and columns at once, the columns' transposed through LDS, and the same
@@ -22,7 +22,7 @@ namespace niti {
 
 namespace {
 
-constexpr int SR = 32, SC = 256; // tile of step 1
+constexpr int SR = 16, SC = 256; // tile of step 1
 constexpr int CT = 128;          // tile of step 3
 constexpr int CP = CT + 4;       // its LDS pitch: lanes that write one row group hit distinct banks, two by two
 constexpr int64_t kPad = 16;     // sums are padded to whole 16-byte pieces
@@ -95,7 +95,7 @@ __device__ __forceinline__ void load_sb(const DzArgs& a, int64_t c, int n, float
     for (int e = 0; e < CH; e++) v[e] = e < n ? a.s_b[a.b_step ? c + e : 0] : 0.f;
 }
 
-// Step 1.  A thread takes 8 columns of 4 rows; 32 lanes a row, 8 threads a column group.
+// Step 1.  A thread takes 8 columns of 2 rows; 32 lanes a row, 8 threads a column group.
 template <typename T, int KIND>
 __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     __shared__ float ssum[8][SC + 8];

@@ -183,31 +183,54 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
     return v;
 }
 
-// exp(x) for |x| <= 80, within three units in the last place: x log2(e) in two parts, the
-// second as a first-order factor.  The library's expf, which also takes the ends
-// of the range, costs about twice that, and an IEEE division ten instructions:
-// the slopes bounded the passes over a gradient with both.
-__device__ __forceinline__ float exp_mid(float x) {
-    const float t = x * 1.44269502e+00f;                       // log2(e) rounded to 32 bits
-    const float r = __builtin_fmaf(x, 1.92596303e-08f, __builtin_fmaf(x, 1.44269502e+00f, -t));
-    const float e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, r * 6.93147182e-01f, e);
-}
+// exp(x) for |x| <= 80 by the hardware's power of two.  The rounding of x log2(e)
+// leaves a relative error of |x| 2^-24: in a sigmoid that is at most s (1 - s) |x| 2^-24 <
+// 0.23 * 2^-24, and a normal density's is as small.  The library's expf and an IEEE
+// division cost ten instructions each; with them the slopes alone bounded the
+// passes over a gradient.
+__device__ __forceinline__ float exp_mid(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float sigmoid_mid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_mid(-x)); }
 
-// Activations and their derivatives.  Below -80 a sigmoid is under 2^-115 and
-// its argument is held there, so that an infinity gives the limit and no NaN.
+// The normal distribution function at z from e = exp(-z^2 / 2): Abramowitz and
+// Stegun, Handbook of Mathematical Functions (1964), 7.1.26, erf(x) = 1 - (a1 t +
+// ... + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), within 1.5e-7 for x >= 0.
+__device__ __forceinline__ float normal_cdf(float z, float e) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.f));
+    float p = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+    p = __builtin_fmaf(t, p, 1.421413741f);
+    p = __builtin_fmaf(t, p, -0.284496736f);
+    p = __builtin_fmaf(t, p, 0.254829592f);
+    const float q = 0.5f * t * p * e;   // the tail beyond |z|
+    return z < 0.f ? q : 1.f - q;
+}
+
+// Activations and their derivatives.  Arguments are held where a sigmoid or a
+// tail is below 2^-115, so that an infinity gives the limit and no NaN.
 __device__ __forceinline__ float act_value(int act, float z) {
     if (act == NITI_ACT_RELU) return z < 0.f ? 0.f : z;
     if (act == NITI_ACT_GELU) {
-        const float c = z < -40.f ? -40.f : z;
-        return 0.5f * c * (1.f + erff(c * 0.70710678118654752f));
+        const float c = z < -12.5f ? -12.5f : z, d = c > 12.5f ? 12.5f : c;
+        return c * normal_cdf(d, exp_mid(-0.5f * d * d));
     }
     if (act == NITI_ACT_SILU) {
         const float c = z < -80.f ? -80.f : z;
         return c * sigmoid_mid(c > 80.f ? 80.f : c);
     }
     return z;
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+    if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+    if (act == NITI_ACT_GELU) {
+        const float c = z < -12.5f ? -12.5f : (z > 12.5f ? 12.5f : z);
+        const float e = exp_mid(-0.5f * c * c);
+        return normal_cdf(c, e) + c * e * 0.39894228040143268f;
+    }
+    if (act == NITI_ACT_SILU) {
+        const float c = z < -80.f ? -80.f : (z > 80.f ? 80.f : z);
+        const float s = sigmoid_mid(c);
+        return s * (1.f + c * (1.f - s));
+    }
+    return 1.f;
 }
 // The same of several values: the choice is made once.
 template <int N>
@@ -223,20 +246,6 @@ __device__ __forceinline__ void act_values(int act, float (&v)[N]) {
         for (int e = 0; e < N; e++) v[e] = act_value(NITI_ACT_SILU, v[e]);
     }
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
-    if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    if (act == NITI_ACT_GELU) {
-        const float c = z < -40.f ? -40.f : (z > 40.f ? 40.f : z);
-        return 0.5f * (1.f + erff(c * 0.70710678118654752f)) + c * exp_mid(fmaxf(-0.5f * c * c, -80.f)) * 0.39894228040143268f;
-    }
-    if (act == NITI_ACT_SILU) {
-        const float c = z < -80.f ? -80.f : (z > 80.f ? 80.f : z);
-        const float s = sigmoid_mid(c);
-        return s * (1.f + c * (1.f - s));
-    }
-    return 1.f;
-}
-
 constexpr int64_t kMaxLd = (int64_t)1 << 22;   // row strides are below this
 constexpr int64_t kMaxDim = (int64_t)1 << 31;
 constexpr int64_t kMaxSum = (int64_t)1 << 17;   // shorter sums of int8 products stay in int32
