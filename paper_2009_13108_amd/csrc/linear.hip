@@ -9,6 +9,7 @@
 
 #include <math.h>
 
+#include <type_traits>
 #include <utility>
 
 namespace niti {
@@ -190,14 +191,15 @@ __device__ __forceinline__ v4i row_piece(const int8_t* row, int k, int K) {
     return __builtin_bit_cast(v4i, x);
 }
 
-// 64 x 64 tiles, four waves of 32 x 32, K steps of 64 bytes through two LDS
-// stages, a thread's pieces of four steps in registers: with those of one step a
-// step took a memory round trip (1000 x 1500 x 1111 18.8 us).  The loads are in no
-// branch, where each would be waited for: past a row's last whole piece they
-// read that one, and the last step sets right what they gave.
-constexpr int GT = 64, GK = 64, GA = 4;
+// 64 x 64 tiles, four waves of 32 x 32, K steps of 128 bytes through two LDS
+// stages, a thread's pieces of three steps in registers: with those of one step
+// a step took a memory round trip, with steps of 64 bytes twice the barriers
+// (1000 x 1500 x 1111 18.8 and 16.9 us).  The loads are in no branch, where
+// each would be waited for: past a row's last whole piece they read that one, and
+// the last step sets right what they gave.
+constexpr int GT = 64, GK = 128, GA = 3;
 
-__device__ __forceinline__ int gswz(int row) { return ((row >> 1) ^ (row >> 2)) & 3; }
+__device__ __forceinline__ int gswz(int row) { return (row >> 1) & 7; }
 
 // The piece at k of a row, as loaded from min(k, K - 16): zeros past K.
 __device__ __forceinline__ v4i cut_piece(v4i v, int k, int K) {
@@ -213,61 +215,77 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * GT, n0 = (int64_t)(blockIdx.x % tiles_n) * GT;
-    // one piece of each operand a thread: rows past the edge read row 0, whose products are not stored
+    // two pieces of each operand a thread, 64 bytes apart: rows past the edge read row 0, whose products are not stored
     const int row = threadIdx.x >> 2, pc = threadIdx.x & 3;
     const int8_t* ra = A.a + (m0 + row < A.M ? (m0 + row) * A.lda : 0);
     const int8_t* rb = A.b + (n0 + row < A.N ? (n0 + row) * A.ldb : 0);
     const int K = (int)A.K, nk = (K + GK - 1) / GK;
-    const int put = row * GK + ((pc ^ gswz(row)) << 4);
     v16i acc[1][1];
     acc[0][0] = v16i{};
     const int wm = wave & 1, wn = wave >> 1;
-    auto step = [&](int8_t* st, v4i pa, v4i pb) {
-        *(v4i*)(st + put) = pa;
-        *(v4i*)(st + GT * GK + put) = pb;
-        // one barrier a step: a wave writes this stage again two steps on, after the barrier in between
-        __syncthreads();
+    auto put = [&](int8_t* st, int h, v4i a, v4i b) {
+        const int at = row * GK + (((pc + 4 * h) ^ gswz(row)) << 4);
+        *(v4i*)(st + at) = a;
+        *(v4i*)(st + GT * GK + at) = b;
     };
     auto products = [&](const int8_t* st) {
+        v4i fa[4], fb[4];
 #pragma unroll
-        for (int ks = 0; ks < 2; ks++) {
-            const int kp = (lane >> 5) + 2 * ks;
-            const int r = lane & 31;
-            const v4i fa = *(const v4i*)(st + (wm * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
-            const v4i fb = *(const v4i*)(st + GT * GK + (wn * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
-            acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb, fa, acc[0][0], 0, 0, 0);
+        for (int ks = 0; ks < 4; ks++) {
+            const int kp = (lane >> 5) + 2 * ks, r = lane & 31;
+            fa[ks] = *(const v4i*)(st + (wm * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
+            fb[ks] = *(const v4i*)(st + GT * GK + (wn * 32 + r) * GK + ((kp ^ gswz(r)) << 4));
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ks++) acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[ks], fa[ks], acc[0][0], 0, 0, 0);
     };
     if (K >= 16) {
-        v4i pa[GA], pb[GA];
+        v4i pa[GA][2], pb[GA][2];
         auto load = [&](int kt, int s) {
-            const int k = min(kt * GK + pc * 16, K - 16);
-            pa[s] = __builtin_bit_cast(v4i, load16_any(ra + k));
-            pb[s] = __builtin_bit_cast(v4i, load16_any(rb + k));
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int k = min(kt * GK + h * 64 + pc * 16, K - 16);
+                pa[s][h] = __builtin_bit_cast(v4i, load16_any(ra + k));
+                pb[s][h] = __builtin_bit_cast(v4i, load16_any(rb + k));
+            }
         };
 #pragma unroll
         for (int s = 0; s < GA; s++) load(s, s);
         load_params<GT, GT, 256>(A, par, m0, n0);
-        for (int k0 = 0; k0 < nk; k0 += GA) {
+        // a step's barrier is its only one: a wave writes this stage again two steps on, after the barrier in between
+        int k0 = 0, stage = 0;
+        for (; k0 + GA < nk; k0 += GA) {
 #pragma unroll
             for (int s = 0; s < GA; s++) {
-                const int kt = k0 + s;
-                if (kt >= nk) break;
-                int8_t* st = lds[s & 1];
-                v4i a = pa[s], b = pb[s];
-                if (kt == nk - 1) {
-                    a = cut_piece(a, kt * GK + pc * 16, K);
-                    b = cut_piece(b, kt * GK + pc * 16, K);
-                }
-                step(st, a, b);
-                load(kt + GA, s);
+                int8_t* st = lds[0] + stage;
+#pragma unroll
+                for (int h = 0; h < 2; h++) put(st, h, pa[s][h], pb[s][h]);
+                __syncthreads();
+                load(k0 + s + GA, s);
                 products(st);
+                stage ^= 2 * GT * GK;
             }
+        }
+#pragma unroll
+        for (int s = 0; s < GA; s++) {   // what is left, the last step among it
+            if (k0 + s >= nk) break;
+            int8_t* st = lds[0] + stage;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int k = (k0 + s) * GK + h * 64 + pc * 16;
+                put(st, h, cut_piece(pa[s][h], k, K), cut_piece(pb[s][h], k, K));
+            }
+            __syncthreads();
+            products(st);
+            stage ^= 2 * GT * GK;
         }
     } else {
         load_params<GT, GT, 256>(A, par, m0, n0);
         if (K > 0) {
-            step(lds[0], row_piece(ra, pc * 16, K), row_piece(rb, pc * 16, K));
+#pragma unroll
+            for (int h = 0; h < 2; h++) put(lds[0], h, row_piece(ra, h * 64 + pc * 16, K), row_piece(rb, h * 64 + pc * 16, K));
+            __syncthreads();
             products(lds[0]);
         }
     }
@@ -330,32 +348,48 @@ __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int ti
 #pragma unroll
             for (int b = 0; b < FM; b++) acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[a], x[b], acc[a][b], 0, 0, 0);
     };
-    const int whole = K >> 7;   // steps without a check
-    int s = wave;
-    for (; s + (KB - 1) * SW < whole; s += KB * SW) {
-        v4i w[2 * KB][FN], x[2 * KB][FM];
+    // NS steps of this wave from step s on, their loads all in flight and none of them in a branch: past a
+    // row's last whole piece they read that one, and the sum's last step sets right what they gave.
+    const int last = (K - 1) >> 7;
+    auto steps = [&](int s, auto count) {
+        constexpr int NS = decltype(count)::value;
+        v4i w[2 * NS][FN], x[2 * NS][FM];
 #pragma unroll
-        for (int j = 0; j < 2 * KB; j++) {
-            const int k = (s + (j >> 1) * SW) * 128 + (j & 1) * 64 + kq;
+        for (int j = 0; j < 2 * NS; j++) {
+            const int k = min((s + (j >> 1) * SW) * 128 + (j & 1) * 64 + kq, K - 16);
 #pragma unroll
             for (int i = 0; i < FN; i++) w[j][i] = __builtin_bit_cast(v4i, load16_any(rb[i] + k));
 #pragma unroll
             for (int i = 0; i < FM; i++) x[j][i] = __builtin_bit_cast(v4i, load16_any(ra[i] + k));
         }
 #pragma unroll
-        for (int j = 0; j < 2 * KB; j++) mma(w[j], x[j]);
-    }
-    for (; s * 128 < K; s += SW)
+        for (int j = 0; j < 2 * NS; j++) {
+            const int at = s + (j >> 1) * SW, k = at * 128 + (j & 1) * 64 + kq;
+            if (at == last) {
 #pragma unroll
-        for (int j = 0; j < 2; j++) {
-            const int k = s * 128 + j * 64 + kq;
-            v4i w[FN], x[FM];
+                for (int i = 0; i < FN; i++) w[j][i] = cut_piece(w[j][i], k, K);
 #pragma unroll
-            for (int i = 0; i < FN; i++) w[i] = row_piece(rb[i], k, K);
-#pragma unroll
-            for (int i = 0; i < FM; i++) x[i] = row_piece(ra[i], k, K);
-            mma(w, x);
+                for (int i = 0; i < FM; i++) x[j][i] = cut_piece(x[j][i], k, K);
+            }
+            mma(w[j], x[j]);
         }
+    };
+    if (K >= 16) {
+        int s = wave;
+        for (; s + (KB - 1) * SW <= last; s += KB * SW) steps(s, std::integral_constant<int, KB>());
+        if (KB > 2 && s + SW <= last) {
+            steps(s, std::integral_constant<int, 2>());
+            s += 2 * SW;
+        }
+        if (KB > 1 && s <= last) steps(s, std::integral_constant<int, 1>());
+    } else if (wave == 0 && K > 0) {
+        v4i w[FN], x[FM];
+#pragma unroll
+        for (int i = 0; i < FN; i++) w[i] = row_piece(rb[i], kq, K);
+#pragma unroll
+        for (int i = 0; i < FM; i++) x[i] = row_piece(ra[i], kq, K);
+        mma(w, x);
+    }
     // element i of acc[a][b]: channel 16 a + 4 (lane / 16) + i of row 16 b + lane % 16
 #pragma unroll
     for (int a = 0; a < FN; a++)
@@ -580,6 +614,7 @@ constexpr Cost kSmall11{16, 16, 2.12f, 0.39f, 0.63f, 0.88f};
 constexpr Cost kSmall12{16, 32, 2.13f, 0.50f, 0.96f, 1.11f};
 constexpr Cost kSmall22{32, 32, 2.03f, 0.88f, 1.13f, 1.49f};
 constexpr Cost kRing64{64, 64, 2.00f, 1.47f, 2.01f, 2.17f};
+constexpr Cost kAny64{64, 64, 2.6f, 1.9f, 2.6f, 2.8f};
 constexpr Cost kRing128{128, 128, 0.41f, 3.40f, 6.84f, 4.92f};
 constexpr Cost kRing256{256, 256, 0.f, 10.3f, 10.4f, 5.22f};
 
@@ -603,7 +638,7 @@ hipError_t run_linear(LinArgs A, void*, size_t, hipStream_t stream) {
             if (ring == r128) return run_ring<T, 128, 128, 2, 4, 2, 128>(A, stream);
             return run_ring<T, 64, 64, 4, 2, 2, 128>(A, stream);
         }
-    } else if (cost(kRing64, A) < small) {
+    } else if (cost(kAny64, A) < small) {
         return run_any<T>(A, stream);
     }
     if (small == s11) return run_small<T, 1, 1>(A, stream);

@@ -89,10 +89,18 @@ struct DzRows {
     }
 };
 
-// b's scales of n columns from c on.
-__device__ __forceinline__ void load_sb(const DzArgs& a, int64_t c, int n, float (&v)[CH]) {
+// A vector's values of 8 columns from c on (stride 0: one value for all); zeros past the edge.
+template <int KIND>
+__device__ __forceinline__ void load_cols(const float* p, int step, int c, int N, float (&v)[CH]) {
+    if (!step) {
+        const float one = p[0];
 #pragma unroll
-    for (int e = 0; e < CH; e++) v[e] = e < n ? a.s_b[a.b_step ? c + e : 0] : 0.f;
+        for (int e = 0; e < CH; e++) v[e] = c + e < N ? one : 0.f;
+    } else if constexpr (KIND > 0) {
+        piece_values<float, KIND == 2>(load_piece<float, KIND == 2>(p, c, N), c, N, v);
+    } else {
+        load_some(p + c, N - c, v);
+    }
 }
 
 // Step 1.  A thread takes 8 columns of 2 rows; 32 lanes a row, 8 threads a column group.
@@ -103,25 +111,25 @@ __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     const int64_t tm = blockIdx.x / a.tiles_n, tn = blockIdx.x % a.tiles_n;
     const int col = (threadIdx.x & 31) * CH, grp = threadIdx.x >> 5;
     const int c = (int)(tn * SC + col);
-    const int n = max(0, min(CH, (int)a.N - c));
     DzRows<T, KIND, SR / 8> rows;
     rows.load(a, tm * SR + grp, 8, c);
-    float sb[CH], sum[CH];
+    float sb[CH], sum[CH], sa[SR / 8];
     uint32_t mx[CH];
-    load_sb(a, c, n, sb);
+#pragma unroll
+    for (int i = 0; i < SR / 8; i++) sa[i] = a.s_a[a.a_step ? min(tm * SR + i * 8 + grp, a.M - 1) : 0];
+    load_cols<KIND>(a.s_b, a.b_step, c, (int)a.N, sb);
 #pragma unroll
     for (int e = 0; e < CH; e++) sum[e] = 0.f, mx[e] = 0;
 #pragma unroll
     for (int i = 0; i < SR / 8; i++) {
         const int64_t m = tm * SR + i * 8 + grp;
-        const float sa = a.s_a[a.a_step ? min(m, a.M - 1) : 0];
         float d[CH];
         rows.get(a, i, m, c, d);
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < CH; e++) {
             sum[e] += d[e];
-            mx[e] = max(mx[e], mag_bits(d[e] * sa));
+            mx[e] = max(mx[e], mag_bits(d[e] * sa[i]));
             top = max(top, mag_bits(d[e] * sb[e]));   // (zeros past the edges)
         }
 #pragma unroll
@@ -152,6 +160,7 @@ __global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks)
         const int64_t m = (int64_t)((int)blockIdx.x - col_blocks) * 1024 + threadIdx.x;
         if (m >= a.M) return;
         uint32_t mx = 0;
+#pragma unroll 8
         for (int64_t t = 0; t < a.tiles_n; t++) mx = max(mx, a.rmax[t * a.M + m]);
         const RowScale rs = row_scale(mx);
         a.r[m] = rs.scale;
@@ -163,9 +172,20 @@ __global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks)
     float s = 0.f;
     uint32_t mx = 0;
     if (c < a.N)
-        for (int64_t i = grp; i < a.tiles_m; i += 16) {
-            s += a.csum[i * a.N + c];
-            mx = max(mx, a.cmax[i * a.N + c]);
+        for (int64_t i = grp; i < a.tiles_m; i += 128) {   // eight tiles' values in flight
+            float x[8];
+            uint32_t y[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const int64_t t = min(i + 16 * j, a.tiles_m - 1);
+                x[j] = a.csum[t * a.N + c];
+                y[j] = a.cmax[t * a.N + c];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                s += i + 16 * j < a.tiles_m ? x[j] : 0.f;
+                mx = max(mx, y[j]);
+            }
         }
     ssum[grp][col] = s;
     smax[grp][col] = mx;
@@ -217,16 +237,25 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
     const int64_t r0 = (int64_t)(block / a.tiles_k) * CT, k0 = (int64_t)(block % a.tiles_k) * CT;
     const int pc = (threadIdx.x & 7) * 16, row = (threadIdx.x >> 3) * 4;   // four rows of 16 bytes a thread
     uint4 v[4];
+    const int64_t k = k0 + pc;
+    if (a.K >= 16) {
+        // (no load in a branch: past the edges the last row's or a row's last piece, set right afterwards)
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int64_t r = r0 + row + i;
-        const int n = r < a.R ? (int)max((int64_t)0, min((int64_t)16, a.K - (k0 + pc))) : 0;
-        v[i] = make_uint4(0, 0, 0, 0);
-        if (n == 16) {
-            v[i] = load16_any(a.x + r * a.ldx + k0 + pc);
-        } else if (n > 0) {
+        for (int i = 0; i < 4; i++) v[i] = load16_any(a.x + min(r0 + row + i, a.R - 1) * a.ldx + min(k, a.K - 16));
+        if (k0 + CT > a.K || r0 + CT > a.R) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int down = r0 + row + i < a.R ? (int)min((int64_t)16, max((int64_t)0, k + 16 - a.K)) : 16;
+                const unsigned __int128 x = __builtin_bit_cast(unsigned __int128, v[i]);
+                v[i] = __builtin_bit_cast(uint4, down < 16 ? x >> (8 * down) : (unsigned __int128)0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
             uint32_t w[4] = {0, 0, 0, 0};
-            for (int e = 0; e < n; e++) w[e >> 2] |= (uint32_t)(uint8_t)a.x[r * a.ldx + k0 + pc + e] << (8 * (e & 3));
+            if (r0 + row + i < a.R)
+                for (int e = 0; e < a.K - k; e++) w[e >> 2] |= (uint32_t)(uint8_t)a.x[(r0 + row + i) * a.ldx + k + e] << (8 * (e & 3));
             v[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
@@ -261,11 +290,9 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
     const int64_t m0 = (int64_t)(block / tiles_c) * CT, n0 = (int64_t)(block % tiles_c) * CT;
     const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 8;   // 8 columns of 8 rows a thread
     const int c = (int)(n0 + col);
-    const int n = max(0, min(CH, (int)a.N - c));
     float sb[CH], ci[CH];
-    load_sb(a, c, n, sb);
-#pragma unroll
-    for (int e = 0; e < CH; e++) ci[e] = a.q && e < n ? a.c[a.N + c + e] : 0.f;
+    load_cols<KIND>(a.s_b, a.b_step, c, (int)a.N, sb);
+    load_cols<KIND>(a.c + a.N, 1, c, (int)a.N, ci);
     uint32_t cmask[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < CH; e++) cmask[e >> 2] |= (code_mask(ci[e]) & 0xFFu) << (8 * (e & 3));
@@ -274,25 +301,30 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
         uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
         DzRows<T, KIND, 4> rows;
         rows.load(a, m0 + row0 + 4 * h, 1, c);
+        float ri[4], sa[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int64_t m = min(m0 + row0 + 4 * h + i, a.M - 1);
+            ri[i] = a.r[a.M + m];
+            sa[i] = a.s_a[a.a_step ? m : 0];
+        }
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int64_t m = m0 + row0 + 4 * h + i;
             const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
             float d[CH], pc[CH], cc[CH];
             rows.get(a, i, m, c, d);
-            const int64_t mi = min(m, a.M - 1);
-            const float ri = a.p ? a.r[a.M + mi] : 0.f, sa = a.s_a[a.a_step ? mi : 0];
             uint64_t r[CH];
 #pragma unroll
             for (int e = 0; e < CH; e++) r[e] = a.sr ? sr_draw(a.seed, a.call, (uint64_t)(m * a.N + c + e)) : 0;
 #pragma unroll
             for (int e = 0; e < CH; e++) {
                 // (past the edges dz is 0, and so are the codes: a draw is below 1)
-                pc[e] = a.sr ? code_sr(d[e] * sb[e], ri, draw_hi(r[e])) : code_rtn(d[e] * sb[e], ri);
-                cc[e] = a.sr ? code_sr(d[e] * sa, ci[e], draw_lo(r[e])) : code_rtn(d[e] * sa, ci[e]);
+                pc[e] = a.sr ? code_sr(d[e] * sb[e], ri[i], draw_hi(r[e])) : code_rtn(d[e] * sb[e], ri[i]);
+                cc[e] = a.sr ? code_sr(d[e] * sa[i], ci[e], draw_lo(r[e])) : code_rtn(d[e] * sa[i], ci[e]);
             }
             if (a.p && in && c < a.Np) {
-                const uint32_t mask = code_mask(ri);
+                const uint32_t mask = code_mask(ri[i]);
                 const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
                 __builtin_memcpy(a.p + m * a.Np + c, w, CH);
             }
