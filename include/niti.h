@@ -403,8 +403,9 @@ niti_status niti_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ld
  * activation, for the backward pass) are optional; res and z have out's type,
  * and out may be res.  K in 0..131071 (longer sums could leave 32 bits:
  * NITI_ERR_UNSUPPORTED).  Workspace: niti_workspace_bytes(NITI_OP_LINEAR_FWD,
- * NULL, M, N, K); it may be NULL with 0 bytes, and such a call takes longer
- * where the products are few and the sum is long. */
+ * NULL, M, N, K), 0 for most sizes; without it (NULL and 0 bytes, or fewer than
+ * that) the call takes longer where the products are few and the sum is long:
+ * parts of the sum are then not formed side by side. */
 niti_status niti_linear_fwd(const int8_t *a, int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b,
                             int64_t ldb, const float *s_b, int64_t s_b_n, const void *bias, int bias_type, int act,
                             const void *res, int64_t ldres, void *z, int64_t ldz, void *out, int64_t ldout, int64_t M,

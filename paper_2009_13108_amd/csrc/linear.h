@@ -19,7 +19,10 @@ struct LinArgs {
     int64_t M, N, K;
     int32_t a_step, b_step;   // 1, or 0 for one scale
     int32_t bias_type, act;
-    int32_t res_dma;          // set by linear_run
+    // Set by linear_run:
+    int32_t res_dma;          // the residual's rows are whole aligned pieces within 32-bit offsets
+    int32_t klen;             // products of one part of a split sum (blockIdx.y), or 0
+    int64_t part;             // elements of a part's sums, from out on
 };
 
 hipError_t linear_run(const LinArgs& a, int type, void* ws, size_t ws_bytes, hipStream_t stream);

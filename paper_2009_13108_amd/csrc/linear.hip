@@ -68,7 +68,19 @@ __device__ __forceinline__ void load_params(const LinArgs& A, float* par, int64_
         par[2 * BN + r] = m0 + r < A.M ? (A.s_a ? A.s_a[A.a_step ? m0 + r : 0] : 1.f) : 0.f;
 }
 
-// res_dma: the residual's rows are whole aligned pieces within 32-bit offsets.
+// A workgroup's part of a split sum: its stretch of K, and its place in the sums (int32_t).
+template <typename T>
+__device__ __forceinline__ void take_part(LinArgs& A) {
+    if constexpr (__is_same(T, int32_t)) {
+        const int64_t k0 = (int64_t)blockIdx.y * A.klen;
+        A.a += k0;
+        A.b += k0;
+        A.K = min((int64_t)A.klen, A.K - k0);
+        A.out = (int32_t*)A.out + blockIdx.y * A.part;
+    }
+}
+
+// T: the result's type, or int32_t for a part of a split sum, which is stored as it is.
 template <typename T, int BM, int BN, int WGM, int WGN, int ROOM>
 __device__ __forceinline__ void epilogue(const LinArgs& A, v16i (&acc)[BN / WGN / 32][BM / WGM / 32], int8_t* lds, const float* par,
                                          int64_t m0, int64_t n0) {
@@ -118,36 +130,41 @@ __device__ __forceinline__ void epilogue(const LinArgs& A, v16i (&acc)[BN / WGN 
                 v16i x = acc[0][0];
                 pick(acc, ta * FM + b0 + tb, x, std::make_integer_sequence<int, FN * FM>());
                 const int row = tb * 32 + (lane & 31);                    // of the wave's turned rows
-                const float sa = par[2 * BN + wm * S::WTM + b0 * 32 + row];
                 const int r = wm * 32 * BG + row;
                 const int c0 = wn * S::WTN + ta * 32 + 4 * (lane >> 5);   // this lane's columns: c0 + 8 j + e
-                v4f sb[4], bias[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    sb[j] = *(const v4f*)(par + c0 + 8 * j);
-                    bias[j] = *(const v4f*)(par + BN + c0 + 8 * j);
-                }
-                float v[16];
-#pragma unroll
-                for (int e = 0; e < 16; e++) v[e] = (float)x[e] * sb[e >> 2][e & 3] * sa + bias[e >> 2][e & 3];
-                if (kind == 1 && A.act != NITI_ACT_NONE) act_values(A.act, v);
                 T* at[4];
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     const int c = c0 + 8 * j;
                     at[j] = (T*)(lds + S::at(r, c / S::EPP) * 16) + c % S::EPP;
                 }
-                if (add) {
-                    float res[4][4];
+                if constexpr (__is_same(T, int32_t)) {
 #pragma unroll
-                    for (int j = 0; j < 4; j++) load_n(at[j], res[j]);
+                    for (int j = 0; j < 4; j++) *(v4i*)at[j] = v4i{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+                } else {
+                    const float sa = par[2 * BN + wm * S::WTM + b0 * 32 + row];
+                    v4f sb[4], bias[4];
 #pragma unroll
-                    for (int e = 0; e < 16; e++) v[e] += res[e >> 2][e & 3];
-                }
+                    for (int j = 0; j < 4; j++) {
+                        sb[j] = *(const v4f*)(par + c0 + 8 * j);
+                        bias[j] = *(const v4f*)(par + BN + c0 + 8 * j);
+                    }
+                    float v[16];
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const float w[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-                    store_n(at[j], w);
+                    for (int e = 0; e < 16; e++) v[e] = (float)x[e] * sb[e >> 2][e & 3] * sa + bias[e >> 2][e & 3];
+                    if (kind == 1 && A.act != NITI_ACT_NONE) act_values(A.act, v);
+                    if (add) {
+                        float res[4][4];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) load_n(at[j], res[j]);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) v[e] += res[e >> 2][e & 3];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float w[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+                        store_n(at[j], w);
+                    }
                 }
             }
             __syncthreads();
@@ -210,6 +227,7 @@ __device__ __forceinline__ v4i cut_piece(v4i v, int k, int K) {
 
 template <typename T>
 __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n) {
+    take_part<T>(A);
     __shared__ __attribute__((aligned(16))) int8_t lds[2][2 * GT * GK];
     __shared__ __attribute__((aligned(16))) float par[3 * GT];
     const int lane = threadIdx.x & 63;
@@ -296,7 +314,8 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
 template <typename T>
 hipError_t run_any(const LinArgs& A, hipStream_t stream) {
     const int64_t tm = (A.M + GT - 1) / GT, tn = (A.N + GT - 1) / GT;
-    hipLaunchKernelGGL((linear_any_kernel<T>), dim3((unsigned)(tm * tn)), dim3(256), 0, stream, A, (int)tn);
+    const dim3 grid((unsigned)(tm * tn), A.klen ? (unsigned)((A.K + A.klen - 1) / A.klen) : 1);
+    hipLaunchKernelGGL((linear_any_kernel<T>), grid, dim3(256), 0, stream, A, (int)tn);
     return hipGetLastError();
 }
 
@@ -307,9 +326,41 @@ hipError_t run_any(const LinArgs& A, hipStream_t stream) {
 // bytes of each row (two 16 x 16 x 64 MFMAs): whole cache lines.  Any strides and
 // addresses.  One token by 4096 x 4096 is 256 such tiles: every CU streams 64 KB
 // of weights.
+// 16 bytes as they are loaded.  BYTES: from an address that is no multiple of 4.
+// The hardware takes such loads apart where the lanes beside one read other rows
+// (one token by 4096 x 4097 took 10.9 us, by 4096 x 4100 6.4; the kernel above,
+// whose lanes read a row four by four, loses by the shifts), so the aligned words that hold the bytes are loaded, five
+// where the address is not aligned, and shifted when they are used.  Every word
+// read holds a byte of the piece.
+template <bool BYTES>
+struct Raw16 {
+    v4i v;
+    uint32_t next;
+    uint32_t shift;
+    __device__ __forceinline__ void load(const int8_t* p) {
+        if (BYTES) {
+            shift = (uint32_t)(uintptr_t)p & 3u;
+            const int8_t* q = p - shift;
+            __builtin_memcpy(&v, __builtin_assume_aligned(q, 4), 16);
+            __builtin_memcpy(&next, __builtin_assume_aligned(q + (shift ? 16 : 12), 4), 4);
+        } else {
+            __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
+        }
+    }
+    __device__ __forceinline__ v4i get() const {
+        if (!BYTES) return v;
+        return v4i{(int)__builtin_amdgcn_alignbyte((uint32_t)v[1], (uint32_t)v[0], shift),
+                   (int)__builtin_amdgcn_alignbyte((uint32_t)v[2], (uint32_t)v[1], shift),
+                   (int)__builtin_amdgcn_alignbyte((uint32_t)v[3], (uint32_t)v[2], shift),
+                   (int)__builtin_amdgcn_alignbyte(next, (uint32_t)v[3], shift)};
+    }
+};
+// Whether rows begin at multiples of 4.
+inline bool word_rows(const LinArgs& A) { return A.lda % 4 == 0 && A.ldb % 4 == 0 && (((uintptr_t)A.a | (uintptr_t)A.b) & 3) == 0 && A.K % 4 == 0; }
+
 constexpr int SW = 8;
 
-template <typename T, int FM, int FN>
+template <typename T, int FM, int FN, bool BYTES>
 __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int tiles_n) {
     constexpr int TM = 16 * FM, TN = 16 * FN, PITCH = TN + 4;
     constexpr int KB = FM + FN <= 2 ? 4 : (FM + FN <= 3 ? 2 : 1);   // steps in flight of a wave
@@ -353,25 +404,30 @@ __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int ti
     const int last = (K - 1) >> 7;
     auto steps = [&](int s, auto count) {
         constexpr int NS = decltype(count)::value;
-        v4i w[2 * NS][FN], x[2 * NS][FM];
+        Raw16<BYTES> rw[2 * NS][FN], rx[2 * NS][FM];
 #pragma unroll
         for (int j = 0; j < 2 * NS; j++) {
             const int k = min((s + (j >> 1) * SW) * 128 + (j & 1) * 64 + kq, K - 16);
 #pragma unroll
-            for (int i = 0; i < FN; i++) w[j][i] = __builtin_bit_cast(v4i, load16_any(rb[i] + k));
+            for (int i = 0; i < FN; i++) rw[j][i].load(rb[i] + k);
 #pragma unroll
-            for (int i = 0; i < FM; i++) x[j][i] = __builtin_bit_cast(v4i, load16_any(ra[i] + k));
+            for (int i = 0; i < FM; i++) rx[j][i].load(ra[i] + k);
         }
 #pragma unroll
         for (int j = 0; j < 2 * NS; j++) {
             const int at = s + (j >> 1) * SW, k = at * 128 + (j & 1) * 64 + kq;
+            v4i w[FN], x[FM];
+#pragma unroll
+            for (int i = 0; i < FN; i++) w[i] = rw[j][i].get();
+#pragma unroll
+            for (int i = 0; i < FM; i++) x[i] = rx[j][i].get();
             if (at == last) {
 #pragma unroll
-                for (int i = 0; i < FN; i++) w[j][i] = cut_piece(w[j][i], k, K);
+                for (int i = 0; i < FN; i++) w[i] = cut_piece(w[i], k, K);
 #pragma unroll
-                for (int i = 0; i < FM; i++) x[j][i] = cut_piece(x[j][i], k, K);
+                for (int i = 0; i < FM; i++) x[i] = cut_piece(x[i], k, K);
             }
-            mma(w[j], x[j]);
+            mma(w, x);
         }
     };
     if (K >= 16) {
@@ -414,7 +470,10 @@ __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int ti
 template <typename T, int FM, int FN>
 hipError_t run_small(const LinArgs& A, hipStream_t stream) {
     const int64_t tm = (A.M + 16 * FM - 1) / (16 * FM), tn = (A.N + 16 * FN - 1) / (16 * FN);
-    hipLaunchKernelGGL((linear_small_kernel<T, FM, FN>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
+    if (word_rows(A))
+        hipLaunchKernelGGL((linear_small_kernel<T, FM, FN, false>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
+    else
+        hipLaunchKernelGGL((linear_small_kernel<T, FM, FN, true>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
     return hipGetLastError();
 }
 
@@ -450,6 +509,7 @@ struct Ring {
 template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
 __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_kernel(LinArgs A, int tiles_n) {
     using R = Ring<BM, BN, NS, WGM, WGN, KS>;
+    take_part<T>(A);
     extern __shared__ __attribute__((aligned(1024))) int8_t ring[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -591,7 +651,8 @@ hipError_t run_ring(const LinArgs& A, hipStream_t stream) {
         attr_done = true;
     }
     const int64_t tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(R::NT), R::LDS, stream, A, (int)tn);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn), A.klen ? (unsigned)((A.K + A.klen - 1) / A.klen) : 1), dim3(R::NT), R::LDS,
+                       stream, A, (int)tn);
     return hipGetLastError();
 }
 
@@ -599,6 +660,56 @@ bool ring_takes(const LinArgs& A) {
     return A.K > 0 && A.K % 16 == 0 && A.lda % 16 == 0 && A.ldb % 16 == 0 && (((uintptr_t)A.a | (uintptr_t)A.b) & 15) == 0;
 }
 
+// ---------------------------------------------------------------- split sums
+// Few tiles and a long sum: each part of the sum has workgroups of its own, which
+// leave int32 sums in the workspace, and a second launch adds the parts up
+// (integers: their order does not matter) and does the epilogue, eight columns
+// a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_join_kernel(LinArgs A, const int32_t* sums, int parts, int64_t ld, int groups_n) {
+    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = idx / groups_n;
+    if (m >= A.M) return;
+    const int64_t n = idx % groups_n * 8;
+    const int left = (int)min((int64_t)8, A.N - n);
+    const int32_t* p = sums + m * ld + n;   // (ld is a multiple of 8: a row's last piece is whole)
+    v4i lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+    for (int i = 0; i < parts; i += 4) {   // four parts in flight; past the last, it again, not added
+        v4i x[4], y[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int32_t* q = p + min(i + j, parts - 1) * A.part;
+            x[j] = *(const v4i*)q;
+            y[j] = *(const v4i*)(q + 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            lo += i + j < parts ? x[j] : v4i{0, 0, 0, 0};
+            hi += i + j < parts ? y[j] : v4i{0, 0, 0, 0};
+        }
+    }
+    float sb[8], bias[8] = {}, v[8];
+    if (A.s_b && A.b_step)
+        load_some(A.s_b + n, left, sb);
+    else
+#pragma unroll
+        for (int e = 0; e < 8; e++) sb[e] = A.s_b ? A.s_b[0] : 1.f;
+    if (A.bias) load_typed(A.bias, A.bias_type, n, left, bias);
+    const float sa = A.s_a ? A.s_a[A.a_step ? m : 0] : 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (float)(e < 4 ? lo[e & 3] : hi[e & 3]) * sb[e] * sa + bias[e];
+    if (A.z) store_some((T*)A.z + m * A.ldz + n, left, v);
+    act_values(A.act, v);
+    if (A.res) {
+        float r[8];
+        load_some((const T*)A.res + m * A.ldres + n, left, r);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] += r[e];
+    }
+    store_some((T*)A.out + m * A.ldout + n, left, v);
+}
+
+// ---------------------------------------------------------------- choice
 // The kernels, and what a product of `tiles` tiles and K takes in each (us):
 //   start + round * max(1, tiles / 256) + K / 1000 * (step + more * max(0, tiles / 256 - 1))
 // (256 x 256 tiles, one a CU at a time: whole rounds).  Small tiles give every
@@ -618,41 +729,100 @@ constexpr Cost kAny64{64, 64, 2.6f, 1.9f, 2.6f, 2.8f};
 constexpr Cost kRing128{128, 128, 0.41f, 3.40f, 6.84f, 4.92f};
 constexpr Cost kRing256{256, 256, 0.f, 10.3f, 10.4f, 5.22f};
 
-float cost(const Cost& c, const LinArgs& A) {
-    const float tiles = (float)((A.M + c.bm - 1) / c.bm) * (float)((A.N + c.bn - 1) / c.bn) / 256.f, k = (float)A.K / 1000.f;
+float cost(const Cost& c, int64_t M, int64_t N, int64_t K, int parts = 1) {
+    const float tiles = (float)((M + c.bm - 1) / c.bm) * (float)((N + c.bn - 1) / c.bn) * (float)parts / 256.f;
+    const float k = (float)K / 1000.f / (float)parts;
     if (c.bm == 256) return c.start + ceilf(tiles) * (c.round + c.step * k) + fminf(tiles, 1.f) * c.more * k;
     return c.start + c.round * fmaxf(1.f, tiles) + k * (c.step + c.more * fmaxf(0.f, tiles - 1.f));
 }
 
+struct Choice {
+    enum { kS11, kS12, kS22, k64, k128, k256 } kernel;
+    int parts;       // of the sum
+    int64_t klen;    // products of a part, whole steps
+    float time;
+};
+
+constexpr int64_t kPartLen = 512;   // least products of a part
+inline int64_t part_ld(int64_t N) { return (N + 7) / 8 * 8; }
+
+// whole: the operands are whole aligned pieces; room: bytes for the sums of parts.
+Choice choose(int64_t M, int64_t N, int64_t K, bool whole, size_t room) {
+    Choice c{Choice::kS11, 1, 0, cost(kSmall11, M, N, K)};
+    auto take = [&](decltype(c.kernel) kernel, float time, int parts, int64_t klen) {
+        if (time < c.time) c = Choice{kernel, parts, klen, time};
+    };
+    take(Choice::kS12, cost(kSmall12, M, N, K), 1, 0);
+    take(Choice::kS22, cost(kSmall22, M, N, K), 1, 0);
+    const Cost& tile = whole ? kRing64 : kAny64;
+    take(Choice::k64, cost(tile, M, N, K), 1, 0);
+    if (whole) {
+        take(Choice::k128, cost(kRing128, M, N, K), 1, 0);
+        take(Choice::k256, cost(kRing256, M, N, K), 1, 0);
+    }
+    // Split sums of 64 x 64 tiles: a second launch (2.3 us), and the parts' sums written and read (8 bytes at 4 TB/s).
+    for (int want = 2; want <= 32 && K >= want * kPartLen; want *= 2) {
+        const int64_t klen = ((K + want - 1) / want + 127) / 128 * 128;
+        const int parts = (int)((K + klen - 1) / klen);
+        const double bytes = (double)parts * (double)M * (double)part_ld(N) * 4.;
+        if (bytes > (double)room) break;
+        take(Choice::k64, cost(tile, M, N, klen * parts, parts) + 2.3f + (float)(bytes * 2. / 4e6), parts, klen);
+    }
+    return c;
+}
+
 template <typename T>
-hipError_t run_linear(LinArgs A, void*, size_t, hipStream_t stream) {
+hipError_t run_64(const LinArgs& A, bool whole, hipStream_t stream) {
+    return whole ? run_ring<T, 64, 64, 4, 2, 2, 128>(A, stream) : run_any<T>(A, stream);
+}
+
+template <typename T>
+hipError_t run_linear(LinArgs A, void* ws, size_t ws_bytes, hipStream_t stream) {
     const int64_t ld = A.ldres * (int64_t)sizeof(T);
     A.res_dma = A.res && ld % 16 == 0 && ((uintptr_t)A.res & 15) == 0 && ld < ((int64_t)1 << 22);
-    const float s11 = cost(kSmall11, A), s12 = cost(kSmall12, A), s22 = cost(kSmall22, A);
-    const float small = fminf(fminf(s11, s12), s22);
-    if (ring_takes(A)) {
-        const float r64 = cost(kRing64, A), r128 = cost(kRing128, A), r256 = cost(kRing256, A);
-        const float ring = fminf(fminf(r64, r128), r256);
-        if (ring < small) {
-            if (ring == r256) return run_ring<T, 256, 256, 4, 2, 4, 64>(A, stream);
-            if (ring == r128) return run_ring<T, 128, 128, 2, 4, 2, 128>(A, stream);
-            return run_ring<T, 64, 64, 4, 2, 2, 128>(A, stream);
-        }
-    } else if (cost(kAny64, A) < small) {
-        return run_any<T>(A, stream);
+    A.klen = 0;
+    const bool whole = ring_takes(A);
+    const Choice c = choose(A.M, A.N, A.K, whole, ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0);
+    if (c.parts > 1) {
+        LinArgs P = A;   // sums only
+        P.s_a = P.s_b = nullptr;
+        P.bias = P.res = nullptr;
+        P.z = nullptr;
+        P.res_dma = 0;
+        P.out = ws;
+        P.ldout = part_ld(A.N);
+        P.klen = (int32_t)c.klen;
+        P.part = A.M * P.ldout;
+        const hipError_t e = run_64<int32_t>(P, whole, stream);
+        if (e != hipSuccess) return e;
+        A.part = P.part;
+        const int64_t groups = (A.N + 7) / 8;
+        hipLaunchKernelGGL((linear_join_kernel<T>), dim3((unsigned)((A.M * groups + 255) / 256)), dim3(256), 0, stream, A,
+                           (const int32_t*)ws, c.parts, P.ldout, (int)groups);
+        return hipGetLastError();
     }
-    if (small == s11) return run_small<T, 1, 1>(A, stream);
-    if (small == s12) return run_small<T, 1, 2>(A, stream);
-    return run_small<T, 2, 2>(A, stream);
+    switch (c.kernel) {
+        case Choice::kS11: return run_small<T, 1, 1>(A, stream);
+        case Choice::kS12: return run_small<T, 1, 2>(A, stream);
+        case Choice::kS22: return run_small<T, 2, 2>(A, stream);
+        case Choice::k64: return run_64<T>(A, whole, stream);
+        case Choice::k128: return run_ring<T, 128, 128, 2, 4, 2, 128>(A, stream);
+        default: return run_ring<T, 256, 256, 4, 2, 4, 64>(A, stream);
+    }
 }
 
 }  // namespace
 
+// For the sums of parts, if that is how this product would go with room for them.
 size_t linear_fwd_workspace(int64_t M, int64_t N, int64_t K) {
-    (void)M;
-    (void)N;
-    (void)K;
-    return 0;
+    if (M < 1 || N < 1 || K < 1 || M >= kMaxDim || N >= kMaxLd || K >= kMaxSum) return 0;
+    size_t most = 0;
+    for (int whole = 0; whole < 2; whole++) {
+        const Choice c = choose(M, N, K, whole != 0, SIZE_MAX);
+        const size_t need = c.parts > 1 ? (size_t)c.parts * (size_t)(M * part_ld(N)) * 4 : 0;
+        most = need > most ? need : most;
+    }
+    return (most + 255) / 256 * 256;
 }
 
 // Very many rows go in slabs, so that a launch stays below 2^32 threads.

@@ -371,7 +371,7 @@ hipError_t run_codes(const DzArgs& a, const Turn& ta, const Turn& tb, int64_t ti
 
 struct BwdSpace {
     int64_t Mp, Np, tiles_m, tiles_n;
-    int64_t p, q, at, bt, r, c, rmax, cmax, csum, total;
+    int64_t p, q, at, bt, r, c, rmax, cmax, csum, sums, sums_bytes, total;
 };
 
 BwdSpace space(int64_t M, int64_t N, int64_t K) {
@@ -395,6 +395,10 @@ BwdSpace space(int64_t M, int64_t N, int64_t K) {
     s.rmax = take(s.tiles_n * M * 4);
     s.cmax = take(s.tiles_m * N * 4);
     s.csum = take(s.tiles_m * N * 4);
+    // the products' own workspace
+    const size_t wa = linear_fwd_workspace(M, K, s.Np), wb = linear_fwd_workspace(N, K, s.Mp);
+    s.sums_bytes = (int64_t)(wa > wb ? wa : wb);
+    s.sums = take(s.sums_bytes);
     s.total = at;
     return s;
 }
@@ -480,12 +484,12 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     if (by_type(type, [&](auto t) { return run_codes<decltype(t)>(d, ta, tb, tr * tc, (int)tc, s); }) != hipSuccess)
         return NITI_ERR_HIP;
     if (db) {
-        const LinArgs A{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0};
-        if (linear_run(A, type, nullptr, 0, s) != hipSuccess) return NITI_ERR_HIP;
+        const LinArgs A{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
+        if (linear_run(A, type, base + w.sums, (size_t)w.sums_bytes, s) != hipSuccess) return NITI_ERR_HIP;
     }
     if (da) {
-        const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0};
-        if (linear_run(A, type, nullptr, 0, s) != hipSuccess) return NITI_ERR_HIP;
+        const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
+        if (linear_run(A, type, base + w.sums, (size_t)w.sums_bytes, s) != hipSuccess) return NITI_ERR_HIP;
     }
     return NITI_OK;
 }
