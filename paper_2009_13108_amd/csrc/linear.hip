@@ -53,19 +53,43 @@ __device__ __forceinline__ void pick(v16i (&acc)[FN][FM], int want, v16i& x, std
     ((want == I ? (void)(x = acc[I / FM][I % FM]) : (void)0), ...);
 }
 
+// Operands of the epilogue that a call may not have are read from these, so that
+// no load is in a branch, where it would be waited for.
+__device__ const float kOnes[1] = {1.f};
+__device__ const float kZeros[1] = {0.f};
+
+// One bias as loaded, of a type known at run time: from one of two places, the other gives zero.
+struct BiasLoad {
+    uint32_t wide;
+    uint16_t narrow;
+    __device__ __forceinline__ void load(const LinArgs& A, int64_t n) {
+        const bool f32 = A.bias && A.bias_type == NITI_F32, f16 = A.bias && A.bias_type != NITI_F32;
+        wide = (f32 ? (const uint32_t*)A.bias : (const uint32_t*)kZeros)[f32 ? n : 0];
+        narrow = (f16 ? (const uint16_t*)A.bias : (const uint16_t*)kZeros)[f16 ? n : 0];
+    }
+    __device__ __forceinline__ float get(const LinArgs& A) const {
+        const uint16_t h = narrow;
+        const float half = A.bias_type == NITI_F16 ? to_f(__builtin_bit_cast(f16, h)) : to_f(bf16{h});
+        return A.bias_type == NITI_F32 ? __uint_as_float(wide) : half;
+    }
+};
+__device__ __forceinline__ float load_scale(const float* s, int step, int64_t i) { return (s ? s : kOnes)[s && step ? i : 0]; }
+
 // Scales and biases of a tile's columns and scales of its rows, to LDS before
 // the sum begins: loaded in the epilogue they cost it two memory round trips.
 template <int BM, int BN, int NT>
 __device__ __forceinline__ void load_params(const LinArgs& A, float* par, int64_t m0, int64_t n0) {
-    for (int c = threadIdx.x; c < BN; c += NT) {
-        const bool in = n0 + c < A.N;
-        float bias[1] = {0.f};
-        if (A.bias && in) load_typed(A.bias, A.bias_type, n0 + c, 1, bias);
-        par[c] = in ? (A.s_b ? A.s_b[A.b_step ? n0 + c : 0] : 1.f) : 0.f;
-        par[BN + c] = bias[0];
+    static_assert(NT >= BM && NT >= BN, "one column and one row a thread");
+    const int t = threadIdx.x;
+    const int64_t n = min(n0 + t % BN, A.N - 1), m = min(m0 + t % BM, A.M - 1);
+    BiasLoad bias;
+    bias.load(A, n);
+    const float sb = load_scale(A.s_b, A.b_step, n), sa = load_scale(A.s_a, A.a_step, m);
+    if (t < BN) {
+        par[t] = sb;
+        par[BN + t] = bias.get(A);
     }
-    for (int r = threadIdx.x; r < BM; r += NT)
-        par[2 * BN + r] = m0 + r < A.M ? (A.s_a ? A.s_a[A.a_step ? m0 + r : 0] : 1.f) : 0.f;
+    if (t < BM) par[2 * BN + t] = sa;
 }
 
 // A workgroup's part of a split sum: its stretch of K, and its place in the sums (int32_t).
@@ -372,6 +396,7 @@ __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int ti
     const int row = threadIdx.x / (4 * FN), col = threadIdx.x % (4 * FN) * 4;
     const int64_t m = m0 + row, n = n0 + col;
     const int left = row < TM && m < A.M && n < A.N ? (int)min((int64_t)4, A.N - n) : 0;
+    // (in a branch, and so waited for, but by the waves of those threads alone)
     float sa = 0.f, sb[4], bias[4] = {0.f, 0.f, 0.f, 0.f}, res[4] = {0.f, 0.f, 0.f, 0.f};
     if (left > 0) {
         sa = A.s_a ? A.s_a[A.a_step ? m : 0] : 1.f;
@@ -582,7 +607,6 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 :
         b_sw[i] = R::swz(row & 15);
     }
     float* par = (float*)(ring + NS * R::STAGE);
-    load_params<BM, BN, R::NT>(A, par, m0, n0);
 #pragma unroll
     for (int s = 0; s < NS - 1; s++) {
         begin_step();
@@ -590,6 +614,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 :
         for (int i = 0; i < R::LA + R::LB; i++) load(i);
         end_step();
     }
+    load_params<BM, BN, R::NT>(A, par, m0, n0);   // behind the ring's first loads, whose latency it shares
     v4i fa[2][R::FM], fb[2][R::FN];
     auto read = [&](const int8_t* st, int d, int i) {   // fragment i of FN + FM of a depth
         const int kp = (lane >> 5) + 2 * d;

@@ -154,15 +154,24 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top_bits) {
 }
 
 // Codes as floats that begin at kCode = 1.5 * 2^23: there a step of a float is 1,
-// so that one multiply-add rounds v * inv to the nearest integer, ties to even, and
-// leaves the code as the float's lowest byte.  For a finite row |v * inv| is at most
-// 127 and a rounding error, which rounds to 127.  Rows that are not finite (inv 0)
-// may leave anything: their words are masked (see code_mask).
+// so that adding it rounds v * inv to the nearest integer, ties to even, and
+// leaves the code as the float's lowest byte.  The product is rounded first: of
+// 16-bit values many lie half way between two codes (half a row's largest is 63.5
+// steps), where the rounding takes back that of inv; one multiply-add would go by
+// inv's error there (a fifth more distance from the exact codes).  For a
+// finite row |v * inv| is at most 127 and a rounding error, which rounds to 127.  Rows that
+// are not finite (inv 0) may leave anything: their words are masked (see code_mask).
 constexpr float kCode = 12582912.f;
-__device__ __forceinline__ float code_rtn(float v, float inv) { return __builtin_fmaf(v, inv, kCode); }
+__device__ __forceinline__ float code_rtn(float v, float inv) {
+#pragma clang fp contract(off)
+    const float r = v * inv;
+    return r + kCode;
+}
 // Stochastically: floor(v * inv + u) is v * inv on average over u in [0, 1).
 __device__ __forceinline__ float code_sr(float v, float inv, float u) {
-    return __builtin_amdgcn_fmed3f(floorf(__builtin_fmaf(v, inv, u)), -127.f, 127.f) + kCode;
+#pragma clang fp contract(off)
+    const float r = v * inv;
+    return __builtin_amdgcn_fmed3f(floorf(r + u), -127.f, 127.f) + kCode;
 }
 __device__ __forceinline__ float code_value(float c) { return c - kCode; }
 // All bits for a row with codes, none for one without.
