@@ -146,11 +146,11 @@ __device__ __forceinline__ void adamw_elements(const Entry& E, const Step& S, in
         const BlockScale bm = block_scale(half_max(tm), kUnitM), bv = block_scale(half_max(tv), kUnitV);
         int8_t cm[PT];
         uint8_t cv[PT];
-        const uint64_t pair0 = ((uint64_t)E.block0 * kBlock + (uint64_t)i) >> 1;
+        DrawStream draws(S.seed, S.call, ((uint64_t)E.block0 * kBlock + (uint64_t)i) >> 1);   // one for each two elements
 #pragma unroll
         for (int e = 0; e < PT; e += 2) {
             uint64_t r = 0;
-            if (S.sr) r = sr_draw(S.seed, S.call, pair0 + e / 2);
+            if (S.sr) r = draws.next();
 #pragma unroll
             for (int o = 0; o < 2; o++) {
                 float rm = 127.f * __builtin_amdgcn_sqrtf(fabsf(m[e + o]) * bm.inv);

@@ -26,6 +26,8 @@ struct LinArgs {
 };
 
 hipError_t linear_run(const LinArgs& a, int type, void* ws, size_t ws_bytes, hipStream_t stream);
+// Both, in one launch where that pays.
+hipError_t linear_run_pair(const LinArgs& a, const LinArgs& b, int type, void* ws, size_t ws_bytes, hipStream_t stream);
 size_t linear_fwd_workspace(int64_t M, int64_t N, int64_t K);
 size_t linear_bwd_workspace(int64_t M, int64_t N, int64_t K);
 size_t rmsnorm_bwd_workspace(int64_t M, int64_t D);

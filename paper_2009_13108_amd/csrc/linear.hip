@@ -385,13 +385,13 @@ inline bool word_rows(const LinArgs& A) { return A.lda % 4 == 0 && A.ldb % 4 == 
 constexpr int SW = 8;
 
 template <typename T, int FM, int FN, bool BYTES>
-__global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int tiles_n) {
+__device__ __forceinline__ void small_tile(const LinArgs& A, int tiles_n, int block) {
     constexpr int TM = 16 * FM, TN = 16 * FN, PITCH = TN + 4;
     constexpr int KB = FM + FN <= 2 ? 4 : (FM + FN <= 3 ? 2 : 1);   // steps in flight of a wave
     __shared__ __attribute__((aligned(16))) int32_t red[SW * TM * PITCH];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * TM, n0 = (int64_t)(blockIdx.x % tiles_n) * TN;
+    const int64_t m0 = (int64_t)(block / tiles_n) * TM, n0 = (int64_t)(block % tiles_n) * TN;
     // the epilogue's operands of the threads that end a row's four channels, ahead of the sum
     const int row = threadIdx.x / (4 * FN), col = threadIdx.x % (4 * FN) * 4;
     const int64_t m = m0 + row, n = n0 + col;
@@ -492,6 +492,24 @@ __global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int ti
     store_some((T*)A.out + m * A.ldout + n, left, v);
 }
 
+template <typename T, int FM, int FN, bool BYTES>
+__global__ __launch_bounds__(64 * SW) void linear_small_kernel(LinArgs A, int tiles_n) {
+    small_tile<T, FM, FN, BYTES>(A, tiles_n, blockIdx.x);
+}
+
+// Two products in one launch (word-aligned rows).
+struct LinPair {
+    LinArgs a[2];
+    int tiles_n[2];
+    int blocks;   // tiles of the first
+};
+
+template <typename T, int FM, int FN>
+__global__ __launch_bounds__(64 * SW) void linear_small_pair_kernel(LinPair P) {
+    const int i = (int)blockIdx.x < P.blocks ? 0 : 1;
+    small_tile<T, FM, FN, false>(P.a[i], P.tiles_n[i], (int)blockIdx.x - i * P.blocks);
+}
+
 template <typename T, int FM, int FN>
 hipError_t run_small(const LinArgs& A, hipStream_t stream) {
     const int64_t tm = (A.M + 16 * FM - 1) / (16 * FM), tn = (A.N + 16 * FN - 1) / (16 * FN);
@@ -532,14 +550,13 @@ struct Ring {
 };
 
 template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
-__global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_kernel(LinArgs A, int tiles_n) {
+__device__ __forceinline__ void ring_tile(const LinArgs& A, int tiles_n, int block) {
     using R = Ring<BM, BN, NS, WGM, WGN, KS>;
-    take_part<T>(A);
     extern __shared__ __attribute__((aligned(1024))) int8_t ring[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WGM, wn = wave / WGM;
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * BM, n0 = (int64_t)(blockIdx.x % tiles_n) * BN;
+    const int64_t m0 = (int64_t)(block / tiles_n) * BM, n0 = (int64_t)(block % tiles_n) * BN;
     const int rows_a = (int)min((int64_t)BM, A.M - m0), rows_b = (int)min((int64_t)BN, A.N - n0);
     const int K = (int)A.K, nk = (K + KS - 1) / KS;
     // Offsets from the tile's first row; rows past the operand lie past the descriptor's end and load zeros.
@@ -666,15 +683,34 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 :
 }
 
 template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
+__global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_kernel(LinArgs A, int tiles_n) {
+    take_part<T>(A);
+    ring_tile<T, BM, BN, NS, WGM, WGN, KS>(A, tiles_n, blockIdx.x);
+}
+
+// Two products in one launch.
+template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
+__global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_pair_kernel(LinPair P) {
+    const int i = (int)blockIdx.x < P.blocks ? 0 : 1;
+    ring_tile<T, BM, BN, NS, WGM, WGN, KS>(P.a[i], P.tiles_n[i], (int)blockIdx.x - i * P.blocks);
+}
+
+// Once for each kernel: it may have more than 64 KiB of LDS.
+template <auto kernel, int LDS>
+hipError_t allow_lds() {
+    static bool done = false;
+    if (done) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    done = e == hipSuccess;
+    return e;
+}
+
+template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
 hipError_t run_ring(const LinArgs& A, hipStream_t stream) {
     using R = Ring<BM, BN, NS, WGM, WGN, KS>;
-    const auto kernel = linear_ring_kernel<T, BM, BN, NS, WGM, WGN, KS>;
-    static bool attr_done = false;
-    if (!attr_done) {
-        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, R::LDS);
-        if (e != hipSuccess) return e;
-        attr_done = true;
-    }
+    constexpr auto kernel = linear_ring_kernel<T, BM, BN, NS, WGM, WGN, KS>;
+    const hipError_t e = allow_lds<kernel, R::LDS>();
+    if (e != hipSuccess) return e;
     const int64_t tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn), A.klen ? (unsigned)((A.K + A.klen - 1) / A.klen) : 1), dim3(R::NT), R::LDS,
                        stream, A, (int)tn);
@@ -735,34 +771,43 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs A, const int32
 }
 
 // ---------------------------------------------------------------- choice
-// The kernels, and what a product of `tiles` tiles and K takes in each (us):
-//   start + round * max(1, tiles / 256) + K / 1000 * (step + more * max(0, tiles / 256 - 1))
-// (256 x 256 tiles, one a CU at a time: whole rounds).  Small tiles give every
-// CU work and split the sum, large ones load less for each product.  Fitted to
-// 540 random products of 1..8192 x 32..9216 x 32..9216 timed with each kernel;
-// what the model picks takes 2.1% longer than the fastest in the mean, and
-// 64 x 64 tiles alone would take 29%.
+// The kernels, and what a product takes in each (us), with t = tiles / 256 CUs and
+// k = K / 1000:
+//   kSpread  start + round * max(1, t) + k * (step + more * max(0, t - 1))
+//   kTwo     start + round * max(1, t) + k * (step * ceil(t / 2) + more * max(1, t))   (two tiles or more a CU at a time)
+//   kRounds  start + ceil(t) * (round + k * step) + k * more * min(1, t)               (one tile a CU at a time)
+// Small tiles give every CU work and split the sum, large ones load less for each
+// product; 128 x 128 tiles have a ring of four stages, one a CU, which a
+// CU with one tile needs to cover a load's latency (800 x 2880 x 3712, 161 tiles: 28.3 ->
+// 20.5 us), or of two, two tiles a CU (2048 x 4096 x 4096: 38 us, 44 with four).  Fitted to
+// 500 random products of 1..8192 x 32..9216 x 32..9216 timed with each kernel;
+// what the model picks takes 1.4% longer than the fastest of these seven in the
+// mean, 64 x 64 tiles alone 33%.
+enum CostForm { kSpread, kTwo, kRounds };
 struct Cost {
     int bm, bn;
+    CostForm form;
     float start, round, step, more;
 };
-constexpr Cost kSmall11{16, 16, 2.12f, 0.39f, 0.63f, 0.88f};
-constexpr Cost kSmall12{16, 32, 2.13f, 0.50f, 0.96f, 1.11f};
-constexpr Cost kSmall22{32, 32, 2.03f, 0.88f, 1.13f, 1.49f};
-constexpr Cost kRing64{64, 64, 2.00f, 1.47f, 2.01f, 2.17f};
-constexpr Cost kAny64{64, 64, 2.6f, 1.9f, 2.6f, 2.8f};
-constexpr Cost kRing128{128, 128, 0.41f, 3.40f, 6.84f, 4.92f};
-constexpr Cost kRing256{256, 256, 0.f, 10.3f, 10.4f, 5.22f};
+constexpr Cost kSmall11{16, 16, kSpread, 1.93f, 0.56f, 0.58f, 0.81f};
+constexpr Cost kSmall12{16, 32, kSpread, 1.92f, 0.61f, 0.95f, 1.33f};
+constexpr Cost kSmall22{32, 32, kSpread, 2.06f, 0.75f, 1.18f, 1.90f};
+constexpr Cost kRing64{64, 64, kTwo, 2.09f, 1.02f, 0.32f, 2.21f};
+constexpr Cost kAny64{64, 64, kTwo, 2.6f, 1.5f, 0.4f, 2.8f};   // 1.3 times the ring's: 1000 x 1500 x 1111 11.4 us, 1000 x 1504 x 1104 8.6
+constexpr Cost kRing128{128, 128, kTwo, 0.96f, 3.17f, 3.79f, 3.45f};
+constexpr Cost kDeep128{128, 128, kRounds, 0.12f, 4.49f, 3.72f, 2.33f};
+constexpr Cost kRing256{256, 256, kRounds, 0.41f, 11.1f, 9.31f, 5.98f};
 
 float cost(const Cost& c, int64_t M, int64_t N, int64_t K, int parts = 1) {
-    const float tiles = (float)((M + c.bm - 1) / c.bm) * (float)((N + c.bn - 1) / c.bn) * (float)parts / 256.f;
-    const float k = (float)K / 1000.f / (float)parts;
-    if (c.bm == 256) return c.start + ceilf(tiles) * (c.round + c.step * k) + fminf(tiles, 1.f) * c.more * k;
-    return c.start + c.round * fmaxf(1.f, tiles) + k * (c.step + c.more * fmaxf(0.f, tiles - 1.f));
+    const float t = (float)((M + c.bm - 1) / c.bm) * (float)((N + c.bn - 1) / c.bn) * (float)parts / 256.f;
+    const float k = (float)K / 1000.f / (float)parts, one = fmaxf(1.f, t);
+    if (c.form == kRounds) return c.start + ceilf(t) * (c.round + c.step * k) + fminf(t, 1.f) * c.more * k;
+    if (c.form == kTwo) return c.start + c.round * one + k * (c.step * ceilf(0.5f * t) + c.more * one);
+    return c.start + c.round * one + k * (c.step + c.more * (one - 1.f));
 }
 
 struct Choice {
-    enum { kS11, kS12, kS22, k64, k128, k256 } kernel;
+    enum { kS11, kS12, kS22, k64, k128, k128d, k256 } kernel;
     int parts;       // of the sum
     int64_t klen;    // products of a part, whole steps
     float time;
@@ -783,6 +828,8 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool whole, size_t room) {
     take(Choice::k64, cost(tile, M, N, K), 1, 0);
     if (whole) {
         take(Choice::k128, cost(kRing128, M, N, K), 1, 0);
+        // (where tiles outnumber the CUs, two a CU come out a little better than the model has them)
+        take(Choice::k128d, cost(kDeep128, M, N, K) * (M * N > 256 * 128 * 128 ? 1.08f : 1.f), 1, 0);
         take(Choice::k256, cost(kRing256, M, N, K), 1, 0);
     }
     // Split sums of 64 x 64 tiles: a second launch (2.3 us), and the parts' sums written and read (8 bytes at 4 TB/s).
@@ -798,7 +845,7 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool whole, size_t room) {
 
 template <typename T>
 hipError_t run_64(const LinArgs& A, bool whole, hipStream_t stream) {
-    return whole ? run_ring<T, 64, 64, 4, 2, 2, 128>(A, stream) : run_any<T>(A, stream);
+    return whole ? run_ring<T, 64, 64, 3, 2, 2, 128>(A, stream) : run_any<T>(A, stream);
 }
 
 template <typename T>
@@ -832,11 +879,58 @@ hipError_t run_linear(LinArgs A, void* ws, size_t ws_bytes, hipStream_t stream) 
         case Choice::kS22: return run_small<T, 2, 2>(A, stream);
         case Choice::k64: return run_64<T>(A, whole, stream);
         case Choice::k128: return run_ring<T, 128, 128, 2, 4, 2, 128>(A, stream);
+        case Choice::k128d: return run_ring<T, 128, 128, 4, 4, 2, 128>(A, stream);
         default: return run_ring<T, 256, 256, 4, 2, 4, 64>(A, stream);
     }
 }
 
+// Two products that are ready together, in one launch where both are small: a
+// launch takes longer than either.
+template <typename T, int FM, int FN>
+hipError_t run_small_pair(const LinArgs& A, const LinArgs& B, hipStream_t stream) {
+    const auto tiles = [](int64_t n, int t) { return (n + t - 1) / t; };
+    const int64_t na = tiles(A.N, 16 * FN), nb = tiles(B.N, 16 * FN), ba = tiles(A.M, 16 * FM) * na, bb = tiles(B.M, 16 * FM) * nb;
+    hipLaunchKernelGGL((linear_small_pair_kernel<T, FM, FN>), dim3((unsigned)(ba + bb)), dim3(64 * SW), 0, stream,
+                       LinPair{{A, B}, {(int)na, (int)nb}, (int)ba});
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_ring64_pair(const LinArgs& A, const LinArgs& B, hipStream_t stream) {
+    using R = Ring<64, 64, 3, 2, 2, 128>;
+    constexpr auto kernel = linear_ring_pair_kernel<T, 64, 64, 3, 2, 2, 128>;
+    const hipError_t e = allow_lds<kernel, R::LDS>();
+    if (e != hipSuccess) return e;
+    const auto tiles = [](int64_t n) { return (n + 63) / 64; };
+    const int64_t na = tiles(A.N), nb = tiles(B.N), ba = tiles(A.M) * na, bb = tiles(B.M) * nb;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(ba + bb)), dim3(R::NT), R::LDS, stream, LinPair{{A, B}, {(int)na, (int)nb}, (int)ba});
+    return hipGetLastError();
+}
+
+constexpr float kLaunch = 2.5f;   // us that a second launch takes at least
+
 }  // namespace
+
+hipError_t linear_run_pair(const LinArgs& a, const LinArgs& b, int type, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const bool whole = ring_takes(a) && ring_takes(b) && !a.res && !b.res && a.M < kMaxSum && b.M < kMaxSum;
+    if (whole) {
+        const Choice ca = choose(a.M, a.N, a.K, true, ws_bytes), cb = choose(b.M, b.N, b.K, true, ws_bytes);
+        const Choice& c = ca.time > cb.time ? ca : cb;
+        const bool small_a = ca.parts == 1 && ca.kernel <= Choice::kS22, small_b = cb.parts == 1 && cb.kernel <= Choice::kS22;
+        if (small_a && small_b) {
+            return by_type(type, [&](auto t) {
+                using T = decltype(t);
+                if (c.kernel == Choice::kS11) return run_small_pair<T, 1, 1>(a, b, stream);
+                if (c.kernel == Choice::kS12) return run_small_pair<T, 1, 2>(a, b, stream);
+                return run_small_pair<T, 2, 2>(a, b, stream);
+            });
+        }
+        if (cost(kRing64, a.M, a.N, a.K) + cost(kRing64, b.M, b.N, b.K) < ca.time + cb.time + kLaunch)
+            return by_type(type, [&](auto t) { return run_ring64_pair<decltype(t)>(a, b, stream); });
+    }
+    const hipError_t e = linear_run(a, type, ws, ws_bytes, stream);
+    return e == hipSuccess ? linear_run(b, type, ws, ws_bytes, stream) : e;
+}
 
 // For the sums of parts, if that is how this product would go with room for them.
 size_t linear_fwd_workspace(int64_t M, int64_t N, int64_t K) {

@@ -6,12 +6,14 @@
 // Folding b's scale into the rows (it varies along their sum) and a's into the
 // columns leaves both sums with integers only.
 //
-// Five launches.  (1) Tiles of 16 x 256 of dz leave the maxima of their rows and
+// Up to five launches.  (1) Tiles of 16 x 256 of dz leave the maxima of their rows and
 // the maxima and sums of their columns; (2) those are joined, in a fixed order:
 // r, c and dbias; (3) dz is formed again, in tiles of 128 x 128, for the codes of
 // rows and columns at once, the columns' transposed through LDS, and the same
 // launch transposes a and b: the products take rows along their sum; (4), (5) the
-// products, by the forward kernels.  dy and z are read twice, the second time
+// products, by the forward kernels.  Where both products are small they share a
+// launch, and where the tiles of step 1 are few step 3 joins them itself: three
+// launches.  dy and z are read twice, the second time
 // mostly from the last-level cache; holding dz for step 3 would round it or cost
 // four bytes an element each way.
 #include <type_traits>
@@ -23,7 +25,7 @@ namespace niti {
 namespace {
 
 constexpr int SR = 16, SC = 256; // tile of step 1
-constexpr int CT = 128;          // tile of step 3
+constexpr int CT = 128, CTH = 512;   // tile of step 3 and its threads
 constexpr int CP = CT + 4;       // its LDS pitch: lanes that write one row group hit distinct banks, two by two
 constexpr int64_t kPad = 16;     // sums are padded to whole 16-byte pieces
 
@@ -39,6 +41,7 @@ struct DzArgs {
     int64_t tiles_m, tiles_n;   // of step 1
     int32_t a_step, b_step;
     int32_t act, sr;
+    int32_t join;     // step 3 joins the tiles of step 1
     uint64_t seed;
     uint32_t call;
     int8_t* p;        // [M][Np] codes of the rows, or NULL
@@ -152,6 +155,14 @@ __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     }
 }
 
+// Row m's and column c's scales from the tiles' values, in the order of the tiles.
+__device__ __forceinline__ RowScale join_row(const DzArgs& a, int64_t m) {
+    uint32_t mx = 0;
+#pragma unroll 8
+    for (int64_t t = 0; t < a.tiles_n; t++) mx = max(mx, a.rmax[t * a.M + m]);
+    return row_scale(mx);
+}
+
 // Step 2.  Columns: 64 a workgroup, the tiles' values shared by 16 groups and joined in order.  Rows: 1024 a workgroup.
 __global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks) {
     __shared__ float ssum[16][64];
@@ -159,10 +170,7 @@ __global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks)
     if ((int)blockIdx.x >= col_blocks) {
         const int64_t m = (int64_t)((int)blockIdx.x - col_blocks) * 1024 + threadIdx.x;
         if (m >= a.M) return;
-        uint32_t mx = 0;
-#pragma unroll 8
-        for (int64_t t = 0; t < a.tiles_n; t++) mx = max(mx, a.rmax[t * a.M + m]);
-        const RowScale rs = row_scale(mx);
+        const RowScale rs = join_row(a, m);
         a.r[m] = rs.scale;
         a.r[a.M + m] = rs.inv;
         return;
@@ -206,8 +214,8 @@ __global__ __launch_bounds__(1024) void dz_join_kernel(DzArgs a, int col_blocks)
 __device__ __forceinline__ void store_turned(const int8_t (*tile)[CP], int8_t* out, int64_t ld, int64_t n0, int64_t rows, int64_t m0,
                                              int64_t cols) {
 #pragma unroll
-    for (int i = 0; i < CT * CT / 16 / 256; i++) {
-        const int idx = i * 256 + threadIdx.x, row = idx / (CT / 16), pc = idx % (CT / 16) * 16;
+    for (int i = 0; i < CT * CT / 16 / CTH; i++) {
+        const int idx = i * CTH + threadIdx.x, row = idx / (CT / 16), pc = idx % (CT / 16) * 16;
         if (n0 + row >= rows || m0 + pc >= cols) continue;
         uint32_t w[4];
         __builtin_memcpy(w, &tile[row][pc], 16);
@@ -235,35 +243,33 @@ struct Turn {
 
 __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*tile)[CP]) {
     const int64_t r0 = (int64_t)(block / a.tiles_k) * CT, k0 = (int64_t)(block % a.tiles_k) * CT;
-    const int pc = (threadIdx.x & 7) * 16, row = (threadIdx.x >> 3) * 4;   // four rows of 16 bytes a thread
-    uint4 v[4];
+    const int pc = (threadIdx.x & 15) * 8, row = (threadIdx.x >> 4) * 4;   // four rows of 8 bytes a thread
+    uint64_t v[4];
     const int64_t k = k0 + pc;
-    if (a.K >= 16) {
+    if (a.K >= 8) {
         // (no load in a branch: past the edges the last row's or a row's last piece, set right afterwards)
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = load16_any(a.x + min(r0 + row + i, a.R - 1) * a.ldx + min(k, a.K - 16));
+        for (int i = 0; i < 4; i++) __builtin_memcpy(&v[i], a.x + min(r0 + row + i, a.R - 1) * a.ldx + min(k, a.K - 8), 8);
         if (k0 + CT > a.K || r0 + CT > a.R) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                const int down = r0 + row + i < a.R ? (int)min((int64_t)16, max((int64_t)0, k + 16 - a.K)) : 16;
-                const unsigned __int128 x = __builtin_bit_cast(unsigned __int128, v[i]);
-                v[i] = __builtin_bit_cast(uint4, down < 16 ? x >> (8 * down) : (unsigned __int128)0);
+                const int down = r0 + row + i < a.R ? (int)min((int64_t)8, max((int64_t)0, k + 8 - a.K)) : 8;
+                v[i] = down < 8 ? v[i] >> (8 * down) : 0;
             }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            uint32_t w[4] = {0, 0, 0, 0};
+            v[i] = 0;
             if (r0 + row + i < a.R)
-                for (int e = 0; e < a.K - k; e++) w[e >> 2] |= (uint32_t)(uint8_t)a.x[(r0 + row + i) * a.ldx + k + e] << (8 * (e & 3));
-            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int e = 0; e < a.K - k; e++) v[i] |= (uint64_t)(uint8_t)a.x[(r0 + row + i) * a.ldx + k + e] << (8 * e);
         }
     }
 #pragma unroll
-    for (int g = 0; g < 4; g++) {
+    for (int g = 0; g < 2; g++) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = g == 0 ? v[i].x : (g == 1 ? v[i].y : (g == 2 ? v[i].z : v[i].w));
+        for (int i = 0; i < 4; i++) w[i] = (uint32_t)(v[i] >> (32 * g));
         turn4(w);
 #pragma unroll
         for (int i = 0; i < 4; i++) *(uint32_t*)&tile[pc + 4 * g + i][row] = w[i];
@@ -274,8 +280,9 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
 
 // Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
 template <typename T, int KIND>
-__global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int tiles_c) {
+__global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int tiles_c) {
     __shared__ __attribute__((aligned(16))) int8_t tile[CT][CP];
+    __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[CT];
     int block = blockIdx.x;
     if (block < ta.blocks) {
         turn_tile(ta, block, tile);
@@ -288,56 +295,93 @@ __global__ __launch_bounds__(256) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
     }
     block -= tb.blocks;
     const int64_t m0 = (int64_t)(block / tiles_c) * CT, n0 = (int64_t)(block % tiles_c) * CT;
-    const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 8;   // 8 columns of 8 rows a thread
+    const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 4;   // 8 columns of 4 rows a thread
     const int c = (int)(n0 + col);
-    float sb[CH], ci[CH];
+    float sb[CH], ci[CH], sa[4];
+    DzRows<T, KIND, 4> rows;
+    rows.load(a, m0 + row0, 1, c);
+#pragma unroll
+    for (int i = 0; i < 4; i++) sa[i] = a.s_a[a.a_step ? min(m0 + row0 + i, a.M - 1) : 0];
     load_cols<KIND>(a.s_b, a.b_step, c, (int)a.N, sb);
-    load_cols<KIND>(a.c + a.N, 1, c, (int)a.N, ci);
+    {   // the tile's factors: 128 threads a row each, 128 a column
+        const int i = threadIdx.x & (CT - 1);
+        const int64_t m = min(m0 + i, a.M - 1), n = min(n0 + i, a.N - 1);
+        if (threadIdx.x < CT) {
+            float inv;
+            if (a.join) {
+                const RowScale rs = join_row(a, m);
+                if (n0 == 0 && m0 + i < a.M) a.r[m] = rs.scale;
+                inv = rs.inv;
+            } else {
+                inv = a.r[a.M + m];
+            }
+            rinv[i] = inv;
+        } else if (threadIdx.x < 2 * CT) {
+            float inv;
+            if (a.join) {
+                float s = 0.f;
+                uint32_t mx = 0;
+#pragma unroll 8
+                for (int64_t t = 0; t < a.tiles_m; t++) {
+                    s += a.csum[t * a.N + n];
+                    mx = max(mx, a.cmax[t * a.N + n]);
+                }
+                const RowScale rs = row_scale(mx);
+                if (m0 == 0 && n0 + i < a.N) {
+                    a.c[n] = rs.scale;
+                    if (a.dbias) a.dbias[n] = s;
+                }
+                inv = rs.inv;
+            } else {
+                inv = a.c[a.N + n];
+            }
+            cinv[i] = n0 + i < a.N ? inv : 0.f;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < CH; e++) ci[e] = cinv[col + e];
     uint32_t cmask[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < CH; e++) cmask[e >> 2] |= (code_mask(ci[e]) & 0xFFu) << (8 * (e & 3));
-#pragma unroll 1
-    for (int h = 0; h < 2; h++) {
-        uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
-        DzRows<T, KIND, 4> rows;
-        rows.load(a, m0 + row0 + 4 * h, 1, c);
-        float ri[4], sa[4];
+    uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int64_t m = min(m0 + row0 + 4 * h + i, a.M - 1);
-            ri[i] = a.r[a.M + m];
-            sa[i] = a.s_a[a.a_step ? m : 0];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int64_t m = m0 + row0 + 4 * h + i;
-            const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
-            float d[CH], pc[CH], cc[CH];
-            rows.get(a, i, m, c, d);
-            uint64_t r[CH];
-#pragma unroll
-            for (int e = 0; e < CH; e++) r[e] = a.sr ? sr_draw(a.seed, a.call, (uint64_t)(m * a.N + c + e)) : 0;
+    for (int i = 0; i < 4; i++) {
+        const int64_t m = m0 + row0 + i;
+        const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
+        float d[CH], pc[CH], cc[CH];
+        rows.get(a, i, m, c, d);
+        const float ri = rinv[row0 + i];
+        if (a.sr) {
+            DrawStream r(a.seed, a.call, (uint64_t)(m * a.N + c));
 #pragma unroll
             for (int e = 0; e < CH; e++) {
-                // (past the edges dz is 0, and so are the codes: a draw is below 1)
-                pc[e] = a.sr ? code_sr(d[e] * sb[e], ri[i], draw_hi(r[e])) : code_rtn(d[e] * sb[e], ri[i]);
-                cc[e] = a.sr ? code_sr(d[e] * sa[i], ci[e], draw_lo(r[e])) : code_rtn(d[e] * sa[i], ci[e]);
+                const uint64_t u = r.next();
+                pc[e] = code_sr(d[e] * sb[e], ri, draw_hi(u));
+                cc[e] = code_sr(d[e] * sa[i], ci[e], draw_lo(u));
             }
-            if (a.p && in && c < a.Np) {
-                const uint32_t mask = code_mask(ri[i]);
-                const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
-                __builtin_memcpy(a.p + m * a.Np + c, w, CH);
+        } else {
+#pragma unroll
+            for (int e = 0; e < CH; e++) {
+                pc[e] = code_rtn(d[e] * sb[e], ri);
+                cc[e] = code_rtn(d[e] * sa[i], ci[e]);
             }
-            qc[i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[0];
-            qc[i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[1];
         }
-#pragma unroll
-        for (int g = 0; g < 2; g++) {
-            uint32_t w[4] = {qc[0][g], qc[1][g], qc[2][g], qc[3][g]};
-            turn4(w);
-#pragma unroll
-            for (int i = 0; i < 4; i++) *(uint32_t*)&tile[col + 4 * g + i][row0 + 4 * h] = w[i];
+        // (past the edges dz is 0, and so are the codes: a draw is below 1)
+        if (a.p && in && c < a.Np) {
+            const uint32_t mask = code_mask(ri);
+            const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
+            __builtin_memcpy(a.p + m * a.Np + c, w, CH);
         }
+        qc[i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[0];
+        qc[i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[1];
+    }
+#pragma unroll
+    for (int g = 0; g < 2; g++) {
+        uint32_t w[4] = {qc[0][g], qc[1][g], qc[2][g], qc[3][g]};
+        turn4(w);
+#pragma unroll
+        for (int i = 0; i < 4; i++) *(uint32_t*)&tile[col + 4 * g + i][row0] = w[i];
     }
     if (!a.q) return;
     __syncthreads();
@@ -363,7 +407,7 @@ hipError_t run_stats(const DzArgs& a, hipStream_t stream) {
 template <typename T>
 hipError_t run_codes(const DzArgs& a, const Turn& ta, const Turn& tb, int64_t tiles, int tiles_c, hipStream_t stream) {
     return by_kind(a.N, [&](auto k) {
-        hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(256), 0,
+        hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(CTH), 0,
                            stream, a, ta, tb, tiles_c);
         return hipGetLastError();
     });
@@ -474,23 +518,25 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.cmax = (uint32_t*)(base + w.cmax);
     d.csum = (float*)(base + w.csum);
     if (by_type(type, [&](auto t) { return run_stats<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
-    const int64_t cols = (N + 63) / 64;
-    hipLaunchKernelGGL(dz_join_kernel, dim3((unsigned)(cols + (M + 1023) / 1024)), dim3(1024), 0, s, d, (int)cols);
-    if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
+    // Tiles of step 3 read those of step 1 that they lie in, each again: up to 16 by 8 of them (256 x 2048) that takes less than a launch.
+    d.join = (da || db) && w.tiles_m <= 16 && w.tiles_n <= 8;
+    if (!d.join) {
+        const int64_t cols = (N + 63) / 64;
+        hipLaunchKernelGGL(dz_join_kernel, dim3((unsigned)(cols + (M + 1023) / 1024)), dim3(1024), 0, s, d, (int)cols);
+        if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
+    }
     if (!da && !db) return NITI_OK;
     const int64_t tr = (M + CT - 1) / CT, tc = (N + CT - 1) / CT, tk = (K + CT - 1) / CT;
     Turn ta{a, (int8_t*)(base + w.at), lda, M, w.Mp, K, db ? (int32_t)(tr * tk) : 0, (int32_t)tk};
     Turn tb{b, (int8_t*)(base + w.bt), ldb, N, w.Np, K, da ? (int32_t)(tc * tk) : 0, (int32_t)tk};
     if (by_type(type, [&](auto t) { return run_codes<decltype(t)>(d, ta, tb, tr * tc, (int)tc, s); }) != hipSuccess)
         return NITI_ERR_HIP;
-    if (db) {
-        const LinArgs A{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
-        if (linear_run(A, type, base + w.sums, (size_t)w.sums_bytes, s) != hipSuccess) return NITI_ERR_HIP;
-    }
-    if (da) {
-        const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
-        if (linear_run(A, type, base + w.sums, (size_t)w.sums_bytes, s) != hipSuccess) return NITI_ERR_HIP;
-    }
+    const LinArgs B{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
+    const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
+    void* sums = base + w.sums;
+    const hipError_t e = da && db ? linear_run_pair(B, A, type, sums, (size_t)w.sums_bytes, s)
+                                  : linear_run(da ? A : B, type, sums, (size_t)w.sums_bytes, s);
+    if (e != hipSuccess) return NITI_ERR_HIP;
     return NITI_OK;
 }
 

@@ -86,12 +86,16 @@ template <typename T>
 __device__ __forceinline__ void put_piece(const RowArgs& a, int64_t m, int64_t c, int n, float (&v)[CH], const RowScale& rs) {
     if (a.q) {
         float code[CH];
+        if (a.sr) {
+            DrawStream r(a.seed, a.call, (uint64_t)((a.m0 + m) * a.D + c));
 #pragma unroll
-        for (int e = 0; e < CH; e++) {
-            const float u = a.sr ? draw_hi(sr_draw(a.seed, a.call, (uint64_t)((a.m0 + m) * a.D + c + e))) : 0.f;
-            code[e] = a.sr ? code_sr(v[e], rs.inv, u) : code_rtn(v[e], rs.inv);
-            v[e] = code_value(code[e]) * rs.scale;
+            for (int e = 0; e < CH; e++) code[e] = code_sr(v[e], rs.inv, draw_hi(r.next()));
+        } else {
+#pragma unroll
+            for (int e = 0; e < CH; e++) code[e] = code_rtn(v[e], rs.inv);
         }
+#pragma unroll
+        for (int e = 0; e < CH; e++) v[e] = code_value(code[e]) * rs.scale;
         store_codes(a.q + m * a.ldq + c, n, code, code_mask(rs.inv));
     }
     if (a.y) store_some((T*)a.y + m * a.ldy + c, n, v);
@@ -289,7 +293,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
 #pragma unroll
         for (int e = 0; e < CH; e++) dg[i][e] = 0.f;
     }
-    // A row's loads go out while the row before it is worked on (past the last row, that one's again).
+    // A row's loads go out while the row before it is worked on (past the last row, that one's again);
+    // sixteen waves hide them for each other, and have no registers for it.
+    constexpr bool AHEAD = NW < 16;
     Piece<T> dyr[VPT], hr[VPT], er[VPT];
     float rstd_r;
     auto load = [&](int64_t m) {
@@ -309,9 +315,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
     int par = 0;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     int64_t m = (int64_t)blockIdx.x * ROWS + (NW == 1 ? wave : 0);
-    load(m);
+    if (AHEAD) load(m);
     for (; m < a.M; m += step, par ^= 1) {
         float dy[VPT][CH], xh[VPT][CH], r[VPT][CH];
+        if (!AHEAD) load(m);
         const float rstd = rstd_r;
         float s = 0.f;
 #pragma unroll
@@ -321,7 +328,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
             piece_values<T, WHOLE>(hr[i], c, D, xh[i]);
             piece_values<T, WHOLE>(er[i], c, D, r[i]);
         }
-        load(m + step);
+        if (AHEAD) load(m + step);
 #pragma unroll
         for (int i = 0; i < VPT; i++)
 #pragma unroll
@@ -529,6 +536,8 @@ hipError_t run_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
 
 // Workgroups of the backward pass, which is also the number of partial rows.
 int64_t bwd_parts(int64_t M, int64_t D) {
+    // A few rows go by one workgroup, whose sums are dgain: a second launch takes longer than its rows.
+    if (M <= (pieces(D) <= 128 ? 8 : 4)) return M > 0 ? 1 : 0;
     const int64_t units = pieces(D) <= 128 ? (M + 3) / 4 : M;
     return units < kMaxParts ? units : kMaxParts;
 }
@@ -591,16 +600,17 @@ niti_status niti_rmsnorm_bwd(const void* dy, int64_t lddy, const void* h, int64_
         if (bad_ld(M > 1 ? lddy : D, D, false) || bad_ld(M > 1 ? ldh : D, D, false) ||
             (dh && bad_ld(M > 1 ? lddh : D, D, false)) || bad_ld(M > 1 ? lddx : D, D, true))
             return NITI_ERR_SHAPE;
-        if (dgain && (!ws || ws_bytes < rmsnorm_bwd_workspace(M, D))) return NITI_ERR_WORKSPACE;
-        if (dgain && ((uintptr_t)ws & 3)) return NITI_ERR_ARG;
+        const size_t need = dgain ? rmsnorm_bwd_workspace(M, D) : 0;
+        if (need > 0 && (!ws || ws_bytes < need)) return NITI_ERR_WORKSPACE;
+        if (need > 0 && ((uintptr_t)ws & 3)) return NITI_ERR_ARG;
     }
     const int64_t parts = bwd_parts(M, D);
     hipStream_t s = (hipStream_t)stream;
     if (M > 0) {
-        RowBwdArgs a{dy, h, gain, rstd, dh, dx, dgain ? (float*)ws : nullptr, lddy, ldh, lddh, lddx, M, D, gain_type};
+        RowBwdArgs a{dy, h, gain, rstd, dh, dx, !dgain ? nullptr : (parts == 1 ? dgain : (float*)ws), lddy, ldh, lddh, lddx, M, D, gain_type};
         if (by_type(type, [&](auto t) { return run_bwd<decltype(t)>(a, parts, s); }) != hipSuccess) return NITI_ERR_HIP;
     }
-    if (dgain) {   // no rows: zeros
+    if (dgain && parts != 1) {   // no rows: zeros
         hipLaunchKernelGGL(dgain_kernel, dim3((unsigned)((D + 31) / 32)), dim3(1024), 0, s, (const float*)ws, dgain, parts, D);
         if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
     }

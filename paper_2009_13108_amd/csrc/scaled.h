@@ -182,6 +182,19 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0C);
     return lo | hi;
 }
+// Consecutive draws idx, idx + 1, ... of sr_draw: its first product is carried as a sum.
+struct DrawStream {
+    uint64_t z;
+    __device__ __forceinline__ DrawStream(uint64_t seed, uint32_t call, uint64_t idx)
+        : z(seed + ((((uint64_t)call) << 40) + idx) * 0x9E3779B97F4A7C15ull) {}
+    __device__ __forceinline__ uint64_t next() {
+        z += 0x9E3779B97F4A7C15ull;
+        uint64_t x = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+        x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+        return x ^ (x >> 31);
+    }
+};
+
 // Uniform fractions of 24 bits from a draw.
 __device__ __forceinline__ float draw_hi(uint64_t r) { return (float)(uint32_t)(r >> 40) * 0x1p-24f; }
 __device__ __forceinline__ float draw_lo(uint64_t r) { return (float)((uint32_t)(r >> 8) & 0xFFFFFFu) * 0x1p-24f; }
