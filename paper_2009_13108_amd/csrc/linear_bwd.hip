@@ -65,9 +65,8 @@ struct DzRows {
 #pragma unroll
             for (int i = 0; i < ROWS; i++) {
                 const int64_t r = min(m + i * step, a.M - 1);
-                const T* dy = (const T*)a.dy + r * a.lddy;
-                y[i] = load_piece<T, KIND == 2>(dy, c, (int)a.N);
-                z[i] = load_piece<T, KIND == 2>(a.act != NITI_ACT_NONE ? (const T*)a.z + r * a.ldz : dy, c, (int)a.N);
+                y[i] = load_piece<T, KIND == 2>((const T*)a.dy + r * a.lddy, c, (int)a.N);
+                z[i] = load_piece<T, KIND == 2>((const T*)a.z + r * a.ldz, c, (int)a.N);
             }
         }
     }
@@ -111,7 +110,7 @@ template <typename T, int KIND>
 __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     __shared__ float ssum[8][SC + 8];
     __shared__ uint32_t smax[8][SC + 8];
-    const int64_t tm = blockIdx.x / a.tiles_n, tn = blockIdx.x % a.tiles_n;
+    const int64_t tm = blockIdx.x / (uint32_t)a.tiles_n, tn = blockIdx.x % (uint32_t)a.tiles_n;
     const int col = (threadIdx.x & 31) * CH, grp = threadIdx.x >> 5;
     const int c = (int)(tn * SC + col);
     DzRows<T, KIND, SR / 8> rows;
@@ -242,7 +241,7 @@ struct Turn {
 };
 
 __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*tile)[CP]) {
-    const int64_t r0 = (int64_t)(block / a.tiles_k) * CT, k0 = (int64_t)(block % a.tiles_k) * CT;
+    const int64_t r0 = (int64_t)((uint32_t)block / (uint32_t)a.tiles_k) * CT, k0 = (int64_t)((uint32_t)block % (uint32_t)a.tiles_k) * CT;
     const int pc = (threadIdx.x & 15) * 8, row = (threadIdx.x >> 4) * 4;   // four rows of 8 bytes a thread
     uint64_t v[4];
     const int64_t k = k0 + pc;
@@ -280,21 +279,17 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
 
 // Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
 template <typename T, int KIND>
-__global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int tiles_c) {
+__global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int codes, int tiles_c) {
     __shared__ __attribute__((aligned(16))) int8_t tile[CT][CP];
     __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[CT];
     int block = blockIdx.x;
-    if (block < ta.blocks) {
-        turn_tile(ta, block, tile);
+    if (block >= codes) {   // the codes' tiles, which take longest, are first
+        block -= codes;
+        if (block < ta.blocks) turn_tile(ta, block, tile);
+        else turn_tile(tb, block - ta.blocks, tile);
         return;
     }
-    block -= ta.blocks;
-    if (block < tb.blocks) {
-        turn_tile(tb, block, tile);
-        return;
-    }
-    block -= tb.blocks;
-    const int64_t m0 = (int64_t)(block / tiles_c) * CT, n0 = (int64_t)(block % tiles_c) * CT;
+    const int64_t m0 = (int64_t)((uint32_t)block / (uint32_t)tiles_c) * CT, n0 = (int64_t)((uint32_t)block % (uint32_t)tiles_c) * CT;
     const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 4;   // 8 columns of 4 rows a thread
     const int c = (int)(n0 + col);
     float sb[CH], ci[CH], sa[4];
@@ -408,7 +403,7 @@ template <typename T>
 hipError_t run_codes(const DzArgs& a, const Turn& ta, const Turn& tb, int64_t tiles, int tiles_c, hipStream_t stream) {
     return by_kind(a.N, [&](auto k) {
         hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(CTH), 0,
-                           stream, a, ta, tb, tiles_c);
+                           stream, a, ta, tb, (int)tiles, tiles_c);
         return hipGetLastError();
     });
 }
@@ -503,8 +498,9 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     if (!da && !db && !dbias) return NITI_OK;
     char* base = (char*)ws;
     DzArgs d{};
-    d.dy = dy, d.z = z, d.s_a = s_a, d.s_b = s_b;
-    d.lddy = lddy, d.ldz = ldz;
+    // without an activation dy stands for z, so that the kernels' loads need no branch
+    d.dy = dy, d.z = act != NITI_ACT_NONE ? z : dy, d.s_a = s_a, d.s_b = s_b;
+    d.lddy = lddy, d.ldz = act != NITI_ACT_NONE ? ldz : lddy;
     d.M = M, d.N = N, d.Mp = w.Mp, d.Np = w.Np;
     d.a_step = s_a_n == 1 ? 0 : 1, d.b_step = s_b_n == 1 ? 0 : 1;
     d.act = act, d.sr = mode == NITI_ROUND_SR, d.seed = seed, d.call = call;
