@@ -404,8 +404,9 @@ niti_status niti_quantize_rows(const void *x, int64_t ldx, int8_t *q, int64_t ld
  * and out may be res.  K in 0..131071 (longer sums could leave 32 bits:
  * NITI_ERR_UNSUPPORTED).  Workspace: niti_workspace_bytes(NITI_OP_LINEAR_FWD,
  * NULL, M, N, K), 0 for most sizes; without it (NULL and 0 bytes, or fewer than
- * that) the call takes longer where the products are few and the sum is long:
- * parts of the sum are then not formed side by side. */
+ * that) the call takes longer where the products are few and the sum is long
+ * (parts of the sum are then not formed side by side) and where K is no
+ * multiple of 16 (large operands are then not copied to whole pieces first). */
 niti_status niti_linear_fwd(const int8_t *a, int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b,
                             int64_t ldb, const float *s_b, int64_t s_b_n, const void *bias, int bias_type, int act,
                             const void *res, int64_t ldres, void *z, int64_t ldz, void *out, int64_t ldout, int64_t M,

@@ -792,8 +792,12 @@ struct Cost {
 constexpr Cost kSmall11{16, 16, kSpread, 1.93f, 0.56f, 0.58f, 0.81f};
 constexpr Cost kSmall12{16, 32, kSpread, 1.92f, 0.61f, 0.95f, 1.33f};
 constexpr Cost kSmall22{32, 32, kSpread, 2.06f, 0.75f, 1.18f, 1.90f};
+// Rows at odd addresses, from 200 random products, 2.6% from the fastest in the mean; 5.8% without the copies below.
+constexpr Cost kBytes11{16, 16, kSpread, 1.88f, 0.64f, 0.78f, 1.73f};
+constexpr Cost kBytes12{16, 32, kSpread, 2.01f, 0.59f, 1.23f, 2.45f};
+constexpr Cost kBytes22{32, 32, kSpread, 2.02f, 0.86f, 1.39f, 3.48f};
 constexpr Cost kRing64{64, 64, kTwo, 2.09f, 1.02f, 0.32f, 2.21f};
-constexpr Cost kAny64{64, 64, kTwo, 2.6f, 1.5f, 0.4f, 2.8f};   // 1.3 times the ring's: 1000 x 1500 x 1111 11.4 us, 1000 x 1504 x 1104 8.6
+constexpr Cost kAny64{64, 64, kSpread, 2.84f, 1.02f, 3.38f, 4.07f};
 constexpr Cost kRing128{128, 128, kTwo, 0.96f, 3.17f, 3.79f, 3.45f};
 constexpr Cost kDeep128{128, 128, kRounds, 0.12f, 4.49f, 3.72f, 2.33f};
 constexpr Cost kRing256{256, 256, kRounds, 0.41f, 11.1f, 9.31f, 5.98f};
@@ -811,19 +815,32 @@ struct Choice {
     int parts;       // of the sum
     int64_t klen;    // products of a part, whole steps
     float time;
+    bool pack;       // the operands are copied to whole aligned pieces first
 };
+
+inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+// Copies of both operands, where K leaves their rows no whole pieces (whole rows at odd
+// strides go without: the workspace is sized before strides are known); less than 2^32 pieces.
+constexpr int64_t kPackBytes = (int64_t)1 << 34;
+inline size_t pack_bytes(int64_t M, int64_t N, int64_t K) {
+    const int64_t Kp = up16(K);
+    return K < 16 || K % 16 == 0 || M > kPackBytes / Kp || N > kPackBytes / Kp ? 0 : (size_t)((M + N) * Kp + 255) / 256 * 256;
+}
 
 constexpr int64_t kPartLen = 512;   // least products of a part
 inline int64_t part_ld(int64_t N) { return (N + 7) / 8 * 8; }
 
-// whole: the operands are whole aligned pieces; room: bytes for the sums of parts.
-Choice choose(int64_t M, int64_t N, int64_t K, bool whole, size_t room) {
-    Choice c{Choice::kS11, 1, 0, cost(kSmall11, M, N, K)};
+// rows: what the operands' rows are made of, aligned; room: bytes of workspace.
+enum Rows { kOfBytes, kOfWords, kOfPieces };
+
+Choice choose(int64_t M, int64_t N, int64_t K, Rows rows, size_t room) {
+    const bool whole = rows == kOfPieces, words = rows != kOfBytes;
+    Choice c{Choice::kS11, 1, 0, cost(words ? kSmall11 : kBytes11, M, N, K), false};
     auto take = [&](decltype(c.kernel) kernel, float time, int parts, int64_t klen) {
-        if (time < c.time) c = Choice{kernel, parts, klen, time};
+        if (time < c.time) c = Choice{kernel, parts, klen, time, false};
     };
-    take(Choice::kS12, cost(kSmall12, M, N, K), 1, 0);
-    take(Choice::kS22, cost(kSmall22, M, N, K), 1, 0);
+    take(Choice::kS12, cost(words ? kSmall12 : kBytes12, M, N, K), 1, 0);
+    take(Choice::kS22, cost(words ? kSmall22 : kBytes22, M, N, K), 1, 0);
     const Cost& tile = whole ? kRing64 : kAny64;
     take(Choice::k64, cost(tile, M, N, K), 1, 0);
     if (whole) {
@@ -840,7 +857,26 @@ Choice choose(int64_t M, int64_t N, int64_t K, bool whole, size_t room) {
         if (bytes > (double)room) break;
         take(Choice::k64, cost(tile, M, N, klen * parts, parts) + 2.3f + (float)(bytes * 2. / 4e6), parts, klen);
     }
+    // Rows at odd addresses: a launch that copies them to whole pieces, and the kernels for
+    // those (4096 x 4096 x 4097: 215 -> 92 us, 2000 x 2000 x 1111: 20 -> 17).
+    const size_t copies = whole ? 0 : pack_bytes(M, N, K);
+    if (copies > 0 && copies <= room) {
+        Choice p = choose(M, N, up16(K), kOfPieces, room - copies);
+        p.time += 2.3f + (float)((double)copies * 2. / 3e6);   // (3 TB/s)
+        p.pack = true;
+        if (p.time < c.time) c = p;
+    }
     return c;
+}
+
+// Both operands' rows, at any addresses, to rows of Kp = ppr * 16 bytes, a's and then b's; zeros past K.
+__global__ __launch_bounds__(256) void linear_pack_kernel(LinArgs A, uint32_t ppr, uint32_t pieces, int8_t* out) {
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= pieces) return;
+    const int64_t r = i / ppr;
+    const int k = (int)(i % ppr) * 16, K = (int)A.K;
+    const int8_t* row = r < A.M ? A.a + r * A.lda : A.b + (r - A.M) * A.ldb;
+    *(v4i*)(out + (int64_t)i * 16) = cut_piece(__builtin_bit_cast(v4i, load16_any(row + min(k, K - 16))), k, K);
 }
 
 template <typename T>
@@ -854,7 +890,19 @@ hipError_t run_linear(LinArgs A, void* ws, size_t ws_bytes, hipStream_t stream) 
     A.res_dma = A.res && ld % 16 == 0 && ((uintptr_t)A.res & 15) == 0 && ld < ((int64_t)1 << 22);
     A.klen = 0;
     const bool whole = ring_takes(A);
-    const Choice c = choose(A.M, A.N, A.K, whole, ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0);
+    const Choice c = choose(A.M, A.N, A.K, whole ? kOfPieces : (word_rows(A) ? kOfWords : kOfBytes), ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0);
+    if (c.pack) {
+        const int64_t Kp = up16(A.K);
+        const uint32_t ppr = (uint32_t)(Kp / 16), pieces = (uint32_t)(A.M + A.N) * ppr;
+        hipLaunchKernelGGL(linear_pack_kernel, dim3((pieces + 255) / 256), dim3(256), 0, stream, A, ppr, pieces, (int8_t*)ws);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        LinArgs P = A;
+        P.a = (const int8_t*)ws, P.b = P.a + A.M * Kp;
+        P.lda = P.ldb = P.K = Kp;
+        const size_t copies = pack_bytes(A.M, A.N, A.K);
+        return run_linear<T>(P, (char*)ws + copies, ws_bytes - copies, stream);
+    }
     if (c.parts > 1) {
         LinArgs P = A;   // sums only
         P.s_a = P.s_b = nullptr;
@@ -914,7 +962,7 @@ constexpr float kLaunch = 2.5f;   // us that a second launch takes at least
 hipError_t linear_run_pair(const LinArgs& a, const LinArgs& b, int type, void* ws, size_t ws_bytes, hipStream_t stream) {
     const bool whole = ring_takes(a) && ring_takes(b) && !a.res && !b.res && a.M < kMaxSum && b.M < kMaxSum;
     if (whole) {
-        const Choice ca = choose(a.M, a.N, a.K, true, ws_bytes), cb = choose(b.M, b.N, b.K, true, ws_bytes);
+        const Choice ca = choose(a.M, a.N, a.K, kOfPieces, ws_bytes), cb = choose(b.M, b.N, b.K, kOfPieces, ws_bytes);
         const Choice& c = ca.time > cb.time ? ca : cb;
         const bool small_a = ca.parts == 1 && ca.kernel <= Choice::kS22, small_b = cb.parts == 1 && cb.kernel <= Choice::kS22;
         if (small_a && small_b) {
@@ -932,13 +980,13 @@ hipError_t linear_run_pair(const LinArgs& a, const LinArgs& b, int type, void* w
     return e == hipSuccess ? linear_run(b, type, ws, ws_bytes, stream) : e;
 }
 
-// For the sums of parts, if that is how this product would go with room for them.
+// For copies of the operands and the sums of parts, if that is how this product would go with room for them.
 size_t linear_fwd_workspace(int64_t M, int64_t N, int64_t K) {
     if (M < 1 || N < 1 || K < 1 || M >= kMaxDim || N >= kMaxLd || K >= kMaxSum) return 0;
     size_t most = 0;
-    for (int whole = 0; whole < 2; whole++) {
-        const Choice c = choose(M, N, K, whole != 0, SIZE_MAX);
-        const size_t need = c.parts > 1 ? (size_t)c.parts * (size_t)(M * part_ld(N)) * 4 : 0;
+    for (Rows rows : {kOfBytes, kOfWords, kOfPieces}) {
+        const Choice c = choose(M, N, K, rows, SIZE_MAX);
+        const size_t need = (c.parts > 1 ? (size_t)c.parts * (size_t)(M * part_ld(N)) * 4 : 0) + (c.pack ? pack_bytes(M, N, K) : 0);
         most = need > most ? need : most;
     }
     return (most + 255) / 256 * 256;

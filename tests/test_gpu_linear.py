@@ -100,6 +100,16 @@ def test_forward_long_sums(m, n, k):
     run_forward(m, n, k, F32, ws=False)
 
 
+@pytest.mark.parametrize("m,n,k,pad", [(4000, 1500, 17, (5, 0)), (1500, 1600, 1803, (0, 16)), (900, 3001, 1999, (1, 3)),
+                                       (1030, 2050, 4001, (0, 0))])
+def test_forward_copied_rows(m, n, k, pad):
+    """Rows at odd addresses that are copied to the workspace first, and the same product without one."""
+    say("linear_fwd copied", m, n, k, pad)
+    assert niti.workspace_bytes(niti.OP_LINEAR_FWD, None, m, n, k) >= (m + n) * k
+    for dtype, ws in ((F32, True), (BF16, True), (F32, False)):
+        run_forward(m, n, k, dtype, act="silu", pad=pad, ws=ws)
+
+
 @pytest.mark.parametrize("m,n", [(1, 3), (20, 40), (140, 130)])
 def test_forward_largest_sum(m, n):
     """131071 products of -128 * -128 and -128 * 127: the ends of what int32 holds, exactly."""
