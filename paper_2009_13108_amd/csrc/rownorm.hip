@@ -285,14 +285,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = NW == 1 ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     const int D = (int)a.D;
-    float g[VPT][CH], dg[VPT][CH];
+    Piece<TG> pg[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; i++) {
-        const int c = (i * NT + t) * CH;
-        piece_values<TG, WHOLE>(load_piece<TG, WHOLE>((const TG*)a.gain, c, D), c, D, g[i]);
-#pragma unroll
-        for (int e = 0; e < CH; e++) dg[i][e] = 0.f;
-    }
+    for (int i = 0; i < VPT; i++) pg[i] = load_piece<TG, WHOLE>((const TG*)a.gain, (i * NT + t) * CH, D);
     // A row's loads go out while the row before it is worked on (past the last row, that one's again);
     // sixteen waves hide them for each other, and have no registers for it.
     constexpr bool AHEAD = NW < 16;
@@ -315,7 +310,15 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_bwd_kernel(RowBwd
     int par = 0;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     int64_t m = (int64_t)blockIdx.x * ROWS + (NW == 1 ? wave : 0);
+    if (NW > 1) __builtin_assume(m < a.M);   // (no more workgroups than rows: the first row's loads do not wait for the gain's)
     if (AHEAD) load(m);
+    float g[VPT][CH], dg[VPT][CH];
+#pragma unroll
+    for (int i = 0; i < VPT; i++) {
+        piece_values<TG, WHOLE>(pg[i], (i * NT + t) * CH, D, g[i]);
+#pragma unroll
+        for (int e = 0; e < CH; e++) dg[i][e] = 0.f;
+    }
     for (; m < a.M; m += step, par ^= 1) {
         float dy[VPT][CH], xh[VPT][CH], r[VPT][CH];
         if (!AHEAD) load(m);
