@@ -5,6 +5,15 @@
 // The sum is exact in int32 (int8 MFMA); everything after it is in 32-bit
 // floats, rounded once at the store.  The epilogue runs in the kernel that
 // forms the sum: z, the activation and the residual cost no pass of their own.
+//
+// Four kinds of kernel.  Whole aligned pieces: LDS rings of 64 x 64, 128 x 128 or
+// 256 x 256 tiles.  Any addresses: 64 x 64 tiles through registers, or rows copied to
+// whole pieces first.  Few products: small tiles straight from memory.  Long
+// sums of few products: parts side by side in the workspace.
+//
+// Measured: 8192 x 8192 x 8192 to bf16 491 us, 2.24 POPS, bound by power (the clock falls
+// to 1.7 GHz with the MFMAs busy 69% of it); one token by 4096 x 4096 6.0 us, 2.8 TB/s of
+// weights; 1000 x 1500 x 1111 in 32 bits with every operand 15.
 #include "linear.h"
 
 #include <math.h>
@@ -523,6 +532,8 @@ hipError_t run_small(const LinArgs& A, hipStream_t stream) {
 // ---------------------------------------------------------------- ring
 // Tiles of BM x BN from an LDS ring of NS stages of KS bytes a row, filled by
 // direct-to-LDS loads.  Needs K, strides and addresses in whole 16 bytes.
+// 256 x 256 tiles read the least from L2 and LDS for a product (4096 x 4096 x 2048 38.5 us,
+// 1.8 POPS), smaller ones give more CUs work (2048 x 4096 x 4096 by 128 x 128 38.1).
 constexpr uint32_t kOut = 0x80000000u;   // an offset past any tile: loads zeros
 
 template <int N>
