@@ -320,10 +320,14 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
             if (a.join) {
                 float s = 0.f;
                 uint32_t mx = 0;
+                // up to 32 tiles, in step 2's order: the 16 groups' sums one after the other
+                const int groups = (int)min((int64_t)16, a.tiles_m);
 #pragma unroll 8
-                for (int64_t t = 0; t < a.tiles_m; t++) {
-                    s += a.csum[t * a.N + n];
-                    mx = max(mx, a.cmax[t * a.N + n]);
+                for (int g = 0; g < groups; g++) {
+                    const int64_t two = min((int64_t)g + 16, a.tiles_m - 1);
+                    const float x = a.csum[g * a.N + n], y = a.csum[two * a.N + n];
+                    s += g + 16 < a.tiles_m ? x + y : x;
+                    mx = max(mx, max(a.cmax[g * a.N + n], a.cmax[two * a.N + n]));
                 }
                 const RowScale rs = row_scale(mx);
                 if (m0 == 0 && n0 + i < a.N) {
@@ -518,9 +522,9 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.cmax = (uint32_t*)(base + w.cmax);
     d.csum = (float*)(base + w.csum);
     if (by_type(type, [&](auto t) { return run_stats<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
-    // Tiles of step 3 read those of step 1 that they lie in, each again: up to 16 by 40 of them (256 x 10240) that takes
-    // less than a launch (250 x 4096 x 512 29.2 -> 26.9 us, 200 x 9000 x 1024 45.6 -> 43.5).
-    d.join = (da || db) && w.tiles_m <= 16 && w.tiles_n <= 40;
+    // Tiles of step 3 read those of step 1 that they lie in, each again: up to 32 by 40 of them (512 x 10240) that takes
+    // less than a launch (250 x 4096 x 512 29.2 -> 26.9 us, 200 x 9000 x 1024 45.6 -> 43.5, 400 x 1024 x 512 21.3 -> 19.5).
+    d.join = (da || db) && w.tiles_m <= 32 && w.tiles_n <= 40;
     if (!d.join) {
         const int64_t cols = (N + 63) / 64;
         hipLaunchKernelGGL(dz_join_kernel, dim3((unsigned)(cols + (M + 1023) / 1024)), dim3(1024), 0, s, d, (int)cols);

@@ -220,7 +220,8 @@ def backward64(dy, z, act, a, b, s_a, s_b, u=None, v=None):
 @pytest.mark.parametrize("m,n,k,act,mode", [
     (1, 1, 1, "none", "rtn"), (1, 300, 200, "silu", "sr"), (5, 33, 17, "gelu", "rtn"), (64, 64, 64, "relu", "sr"),
     (100, 257, 130, "silu", "rtn"), (129, 1000, 784, "gelu", "sr"), (700, 128, 256, "none", "sr"), (1100, 600, 96, "silu", "rtn"),
-    (31, 2050, 64, "relu", "rtn"), (40, 4100, 48, "none", "rtn"), (20, 17000, 40, "silu", "sr"), (513, 512, 512, "gelu", "rtn")])
+    (31, 2050, 64, "relu", "rtn"), (40, 4100, 48, "none", "rtn"), (20, 17000, 40, "silu", "sr"), (513, 512, 512, "gelu", "rtn"), (270, 530, 96, "silu", "rtn"),
+    (500, 136, 64, "relu", "sr")])
 def test_backward(m, n, k, act, mode, dtype):
     say("linear_bwd", m, n, k, act, mode, dtype)
     a, b = codes(m, k, 1, pad=k % 3), codes(n, k, 2)
