@@ -544,9 +544,11 @@ hipError_t run_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
 
 // Workgroups of the backward pass, which is also the number of partial rows.
 int64_t bwd_parts(int64_t M, int64_t D) {
-    // A few rows go by one workgroup, whose sums are dgain: a second launch takes longer than its rows.
-    if (M <= (pieces(D) <= 128 ? 8 : 4)) return M > 0 ? 1 : 0;
-    const int64_t units = pieces(D) <= 128 ? (M + 3) / 4 : M;
+    // A few rows go by one workgroup, whose sums are dgain and which saves the second launch.  One
+    // launch and two (us): 16 rows of 1000 6.5, 6.7, 32 9.6, 6.6; 4 rows of 4096 7.1, 6.9, 8 10.8, 7.0; 4 of 9216 10.5, 8.1.
+    const int p = pieces(D), few = p <= 128 ? 16 : (p <= 512 ? 4 : 2);
+    if (M <= few) return M > 0 ? 1 : 0;
+    const int64_t units = p <= 128 ? (M + 3) / 4 : M;
     return units < kMaxParts ? units : kMaxParts;
 }
 
