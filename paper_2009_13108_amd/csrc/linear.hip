@@ -129,8 +129,10 @@ __device__ __forceinline__ void epilogue(const LinArgs& A, v16i (&acc)[BN / WGN 
         for (int kind = A.z ? 0 : 1; kind < 2; kind++) {   // z, then out
             const bool add = kind == 1 && A.res;
             if (add && A.res_dma) {
+                // The descriptor's range is checked by 32-bit words, and a word that it cuts loads zeros: it ends after
+                // the word that holds the last element (the residual's address is a multiple of 16).
                 const u32x4 rs = raw_rsrc((const T*)A.res + m0 * A.ldres + n0,
-                                          (uint32_t)(((int64_t)(rows - 1) * A.ldres + ncol) * (int64_t)sizeof(T)));
+                                          (uint32_t)(((int64_t)(rows - 1) * A.ldres + ncol) * (int64_t)sizeof(T) + 3) & ~3u);
                 const uint32_t base = lds_address(lds);
 #pragma unroll 4
                 for (int i = 0; i < S::PIECES / S::NT; i++) {
