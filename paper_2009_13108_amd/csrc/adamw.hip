@@ -92,7 +92,18 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top_bits, float unit)
 }
 
 // Square roots and reciprocals are the hardware's, good to one unit in the last
-// place; the IEEE sequences around them took as long as the memory traffic.
+// place; the IEEE sequences around them took as long as the memory traffic.  They
+// take a value below the normal range for zero, so m / (sqrt(v) root + eps) scales small
+// ones up by powers of two, which is exact: gradients below 1e-17 have such v, and with eps = 0
+// nothing else is in the divisor.  (The codes' roots need no such care: what is that
+// much smaller than its block's largest has code 0, or 1, either way.)
+__device__ __forceinline__ float root_ratio(float m, float v, float root, float eps) {
+    const bool low = v < 0x1p-100f;
+    const float d = __builtin_amdgcn_sqrtf(low ? v * 0x1p60f : v) * (low ? 0x1p-30f : 1.f) * root + eps;
+    const bool tiny = d < 0x1p-60f;
+    const float r = __builtin_amdgcn_rcpf(tiny ? d * 0x1p64f : d);
+    return m * r * (tiny ? 0x1p64f : 1.f);
+}
 constexpr float kUnitM = 1.f / 16129.f;                       // 1 / 127^2
 constexpr float kUnitV = 1.f / (255.f * 255.f * 255.f * 255.f);   // 1 / 255^4
 
@@ -134,7 +145,7 @@ __device__ __forceinline__ void adamw_elements(const Entry& E, const Step& S, in
         const float x = g[e] * gs;
         m[e] = S.b1 * m[e] + S.c1 * x;
         v[e] = S.b2 * v[e] + S.c2 * (x * x);
-        p[e] = p[e] * S.keep - S.lr * (m[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) * S.root + S.eps));
+        p[e] = p[e] * S.keep - S.lr * root_ratio(m[e], v[e], S.root, S.eps);
     }
     store_some((TP*)E.p + i, n, p);
     if constexpr (BITS == 32) {
