@@ -213,14 +213,17 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
 __device__ __forceinline__ float exp_mid(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float sigmoid_mid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_mid(-x)); }
 
-// The normal distribution function at z, |z| <= 12.5, from e = exp(-z^2 / 2): about 0
+__device__ __forceinline__ float half_exp(float s) { return __builtin_amdgcn_exp2f(s * (-0.5f * 1.44269504088896341f)); }   // exp(-s / 2)
+
+// The normal distribution function at z >= -12.5 from s = z^2 and e = exp(-s / 2): about 0
 // it is 1/2 + z P(z^2), beyond that the tail outside |z| is e Q(t) with t = 1 / (1 + 0.4 |z|),
 // which keeps its relative error however small it is.  P and Q are fitted in 64
 // bits for the least largest error: P within 2.1e-9 of the function for |z| < 1.25, Q within 9e-9
 // of the tail, relative, from there to 12.5.  In 32 bits GELU is then nowhere further from
 // its exact value than z (1 + erf(z / sqrt 2)) / 2 is, which loses the tail of negative z.
-__device__ __forceinline__ float normal_cdf(float z, float e) {
-    const float s = z * z;
+// A five-term error function costs less (4096 x 4096 x 512 to bf16 39.9 us for 42.5, 1000 x 1500 x 1111
+// in 32 bits 15.4 for 15.5) and was up to 1e-2 of the value off there.
+__device__ __forceinline__ float normal_cdf(float z, float s, float e) {
     float p = __builtin_fmaf(s, -6.66287769e-06f, 0.000110409092f);
     p = __builtin_fmaf(s, p, -0.00118284649f);
     p = __builtin_fmaf(s, p, 0.00997160375f);
@@ -244,8 +247,8 @@ __device__ __forceinline__ float normal_cdf(float z, float e) {
 __device__ __forceinline__ float act_value(int act, float z) {
     if (act == NITI_ACT_RELU) return z < 0.f ? 0.f : z;
     if (act == NITI_ACT_GELU) {
-        const float c = z < -12.5f ? -12.5f : z, d = c > 12.5f ? 12.5f : c;
-        return c * normal_cdf(d, exp_mid(-0.5f * d * d));
+        const float c = z < -12.5f ? -12.5f : z;   // (upwards the tail ends at 0 by itself)
+        return c * normal_cdf(c, c * c, half_exp(c * c));
     }
     if (act == NITI_ACT_SILU) {
         const float c = z < -80.f ? -80.f : z;
@@ -257,8 +260,8 @@ __device__ __forceinline__ float act_slope(int act, float z) {
     if (act == NITI_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
     if (act == NITI_ACT_GELU) {
         const float c = z < -12.5f ? -12.5f : (z > 12.5f ? 12.5f : z);
-        const float e = exp_mid(-0.5f * c * c);
-        return normal_cdf(c, e) + c * e * 0.39894228040143268f;
+        const float e = half_exp(c * c);
+        return normal_cdf(c, c * c, e) + c * e * 0.39894228040143268f;
     }
     if (act == NITI_ACT_SILU) {
         const float c = z < -80.f ? -80.f : (z > 80.f ? 80.f : z);
