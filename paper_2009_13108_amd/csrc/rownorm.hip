@@ -71,9 +71,14 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* red, int wave)
     return v;
 }
 
-// Values above 2^64 or so leave the 32-bit range when squared: such a row is
-// summed again with its elements scaled down by 2^-80.
-constexpr float kDown = 0x1p-80f;
+// Squares of values above 2^64 or so leave the 32-bit range, and those of values
+// below 2^-50 its normal part: where the mean of the squares and eps, the smaller of
+// which is then lost or inexact, is that large or small, the row is summed again with its elements
+// scaled by a power of two (exact), and eps by its square.
+constexpr float kDown = 0x1p-80f, kUp = 0x1p100f, kLow = 0x1p-100f;
+__device__ __forceinline__ float norm_factor(float ss, float D, float eps) {
+    return !(ss < __uint_as_float(kInfBits)) ? kDown : (ss + eps * D < kLow * D ? kUp : 1.f);
+}
 
 __device__ __forceinline__ void store_codes(int8_t* q, int n, const float (&c)[CH], uint32_t mask) {
     uint32_t w[2] = {pack4(c[0], c[1], c[2], c[3]) & mask, pack4(c[4], c[5], c[6], c[7]) & mask};
@@ -154,15 +159,15 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void row_fwd_kernel(RowArg
             }
         }
         ss = row_sum<NW>(ss, red_s, wave);
-        float down = 1.f, eps = a.eps;
-        if (!(ss < __uint_as_float(kInfBits))) {   // the same for the whole row
-            down = kDown;
-            eps = 0.f;   // eps 2^-160, far below the sum
+        float eps = a.eps;
+        const float down = norm_factor(ss, (float)D, eps);   // the same for the whole row
+        if (down != 1.f) {
+            eps = eps * down * down;
             ss = 0.f;
 #pragma unroll
             for (int i = 0; i < VPT; i++)
 #pragma unroll
-                for (int e = 0; e < CH; e++) ss += (v[i][e] * kDown) * (v[i][e] * kDown);
+                for (int e = 0; e < CH; e++) ss += (v[i][e] * down) * (v[i][e] * down);
             ss = row_sum<NW>(ss, red_t, wave);
         }
         const float rstd = 1.f / sqrtf(ss / (float)D + eps);
@@ -215,23 +220,21 @@ __global__ __launch_bounds__(NT_LONG) void row_fwd_long_kernel(RowArgs a) {
     };
     float down = 1.f, rstd = 1.f;
     if constexpr (NORM) {
-        float s = 0.f, sd = 0.f;
-        for (int64_t c = threadIdx.x * CH; c < a.D; c += NT_LONG * CH) {
-            float v[CH];
-            load(c, v);
+        auto squares = [&](float factor) {
+            float s = 0.f;
+            for (int64_t c = threadIdx.x * CH; c < a.D; c += NT_LONG * CH) {
+                float v[CH];
+                load(c, v);
 #pragma unroll
-            for (int e = 0; e < CH; e++) {
-                s += v[e] * v[e];
-                sd += (v[e] * kDown) * (v[e] * kDown);
+                for (int e = 0; e < CH; e++) s += (v[e] * factor) * (v[e] * factor);
             }
-        }
-        s = row_sum<NW>(s, red_s, wave);
-        sd = row_sum<NW>(sd, red_t, wave);
-        float eps = a.eps;
-        if (!(s < __uint_as_float(kInfBits))) {
-            down = kDown;
-            eps = 0.f;
-            s = sd;
+            return s;
+        };
+        float s = row_sum<NW>(squares(1.f), red_s, wave), eps = a.eps;
+        down = norm_factor(s, (float)a.D, eps);
+        if (down != 1.f) {
+            eps = eps * down * down;
+            s = row_sum<NW>(squares(down), red_t, wave);
         }
         rstd = 1.f / sqrtf(s / (float)a.D + eps);
         if (a.rstd && threadIdx.x == 0) a.rstd[m] = rstd * down;
