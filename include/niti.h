@@ -339,7 +339,9 @@ niti_status niti_dropout_bwd(const int8_t *dy, const uint8_t *keep, int8_t *dx, 
  *               draw number call * 2^40 + i + 1 of the SplitMix64 stream of
  *               seed, i = the element's index m * columns + n);
  *               NITI_ROUND_PSR, which reads the fraction of an integer, gives
- *               NITI_ERR_ARG.
+ *               NITI_ERR_ARG.  Calls that are to round independently take
+ *               different seeds or different `call`s; niti_adamw_step's `call`
+ *               is its step, so that it takes a seed of its own.
  *   Aliasing    An output may be one of the call's own inputs (same address,
  *               type and stride) where that is said; otherwise they must not
  *               overlap.

@@ -21,6 +21,8 @@ class FeedForward:
     def __init__(self, d, f, tokens, dtype, act=niti.ACT_SILU, state_bits=8, mode=niti.SR, seed=1, device="cuda"):
         import torch
         self.d, self.f, self.tokens, self.act, self.mode, self.seed, self.steps = d, f, tokens, act, mode, seed, 0
+        # the optimiser counts its draws by steps, the gradients by calls: under one seed they would meet
+        self.state_seed = seed ^ 1 << 63
         g = torch.Generator(device=device)
         g.manual_seed(seed)
         new = lambda *shape, t=dtype: torch.zeros(shape, dtype=t, device=device)  # noqa: E731
@@ -72,7 +74,9 @@ class FeedForward:
         return self.out
 
     def backward(self, dout):
-        """Gradients of the last forward pass; returns that of x (and of res)."""
+        """Gradients of the last forward pass; returns that of x (and of res).  Their
+        stochastic draws go by the number of steps taken: repeated before the next, it
+        gives the same again."""
         (wu, su), (wd, sd) = self.wq["up"], self.wq["down"]
         kw = dict(mode=self.mode, seed=self.seed)
         niti.linear_bwd(dout, self.uq, wd, self.us, sd, self.ws, da=self.du, db=self.dw["down"], dbias=self.dvec["bd"],
@@ -87,7 +91,7 @@ class FeedForward:
         self.steps += 1
         for plan in self.plans:
             niti.adamw_step(plan, self.steps, lr, weight_decay=weight_decay, grad_scale=grad_scale, mode=self.mode,
-                            seed=self.seed)
+                            seed=self.state_seed)
         self.lay_out()
 
 
