@@ -341,7 +341,9 @@ niti_status niti_dropout_bwd(const int8_t *dy, const uint8_t *keep, int8_t *dx, 
  *               NITI_ROUND_PSR, which reads the fraction of an integer, gives
  *               NITI_ERR_ARG.  Calls that are to round independently take
  *               different seeds or different `call`s; niti_adamw_step's `call`
- *               is its step, so that it takes a seed of its own.
+ *               is its step, so that it takes a seed of its own.  Seed and
+ *               `call` are the call's arguments: a captured graph repeats
+ *               its draws on every replay.
  *   Aliasing    An output may be one of the call's own inputs (same address,
  *               type and stride) where that is said; otherwise they must not
  *               overlap.
@@ -466,7 +468,9 @@ typedef struct niti_adamw_tensor {
  * 32-47 and 48-63 where it is odd.  A block of m or v with
  * a value that is not finite gets the scale NaN, and its parameters are NaN
  * from the next step on (with 32-bit states only that element's is).  step >= 1,
- * 0 <= beta < 1, eps >= 0. */
+ * 0 <= beta < 1, eps >= 0.  Step, rates and draws are arguments, and a graph
+ * would repeat that step: on a stream that is being captured the call gives
+ * NITI_ERR_UNSUPPORTED. */
 niti_status niti_adamw_step(const niti_adamw_tensor *tensors, int64_t count, int p_type, int g_type, int state_bits,
                             int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
                             const float *grad_scale, niti_round_mode mode, uint64_t seed, void *stream);

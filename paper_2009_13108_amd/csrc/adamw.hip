@@ -298,6 +298,16 @@ niti_status check_tensors(const niti_adamw_tensor* t, int64_t count, int bits) {
     return NITI_OK;
 }
 
+// The step's number, rates and draws are kernel arguments: a graph of it would take that step again and again.
+bool capturing(hipStream_t stream) {
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(stream, &st) != hipSuccess) {
+        (void)hipGetLastError();   // (the launch finds out for itself)
+        return false;
+    }
+    return st != hipStreamCaptureStatusNone;
+}
+
 template <typename TP, typename TG>
 hipError_t run_step(const niti_adamw_tensor* t, int64_t count, int bits, const Step& s, hipStream_t stream) {
     return for_tables(t, count, bits, sizeof(TP), sizeof(TG), false, s, [&](const Table& tab, unsigned grid) {
@@ -328,6 +338,7 @@ niti_status niti_adamw_step(const niti_adamw_tensor* tensors, int64_t count, int
     if (st != NITI_OK) return st;
     for (int64_t i = 0; i < count; i++)
         if (tensors[i].n > 0 && (!tensors[i].p || !tensors[i].g)) return NITI_ERR_NULL;
+    if (capturing((hipStream_t)stream)) return NITI_ERR_UNSUPPORTED;
     Step s{};
     s.b1 = (float)beta1;
     s.c1 = (float)(1 - beta1);

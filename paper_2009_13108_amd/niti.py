@@ -322,7 +322,9 @@ def stream_wait(stream, event):
 
 
 def replay(calls):
-    """Reissue recorded calls (see recording); raises on the first error."""
+    """Reissue recorded calls (see recording); raises on the first error.  The row
+    operators' stochastic calls repeat their draws, which go by the arguments
+    seed and call; those with a stats block go on by its call count."""
     for f, args, name in calls:
         st = f(*args)
         if st != 0:
@@ -836,7 +838,10 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, m_read=None, v_r
 def adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=None, mode=RTN, seed=0,
                stream=None):
     """One AdamW step (number `step`, from 1 on) of all tensors of a plan;
-    grad_scale: a float32 device scalar that multiplies the gradients."""
+    grad_scale: a float32 device scalar that multiplies the gradients.  A step
+    cannot be recorded or captured into a graph: replayed, it would stay step `step`."""
+    if _recorder is not None:
+        raise ValueError("adamw_step cannot be recorded: a replay would repeat step %d" % step)
     gs = None if grad_scale is None else _vec(grad_scale, plan.device, 1, "grad_scale", _torch_mod.float32)
     _run("niti_adamw_step", plan.table, plan.count, plan.p_type, plan.g_type, plan.bits, step, lr, beta1, beta2, eps,
          weight_decay, gs, mode, seed & 0xFFFFFFFFFFFFFFFF, _stream(stream))
