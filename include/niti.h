@@ -491,9 +491,11 @@ size_t niti_stats_bytes(void);
  *                       niti_conv_bwd_weight call (for short reductions,
  *                       which have no passes of their own, the whole call);
  *   NITI_TIMING_KERNEL  every contraction kernel launch alone (the main
- *                       implicit-GEMM or weight-gradient kernel), labelled
- *                       with the kernel and its template arguments;
- *   NITI_TIMING_SUM     the split-sum and maximum pass of a weight gradient;
+ *                       implicit-GEMM or weight-gradient kernel, the
+ *                       products of int8 rows), labelled with the kernel and
+ *                       its template arguments;
+ *   NITI_TIMING_SUM     the split-sum and maximum pass of a weight gradient,
+ *                       and the pass that joins a row product's parts;
  *   NITI_TIMING_UPDATE  the rounding and update pass of a weight gradient;
  *   NITI_TIMING_LOSS    the two launches of niti_int_ce_loss_grad.
  * niti_timing_enable(1) clears the record and starts, niti_timing_enable(0)

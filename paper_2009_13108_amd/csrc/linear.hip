@@ -346,11 +346,21 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
     epilogue<T, GT, GT, 2, 2, sizeof(lds)>(A, acc, lds[0], par, m0, n0);
 }
 
+// Timing record of a launch (NITI_TIMING_KERNEL, or the sum of parts), closed by timing_end.
+template <typename T>
+const char* type_name() { return __is_same(T, int32_t) ? "i32" : (__is_same(T, float) ? "f32" : (__is_same(T, bf16) ? "bf16" : "f16")); }
+template <typename... V>
+int time_launch(int family, hipStream_t stream, const char* fmt, V... v) {
+    return timing_on() ? timing_begin(family, stream, kernel_label(fmt, v...)) : -1;
+}
+
 template <typename T>
 hipError_t run_any(const LinArgs& A, hipStream_t stream) {
     const int64_t tm = (A.M + GT - 1) / GT, tn = (A.N + GT - 1) / GT;
     const dim3 grid((unsigned)(tm * tn), A.klen ? (unsigned)((A.K + A.klen - 1) / A.klen) : 1);
+    const int tk = time_launch(NITI_TIMING_KERNEL, stream, "linear_any_kernel<%s>", type_name<T>());
     hipLaunchKernelGGL((linear_any_kernel<T>), grid, dim3(256), 0, stream, A, (int)tn);
+    timing_end(tk, stream);
     return hipGetLastError();
 }
 
@@ -524,10 +534,13 @@ __global__ __launch_bounds__(64 * SW) void linear_small_pair_kernel(LinPair P) {
 template <typename T, int FM, int FN>
 hipError_t run_small(const LinArgs& A, hipStream_t stream) {
     const int64_t tm = (A.M + 16 * FM - 1) / (16 * FM), tn = (A.N + 16 * FN - 1) / (16 * FN);
-    if (word_rows(A))
+    const bool words = word_rows(A);
+    const int tk = time_launch(NITI_TIMING_KERNEL, stream, "linear_small_kernel<%s,%d,%d,%d>", type_name<T>(), FM, FN, !words);
+    if (words)
         hipLaunchKernelGGL((linear_small_kernel<T, FM, FN, false>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
     else
         hipLaunchKernelGGL((linear_small_kernel<T, FM, FN, true>), dim3((unsigned)(tm * tn)), dim3(64 * SW), 0, stream, A, (int)tn);
+    timing_end(tk, stream);
     return hipGetLastError();
 }
 
@@ -725,8 +738,10 @@ hipError_t run_ring(const LinArgs& A, hipStream_t stream) {
     const hipError_t e = allow_lds<kernel, R::LDS>();
     if (e != hipSuccess) return e;
     const int64_t tm = (A.M + BM - 1) / BM, tn = (A.N + BN - 1) / BN;
+    const int tk = time_launch(NITI_TIMING_KERNEL, stream, "linear_ring_kernel<%s,%d,%d,%d,%d,%d,%d>", type_name<T>(), BM, BN, NS, WGM, WGN, KS);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn), A.klen ? (unsigned)((A.K + A.klen - 1) / A.klen) : 1), dim3(R::NT), R::LDS,
                        stream, A, (int)tn);
+    timing_end(tk, stream);
     return hipGetLastError();
 }
 
@@ -930,8 +945,10 @@ hipError_t run_linear(LinArgs A, void* ws, size_t ws_bytes, hipStream_t stream) 
         if (e != hipSuccess) return e;
         A.part = P.part;
         const int64_t groups = (A.N + 7) / 8;
+        const int tk = time_launch(NITI_TIMING_SUM, stream, "linear_join_kernel<%s>", type_name<T>());
         hipLaunchKernelGGL((linear_join_kernel<T>), dim3((unsigned)((A.M * groups + 255) / 256)), dim3(256), 0, stream, A,
                            (const int32_t*)ws, c.parts, P.ldout, (int)groups);
+        timing_end(tk, stream);
         return hipGetLastError();
     }
     switch (c.kernel) {
@@ -951,8 +968,10 @@ template <typename T, int FM, int FN>
 hipError_t run_small_pair(const LinArgs& A, const LinArgs& B, hipStream_t stream) {
     const auto tiles = [](int64_t n, int t) { return (n + t - 1) / t; };
     const int64_t na = tiles(A.N, 16 * FN), nb = tiles(B.N, 16 * FN), ba = tiles(A.M, 16 * FM) * na, bb = tiles(B.M, 16 * FM) * nb;
+    const int tk = time_launch(NITI_TIMING_KERNEL, stream, "linear_small_pair_kernel<%s,%d,%d>", type_name<T>(), FM, FN);
     hipLaunchKernelGGL((linear_small_pair_kernel<T, FM, FN>), dim3((unsigned)(ba + bb)), dim3(64 * SW), 0, stream,
                        LinPair{{A, B}, {(int)na, (int)nb}, (int)ba});
+    timing_end(tk, stream);
     return hipGetLastError();
 }
 
@@ -964,7 +983,9 @@ hipError_t run_ring64_pair(const LinArgs& A, const LinArgs& B, hipStream_t strea
     if (e != hipSuccess) return e;
     const auto tiles = [](int64_t n) { return (n + 63) / 64; };
     const int64_t na = tiles(A.N), nb = tiles(B.N), ba = tiles(A.M) * na, bb = tiles(B.M) * nb;
+    const int tk = time_launch(NITI_TIMING_KERNEL, stream, "linear_ring_pair_kernel<%s,64,64,3,2,2,128>", type_name<T>());
     hipLaunchKernelGGL(kernel, dim3((unsigned)(ba + bb)), dim3(R::NT), R::LDS, stream, LinPair{{A, B}, {(int)na, (int)nb}, (int)ba});
+    timing_end(tk, stream);
     return hipGetLastError();
 }
 
