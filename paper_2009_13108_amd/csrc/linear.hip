@@ -18,6 +18,7 @@
 
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -721,13 +722,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 :
     ring_tile<T, BM, BN, NS, WGM, WGN, KS>(P.a[i], P.tiles_n[i], (int)blockIdx.x - i * P.blocks);
 }
 
-// Once for each kernel: it may have more than 64 KiB of LDS.
+// Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
 template <auto kernel, int LDS>
 hipError_t allow_lds() {
-    static bool done = false;
-    if (done) return hipSuccess;
-    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    done = e == hipSuccess;
+    static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
     return e;
 }
 
