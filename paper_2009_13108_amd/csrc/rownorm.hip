@@ -547,9 +547,10 @@ hipError_t run_bwd(const RowBwdArgs& a, int64_t parts, hipStream_t stream) {
 
 // Workgroups of the backward pass, which is also the number of partial rows.
 int64_t bwd_parts(int64_t M, int64_t D) {
-    // A few rows go by one workgroup, whose sums are dgain and which saves the second launch.  One
-    // launch and two (us): 16 rows of 1000 6.5, 6.7, 32 9.6, 6.6; 4 rows of 4096 7.1, 6.9, 8 10.8, 7.0; 4 of 9216 10.5, 8.1.
-    const int p = pieces(D), few = p <= 128 ? 16 : (p <= 512 ? 4 : 2);
+    // A few rows go by one workgroup, whose sums are dgain and which saves the second launch.  Both ways (us, one launch
+    // and two; bf16, 32 bits in brackets): 16 rows of 512 4.6, 5.1 (4.4, 5.1), of 1000 5.7, 5.7 (6.3, 5.8), 24 of 512 5.6, 5.1;
+    // 3 rows of 4096 5.4, 5.9 (6.1, 6.1), 4 of 1111 5.9, 5.5, 4 of 4096 6.4, 6.0; 2 rows of 9216 6.5, 7.2 (8.3, 8.5), 3 8.1, 7.3.
+    const int p = pieces(D), few = p <= 128 ? 16 : (p <= 512 ? 3 : 2);
     if (M <= few) return M > 0 ? 1 : 0;
     const int64_t units = p <= 128 ? (M + 3) / 4 : M;
     return units < kMaxParts ? units : kMaxParts;
