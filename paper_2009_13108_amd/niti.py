@@ -670,8 +670,20 @@ def _matrix(x, what):
     return shape, dev
 
 
-def _width(t, axis):
-    return t.shape[axis] if isinstance(t, _Tensor) and t.dim() == 2 else -1
+def _width(t, axis, what):
+    """Size of a matrix that gives a call one of its sizes."""
+    if not isinstance(t, _Tensor):
+        raise TypeError("%s must be a device tensor" % what)
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % what)
+    return t.shape[axis]
+
+
+def _dtype(t, what):
+    """Type of an operand that a call cannot go without."""
+    if not isinstance(t, _Tensor):
+        raise TypeError("%s must be a device tensor" % what)
+    return t.dtype
 
 
 def _ws_args(ws, dev):
@@ -694,7 +706,7 @@ def rmsnorm_fwd(x, gain, res=None, h=None, y=None, q=None, scale=None, rstd=None
     ph, ldh = _mat(h, dev, dt, (M, D), "h", True)
     py, ldy = _mat(y, dev, dt, (M, D), "y", True)
     pq, ldq = _mat(q, dev, _torch_mod.int8, (M, D), "q", True)
-    _run("niti_rmsnorm_fwd", px, ldx, pr, ldr, _vec(gain, dev, D, "gain"), _type_of(gain.dtype, "gain"), ph, ldh, py, ldy, pq,
+    _run("niti_rmsnorm_fwd", px, ldx, pr, ldr, _vec(gain, dev, D, "gain"), _type_of(_dtype(gain, "gain"), "gain"), ph, ldh, py, ldy, pq,
          ldq, _vec(scale, dev, M, "scale", f32), _vec(rstd, dev, M, "rstd", f32), M, D, eps, kind, _stream(stream))
 
 
@@ -709,7 +721,7 @@ def rmsnorm_bwd(dy, h, gain, rstd, dx, dgain=None, ws=None, dh=None, stream=None
     pdh, lddh = _mat(dh, dev, dt, (M, D), "dh")
     pdx, lddx = _mat(dx, dev, dt, (M, D), "dx", True)
     pws, nws = _ws_args(ws, dev)
-    _run("niti_rmsnorm_bwd", pdy, lddy, ph, ldh, _vec(gain, dev, D, "gain"), _type_of(gain.dtype, "gain"),
+    _run("niti_rmsnorm_bwd", pdy, lddy, ph, ldh, _vec(gain, dev, D, "gain"), _type_of(_dtype(gain, "gain"), "gain"),
          _vec(rstd, dev, M, "rstd", f32), pdh, lddh, pdx, lddx, _vec(dgain, dev, D, "dgain", f32), M, D, kind, pws, nws,
          _stream(stream))
 
@@ -730,8 +742,8 @@ def linear_fwd(a, b, out, s_a, s_b, bias=None, act=ACT_NONE, res=None, z=None, w
     """out = act(s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n]) + res; z: the
     value before the activation; ws as workspace_bytes(OP_LINEAR_FWD, None, M, N, K), or None (niti_linear_fwd)."""
     (M, K), dev = _matrix(a, "a")
-    N = _width(b, 0)
-    i8, dt = _torch_mod.int8, out.dtype
+    N = _width(b, 0, "b")
+    i8, dt = _torch_mod.int8, _dtype(out, "out")
     kind = _type_of(dt, "out")
     pa, lda = _mat(a, dev, i8, (M, K), "a")
     pb, ldb = _mat(b, dev, i8, (N, K), "b")
@@ -751,7 +763,7 @@ def linear_bwd(dy, a, b, s_a, s_b, ws, z=None, act=ACT_NONE, da=None, db=None, d
     """Gradients of the values that a and b stand for and of the bias, by int8
     products; ws as workspace_bytes(OP_LINEAR_BWD, None, M, N, K) (niti_linear_bwd)."""
     (M, N), dev = _matrix(dy, "dy")
-    K = _width(a, 1)
+    K = _width(a, 1, "a")
     i8, f32, dt = _torch_mod.int8, _torch_mod.float32, dy.dtype
     kind = _type_of(dt, "dy")
     pdy, lddy = _mat(dy, dev, dt, (M, N), "dy")
@@ -807,6 +819,9 @@ def adamw_plan(params, grads, m, v, m_scale=None, v_scale=None, m_read=None, v_r
     for name, x in lists.items():
         if x is not None and len(x) != count:
             raise ValueError("adamw_plan: %d params and %d %s" % (count, len(x), name))
+    for name, x in [("params", params)] + list(lists.items()):
+        if x is not None and not all(isinstance(t, _Tensor) for t in x):
+            raise TypeError("adamw_plan: %s must be device tensors" % name)
     p_dt = params[0].dtype if count else torch.float32
     g_dt = grads[0].dtype if count else torch.float32
     r_dt = next((x[0].dtype for x in (m_read, v_read) if x), torch.float32)
