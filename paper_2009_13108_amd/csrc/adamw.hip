@@ -53,6 +53,7 @@ struct Step {
     uint64_t seed;
     uint32_t call;
     int sr;
+    int exact;              // eps is too small for the hardware's roots and reciprocals as they are
 };
 
 struct Table {
@@ -93,11 +94,16 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top_bits, float unit)
 
 // Square roots and reciprocals are the hardware's, good to one unit in the last
 // place; the IEEE sequences around them took as long as the memory traffic.  They
-// take a value below the normal range for zero, so m / (sqrt(v) root + eps) scales small
-// ones up by powers of two, which is exact: gradients below 1e-17 have such v, and with eps = 0
-// nothing else is in the divisor.  (The codes' roots need no such care: what is that
-// much smaller than its block's largest has code 0, or 1, either way.)
+// take a value below the normal range for zero: a root of at most 2^-63, which is
+// below half a unit of an eps of 2^-36 / sqrt(1 - b2^t) or more.  With a smaller eps (Step::exact)
+// small values are scaled up first by powers of two, which loses nothing: gradients below 1e-17
+// have such v, and with eps = 0 nothing else is in the divisor.  For every eps that took
+// 6 us more of the 163 of a step with 8-bit states.  (The codes' roots need no such care: what is
+// that much smaller than its block's largest has code 0, or 1, either way.)
 __device__ __forceinline__ float root_ratio(float m, float v, float root, float eps) {
+    return m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * root + eps);
+}
+__device__ __forceinline__ float root_ratio_exact(float m, float v, float root, float eps) {
     const bool low = v < 0x1p-100f;
     const float d = __builtin_amdgcn_sqrtf(low ? v * 0x1p60f : v) * (low ? 0x1p-30f : 1.f) * root + eps;
     const bool tiny = d < 0x1p-60f;
@@ -145,7 +151,13 @@ __device__ __forceinline__ void adamw_elements(const Entry& E, const Step& S, in
         const float x = g[e] * gs;
         m[e] = S.b1 * m[e] + S.c1 * x;
         v[e] = S.b2 * v[e] + S.c2 * (x * x);
-        p[e] = p[e] * S.keep - S.lr * root_ratio(m[e], v[e], S.root, S.eps);
+    }
+    if (S.exact) {
+#pragma unroll
+        for (int e = 0; e < PT; e++) p[e] = p[e] * S.keep - S.lr * root_ratio_exact(m[e], v[e], S.root, S.eps);
+    } else {
+#pragma unroll
+        for (int e = 0; e < PT; e++) p[e] = p[e] * S.keep - S.lr * root_ratio(m[e], v[e], S.root, S.eps);
     }
     store_some((TP*)E.p + i, n, p);
     if constexpr (BITS == 32) {
@@ -348,6 +360,7 @@ niti_status niti_adamw_step(const niti_adamw_tensor* tensors, int64_t count, int
     s.lr = (float)(lr / (1 - pow(beta1, (double)step)));
     s.root = (float)(1 / sqrt(1 - pow(beta2, (double)step)));
     s.eps = (float)eps;
+    s.exact = s.eps < 0x1p-36f * s.root;
     s.gscale = grad_scale;
     s.seed = seed;
     s.call = (uint32_t)step;

@@ -49,3 +49,10 @@ def test_eight_bit_states_with_small_gradients():
     sm, sv = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
     niti.adamw_step(niti.adamw_plan([p], [g], [m], [v], [sm], [sv]), 1, LR, beta1=B1, beta2=B2, eps=0.0)
     assert math.isfinite(float(p.sum())) and torch.allclose(p, torch.full_like(p, -LR), rtol=1e-5, atol=0)
+
+
+@pytest.mark.parametrize("step,limit", [(1, 2.0 ** -36 / math.sqrt(1 - B2)), (100000, 2.0 ** -36)])
+@pytest.mark.parametrize("factor", [0.98, 1.02])
+def test_both_sides_of_the_least_plain_eps(step, limit, factor):
+    """eps just below and above what lets the hardware's roots be taken as they are."""
+    test_small_gradients(step, limit * factor)
