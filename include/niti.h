@@ -267,7 +267,8 @@ niti_status niti_int_ce_loss_grad(const int8_t *logits, const int8_t *s_logits,
 niti_status niti_sgd_update(int8_t *w, const int32_t *g32, int64_t n, int mu,
                             niti_round_mode mode, niti_stats *stats, void *stream);
 
-/* Bytes of workspace an operation needs (0 when none).  d is used by the
+/* Bytes of workspace an operation needs (0 when none, and for sizes that the
+ * operators on int8 rows refuse).  d is used by the
  * convolution ops, (M, N) = (batch, classes) by the loss, and (M, N, K) by the
  * operators on int8 rows as their ids say. */
 size_t niti_workspace_bytes(int op, const niti_conv_desc *d, int64_t M, int64_t N, int64_t K);

@@ -453,7 +453,7 @@ BwdSpace space(int64_t M, int64_t N, int64_t K) {
 }  // namespace
 
 size_t linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
-    return M > 0 && N > 0 && K >= 0 ? (size_t)space(M, N, K).total : 0;
+    return M > 0 && N > 0 && K >= 0 && M < kMaxSum && N < kMaxSum && K < kMaxLd ? (size_t)space(M, N, K).total : 0;
 }
 
 }  // namespace niti

@@ -560,7 +560,7 @@ int64_t bwd_parts(int64_t M, int64_t D) {
 }  // namespace
 
 size_t rmsnorm_bwd_workspace(int64_t M, int64_t D) {
-    return M > 0 && D > 0 ? (size_t)(bwd_parts(M, D) * D * 4 + 255) / 256 * 256 : 0;
+    return M > 0 && D > 0 && M < kMaxDim && D < kMaxLd ? (size_t)(bwd_parts(M, D) * D * 4 + 255) / 256 * 256 : 0;
 }
 
 }  // namespace niti
