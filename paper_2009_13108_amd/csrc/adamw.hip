@@ -5,8 +5,8 @@
 //
 // Every element is read and written once, so memory bounds it: 28 bytes an
 // element with p, g, m, v in 32 bits, 14 with 8-bit states and g in 16 (62 M such
-// elements: 165 us, 5.3 TB/s, and 70 us for reading their states as bf16, 5.3 TB/s;
-// 61 thousand with 32-bit states 4.1 us, which is a launch).  The
+// elements: 164 us, 5.3 TB/s, and 70 us for reading their states as bf16, 5.3 TB/s;
+// 61 thousand with 32-bit states 4.2 us, which is a launch).  The
 // tensors of a call share launches: the table of their addresses travels in
 // the kernel's arguments (no copy to the device, nothing to keep alive), a
 // workgroup finds the tensor of its chunk by comparing its index with all

@@ -11,9 +11,9 @@
 // whole pieces first.  Few products: small tiles straight from memory.  Long
 // sums of few products: parts side by side in the workspace.
 //
-// Measured: 8192 x 8192 x 8192 to bf16 491 us, 2.24 POPS, bound by power (the clock falls
-// to 1.7 GHz with the MFMAs busy 69% of it); one token by 4096 x 4096 6.0 us, 2.8 TB/s of
-// weights; 1000 x 1500 x 1111 in 32 bits with every operand 15.
+// Measured: 8192 x 8192 x 8192 to bf16 484 to 491 us, 2.24 to 2.27 POPS, bound by power (the
+// clock falls to 1.55 to 1.73 GHz with the MFMAs busy 65 to 60% of it); one token by 4096 x 4096
+// 6.1 us, 2.8 TB/s of weights; 1000 x 1500 x 1111 in 32 bits with every operand 15.
 #include "linear.h"
 
 #include <math.h>
@@ -374,7 +374,7 @@ hipError_t run_any(const LinArgs& A, hipStream_t stream) {
 // of weights.
 // 16 bytes as they are loaded.  BYTES: from an address that is no multiple of 4.
 // The hardware takes such loads apart where the lanes beside one read other rows
-// (one token by 4096 x 4097 took 10.9 us, by 4096 x 4100 6.4; the kernel above,
+// (one token by 4096 x 4097 took 10.9 us, with aligned words 7.1, by 4096 x 4100 5.8; the kernel above,
 // whose lanes read a row four by four, loses by the shifts), so the aligned words that hold the bytes are loaded, five
 // where the address is not aligned, and shifted when they are used.  Every word
 // read holds a byte of the piece.
@@ -548,8 +548,8 @@ hipError_t run_small(const LinArgs& A, hipStream_t stream) {
 // ---------------------------------------------------------------- ring
 // Tiles of BM x BN from an LDS ring of NS stages of KS bytes a row, filled by
 // direct-to-LDS loads.  Needs K, strides and addresses in whole 16 bytes.
-// 256 x 256 tiles read the least from L2 and LDS for a product (4096 x 4096 x 2048 38.5 us,
-// 1.8 POPS), smaller ones give more CUs work (2048 x 4096 x 4096 by 128 x 128 38.1).
+// 256 x 256 tiles read the least from L2 and LDS for a product (4096 x 4096 x 2048 44 us, by
+// 128 x 128 50), smaller ones give more CUs work (2048 x 4096 x 4096 by 128 x 128 44, by 256 x 256 58).
 constexpr uint32_t kOut = 0x80000000u;   // an offset past any tile: loads zeros
 
 template <int N>
@@ -811,11 +811,11 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinArgs A, const int32
 //   kRounds  start + ceil(t) * (round + k * step) + k * more * min(1, t)               (one tile a CU at a time)
 // Small tiles give every CU work and split the sum, large ones load less for each
 // product; 128 x 128 tiles have a ring of four stages, one a CU, which a
-// CU with one tile needs to cover a load's latency (800 x 2880 x 3712, 161 tiles: 28.3 ->
-// 20.5 us), or of two, two tiles a CU (2048 x 4096 x 4096: 38 us, 44 with four).  Fitted to
+// CU with one tile needs to cover a load's latency (800 x 2880 x 3712, 161 tiles: 25.9 ->
+// 19.4 us), or of two, two tiles a CU (2048 x 4096 x 4096: 44 us, 48 with four).  Fitted to
 // 500 random products of 1..8192 x 32..9216 x 32..9216 timed with each kernel;
 // what the model picks takes 1.4% longer than the fastest of these seven in the
-// mean, 64 x 64 tiles alone 33%.
+// mean, on 250 others 1.8%; 64 x 64 tiles alone 33% and 36%.
 enum CostForm { kSpread, kTwo, kRounds };
 struct Cost {
     int bm, bn;
@@ -891,7 +891,7 @@ Choice choose(int64_t M, int64_t N, int64_t K, Rows rows, size_t room) {
         take(Choice::k64, cost(tile, M, N, klen * parts, parts) + 2.3f + (float)(bytes * 2. / 4e6), parts, klen);
     }
     // Rows at odd addresses: a launch that copies them to whole pieces, and the kernels for
-    // those (4096 x 4096 x 4097: 215 -> 92 us, 2000 x 2000 x 1111: 20 -> 17).
+    // those (4096 x 4096 x 4097: 246 -> 96 us, 2000 x 2000 x 1111: 20 -> 17).
     const size_t copies = whole ? 0 : pack_bytes(M, N, K);
     if (copies > 0 && copies <= room) {
         Choice p = choose(M, N, up16(K), kOfPieces, room - copies);

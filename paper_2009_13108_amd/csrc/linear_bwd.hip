@@ -17,8 +17,8 @@
 // mostly from the last-level cache; holding dz for step 3 would round it or cost
 // four bytes an element each way.
 //
-// Measured, 2048 x 4096 x 4096 bf16 with SiLU: 13.6, 4.8, 24.8 (96 MB, 3.9 TB/s), 38.5 and
-// 38.1 us (1.8 POPS), 115 together: the products' tiles make one and two rounds of the
+// Measured, 2048 x 4096 x 4096 bf16 with SiLU: 13.7, 5.0, 24.8 (96 MB, 3.9 TB/s), 40.9 and
+// 37.9 us (1.7 and 1.8 POPS), 109 to 117 together: the products' tiles make one and two rounds of the
 // CUs, steps 1 and 3 are bound by memory with the activation's slope on top.
 #include <type_traits>
 
@@ -523,7 +523,8 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.csum = (float*)(base + w.csum);
     if (by_type(type, [&](auto t) { return run_stats<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
     // Tiles of step 3 read those of step 1 that they lie in, each again: up to 32 by 40 of them (512 x 10240) that takes
-    // less than a launch (250 x 4096 x 512 29.2 -> 26.9 us, 200 x 9000 x 1024 45.6 -> 43.5, 400 x 1024 x 512 21.3 -> 19.5).
+    // less than a launch (250 x 4096 x 512 26.3 -> 24.5 us, 200 x 9000 x 1024 45.2 -> 42.9, 400 x 1024 x 512 18.2 -> 16.5,
+    // 512 x 10240 x 512 44.6 -> 42.7).
     d.join = (da || db) && w.tiles_m <= 32 && w.tiles_n <= 40;
     if (!d.join) {
         const int64_t cols = (N + 63) / 64;

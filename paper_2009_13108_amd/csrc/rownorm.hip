@@ -15,10 +15,11 @@
 // registers, writes them once to the workspace, and a second launch adds the G
 // partial rows in a fixed order.
 //
-// Measured, bf16: 4096 x 4096 with residual and codes 30.6 us (151 MB, 4.9 TB/s; a copy
-// reaches 5.3), one such row 3.2; codes of 4096 x 9216 35.6 (189 MB, 5.3 TB/s); backward of
-// 4096 x 4096 28.0 (134 MB, 4.8 TB/s) and 4.1 for the second launch.  In 32 bits, backward of
-// 1777 x 1111: 8.4 and 3.8, bound by latency with three or four rows a workgroup.
+// Measured, bf16: 4096 x 4096 with residual and codes 30.4 us (151 MB, 5.0 TB/s; a copy
+// reaches 5.3), one such row 3.0; codes of 4096 x 9216 35.9 (189 MB, 5.3 TB/s), rounded stochastically
+// 50.9: two 64-bit products an element; backward of 4096 x 4096 28.5 (134 MB, 4.7 TB/s) and 4.2 for
+// the second launch.  In 32 bits, backward of 1777 x 1111: 8.6 and 3.8, bound by latency with three or
+// four rows a workgroup.
 #include "scaled.h"
 
 namespace niti {

@@ -207,9 +207,9 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
 
 // exp(x) for |x| <= 80 by the hardware's power of two.  The rounding of x log2(e)
 // leaves a relative error of |x| 2^-24: in a sigmoid that is at most s (1 - s) |x| 2^-24 <
-// 0.23 * 2^-24, and a normal density's is as small.  The library's expf and an IEEE
-// division cost ten instructions each; with them the slopes alone bounded the
-// passes over a gradient.
+// 0.23 * 2^-24.  SiLU in 32 bits is up to 1.2e-6 off (z near 12), as the plain form is, and up to 9e-7 of
+// its value, z / (1 + exp(-z)) with the library's expf 1.6e-7.  That and an IEEE division cost ten
+// instructions each; with them the slopes alone bounded the passes over a gradient.
 __device__ __forceinline__ float exp_mid(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float sigmoid_mid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_mid(-x)); }
 
@@ -221,8 +221,8 @@ __device__ __forceinline__ float half_exp(float s) { return __builtin_amdgcn_exp
 // bits for the least largest error: P within 2.1e-9 of the function for |z| < 1.25, Q within 9e-9
 // of the tail, relative, from there to 12.5.  In 32 bits GELU is then nowhere further from
 // its exact value than z (1 + erf(z / sqrt 2)) / 2 is, which loses the tail of negative z.
-// A five-term error function costs less (4096 x 4096 x 512 to bf16 39.9 us for 42.5, 1000 x 1500 x 1111
-// in 32 bits 15.4 for 15.5) and was up to 1e-2 of the value off there.
+// A five-term error function costs less (4096 x 4096 x 512 to bf16 39.9 us for 42.5 on the same card,
+// 1000 x 1500 x 1111 in 32 bits 15.4 for 15.5) and was up to 3e-2 of the value off there.
 __device__ __forceinline__ float normal_cdf(float z, float s, float e) {
     float p = __builtin_fmaf(s, -6.66287769e-06f, 0.000110409092f);
     p = __builtin_fmaf(s, p, -0.00118284649f);
