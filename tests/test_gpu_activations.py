@@ -33,9 +33,10 @@ def slope(z, act):
     n = z.numel()
     a, b = torch.zeros(1, 1, dtype=torch.int8, device="cuda"), torch.zeros(n, 1, dtype=torch.int8, device="cuda")
     dbias, one = torch.empty(n, device="cuda"), torch.ones(1, device="cuda")
-    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, 1, n, 1))
-    for at in range(0, n, 1 << 16):   # columns of one call
-        part = z[at:at + (1 << 16)].view(1, -1)
+    most = min(n, 1 << 16)   # columns of one call
+    ws = niti.new_workspace(niti.workspace_bytes(niti.OP_LINEAR_BWD, None, 1, most, 1))
+    for at in range(0, n, most):
+        part = z[at:at + most].view(1, -1)
         k = part.shape[1]
         niti.linear_bwd(torch.ones_like(part), a, b[:k], one, one, ws, z=part, act=act, dbias=dbias[at:at + k])
     return dbias.double()
