@@ -352,7 +352,8 @@ niti_status niti_dropout_bwd(const int8_t *dy, const uint8_t *keep, int8_t *dx, 
 typedef enum niti_type {
     NITI_F32 = 0,
     NITI_BF16 = 1,
-    NITI_F16 = 2
+    NITI_F16 = 2,
+    NITI_I8 = 3    /* int8 rows with a scale each: where an operand's description says so */
 } niti_type;
 
 typedef enum niti_act {
@@ -366,6 +367,11 @@ typedef enum niti_act {
 #define NITI_OP_RMSNORM_BWD 5   /* (M, D, -) */
 #define NITI_OP_LINEAR_FWD  6   /* (M, N, K) */
 #define NITI_OP_LINEAR_BWD  7   /* (M, N, K) */
+#define NITI_OP_GATED_FWD   8   /* (M, F, K) */
+#define NITI_OP_GATED_BWD   9   /* (M, F, K) */
+#define NITI_OP_EMBEDDING_BWD  10   /* (M, V, D) */
+#define NITI_OP_TOKEN_LOGPROBS 11   /* (M, V, top) */
+#define NITI_OP_DISTILL_FWD    12   /* (M, V, -) */
 
 /* Root-mean-square norm with the residual's addition.  Per row of D elements
  *     h = x + res,  rstd = 1 / sqrt(mean(h^2) + eps),  y = h * rstd * gain,
@@ -433,6 +439,96 @@ niti_status niti_linear_bwd(const void *dy, int64_t lddy, const void *z, int64_t
                             const float *s_b, int64_t s_b_n, void *da, int64_t ldda, void *db, int64_t lddb,
                             float *dbias, int64_t M, int64_t N, int64_t K, niti_round_mode mode, uint64_t seed,
                             uint32_t call, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Gated product of int8 rows: both projections of a feed-forward block, the
+ * activation and the product.  a [M][K], b [2 F][K] (the gates' rows, then
+ * their partners'),
+ *     z[m][n] = s_a[m] * s_b[n] * sum_k a[m][k] b[n][k] + bias[n],  n < 2 F,
+ *     out[m][n] = act(z[m][n]) * z[m][F + n],
+ * formed from z in 32 bits.  s_a holds M scales or one, s_b 2 F or one; bias
+ * [2 F] and z [M][2 F] (for the backward pass, in out's type) are optional.  K
+ * in 0..131071.  Workspace: niti_workspace_bytes(NITI_OP_GATED_FWD, NULL, M, F,
+ * K), 0 where K is a multiple of 16; without it the call takes longer for
+ * other K (large operands are then not copied to whole pieces first). */
+niti_status niti_gated_fwd(const int8_t *a, int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b, int64_t ldb,
+                           const float *s_b, int64_t s_b_n, const void *bias, int bias_type, int act, void *z,
+                           int64_t ldz, void *out, int64_t ldout, int64_t M, int64_t F, int64_t K, int type, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* Its backward pass, for the gradient dy [M][F] of out, from the forward call's
+ * z [M][2 F]: with
+ *     dz[m][n] = dy[m][n] z[m][F + n] act'(z[m][n]),   dz[m][F + n] = dy[m][n] act(z[m][n]),
+ * da, db [2 F][K] and dbias [2 F] are those of niti_linear_bwd with N = 2 F (its
+ * draws' indices too: m * 2 F + n).  M up to 131071, F up to 65535.  Workspace:
+ * niti_workspace_bytes(NITI_OP_GATED_BWD, NULL, M, F, K). */
+niti_status niti_gated_bwd(const void *dy, int64_t lddy, const void *z, int64_t ldz, int act, const int8_t *a,
+                           int64_t lda, const float *s_a, int64_t s_a_n, const int8_t *b, int64_t ldb,
+                           const float *s_b, int64_t s_b_n, void *da, int64_t ldda, void *db, int64_t lddb,
+                           float *dbias, int64_t M, int64_t F, int64_t K, niti_round_mode mode, uint64_t seed,
+                           uint32_t call, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Embedding lookup with scaling: out[m] = alpha * table[tokens[m]], rows of D
+ * elements, tokens int32 [M].  The table [V][D] is of table_type: a float
+ * type, or NITI_I8 with one scale a row in table_scale [V] (NULL otherwise).
+ * A token outside 0..V-1 (padding) gets a row of zeros.  alpha is finite. */
+niti_status niti_embedding_fwd(const void *table, int64_t ldt, int table_type, const float *table_scale,
+                               const int32_t *tokens, void *out, int64_t ldout, int64_t M, int64_t V, int64_t D,
+                               float alpha, int type, void *stream);
+
+/* The table's gradient, for the gradient dy [M][D] of out:
+ *     dtable[v] = alpha * sum of dy[m] over the m with tokens[m] = v,
+ * summed in 32 bits in an order that the tokens fix, and rounded once to
+ * dtable_type.  accumulate != 0 adds to what dtable holds, and leaves the rows
+ * of tokens that do not occur as they are; otherwise these are zeros.
+ * Tokens outside 0..V-1 contribute nothing.  M up to 2^22.  Workspace:
+ * niti_workspace_bytes(NITI_OP_EMBEDDING_BWD, NULL, M, V, D). */
+niti_status niti_embedding_bwd(const void *dy, int64_t lddy, int type, const int32_t *tokens, void *dtable,
+                               int64_t ldt, int dtable_type, int64_t M, int64_t V, int64_t D, float alpha,
+                               int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* Log probabilities of logits x [M][V] (softmax of scale * x along the rows,
+ * 0 < scale < inf: the reciprocal of a temperature), each output optional:
+ *   logp      [M] of tokens[m] (int32; given exactly where logp is); 0 for a
+ *             token outside 0..V-1;
+ *   lse       [M] log sum exp(scale * x);
+ *   entropy   [M];
+ *   top_logp, top_idx   [M][top]: the `top` largest log probabilities in
+ *             order, equal ones by column, and their columns (int32).  top is
+ *             0..64, at most V, and 0 exactly where neither is given.
+ * Masked logits are minus infinity.  A row of nothing else has the
+ * log probability and lse minus infinity, entropy 0, and its first columns as
+ * alternatives; a row with a NaN or plus infinity is NaN throughout, its
+ * alternatives' columns -1.  Workspace: niti_workspace_bytes(
+ * NITI_OP_TOKEN_LOGPROBS, NULL, M, V, top), 0 for most sizes. */
+niti_status niti_token_logprobs(const void *x, int64_t ldx, const int32_t *tokens, float *logp, float *lse,
+                                float *entropy, float *top_logp, int32_t *top_idx, int64_t M, int64_t V, int64_t top,
+                                float scale, int type, void *ws, size_t ws_bytes, void *stream);
+
+/* Divergence of a row's softmax q of scale * x [M][V] from a teacher's
+ * distribution p, the softmax of scale * t_val over the row's list of `top`
+ * columns t_idx (int32) with their logits t_val (t_type), both [M][top]:
+ *     loss[m] = sum_j p_j (log p_j - log q[t_idx_j]).
+ * top is 1..256.  A column outside 0..V-1 is no part of the list (lists of
+ * different lengths are filled up with -1); one that is listed twice counts
+ * twice.  An empty list, or one of minus infinities, has loss 0 and gradient 0.  lse [M],
+ * optional, is kept for the backward pass.  dx, optional, receives the
+ * gradient in the same pass,
+ *     dx[m][v] = dloss[m] * scale * (q_v - sum of the p_j with t_idx_j = v),
+ * with dloss float [M], or one for all (dloss_n = 1), or NULL for 1; dx may be
+ * x.  A row of x with a NaN or plus infinity gives NaN, one of minus infinities
+ * the loss plus infinity and q = 0.  Workspace:
+ * niti_workspace_bytes(NITI_OP_DISTILL_FWD, NULL, M, V, 0), 0 up to 65536 columns. */
+niti_status niti_distill_fwd(const void *x, int64_t ldx, const void *t_val, int64_t ldt, int t_type,
+                             const int32_t *t_idx, int64_t ldi, float *loss, float *lse, const float *dloss,
+                             int64_t dloss_n, void *dx, int64_t lddx, int64_t M, int64_t V, int64_t top, float scale,
+                             int type, void *ws, size_t ws_bytes, void *stream);
+
+/* The gradient alone, from the forward call's lse, for a dloss that is known
+ * later.  dx may be x. */
+niti_status niti_distill_bwd(const void *x, int64_t ldx, const void *t_val, int64_t ldt, int t_type,
+                             const int32_t *t_idx, int64_t ldi, const float *lse, const float *dloss, int64_t dloss_n,
+                             void *dx, int64_t lddx, int64_t M, int64_t V, int64_t top, float scale, int type,
+                             void *stream);
 
 /* One tensor of an optimiser's step: n elements, all arrays contiguous.  p is
  * the parameter, g its gradient.  32-bit states: m and v are float, m_scale

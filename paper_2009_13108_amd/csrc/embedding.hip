@@ -1,0 +1,456 @@
+// Embedding lookup with scaling, and the table's gradient.
+//
+// Forward:   out[m] = alpha table[token m], the table in a float type or as int8 rows with a scale each.
+// Gradient:  dtable[v] = alpha sum over the m with token v of dy[m]  (+ dtable[v]).
+//
+// The gradient goes by sorted tokens, so that every sum has a fixed order and no
+// atomics.  (1) A workgroup sorts up to 16384 tokens in its LDS (radix sort, stable; longer
+// batches are sorted in such chunks and placed by binary searches in the other chunks); meanwhile the other
+// workgroups of the launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
+// read and added up: a token whose rows lie inside such a stretch gets its row
+// at once, one that crosses its ends leaves partial sums in the workspace, and (3) those are joined
+// in order.  However often a token occurs, the work is split evenly.
+#include "linear.h"
+
+#include <atomic>
+#include <type_traits>
+
+namespace niti {
+
+namespace {
+
+constexpr int kSortMax = 16384;   // tokens that one workgroup sorts
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kRounds = kSortMax / kSortThreads;
+constexpr int kBins = 256;
+constexpr int kRun = 16;          // sorted rows of a stretch
+constexpr int64_t kMaxTokens = (int64_t)1 << 22;
+
+// ---------------------------------------------------------------- forward
+struct EmbArgs {
+    const void* table;
+    const float* scale;      // of int8 rows
+    const int32_t* tokens;
+    void* out;
+    int64_t ldt, ldo, M, V, D;
+    uint32_t ppr;            // pieces of a row
+    float alpha;
+};
+
+// Eight codes of column c on, moved down where the row ends (D >= 8).
+__device__ __forceinline__ void load_codes(const int8_t* row, int c, int D, float (&v)[CH]) {
+    const int from = min(c, D - CH);
+    uint64_t w;
+    __builtin_memcpy(&w, row + from, 8);
+    const int down = c - from;
+    w >>= 8 * min(down, 7);
+#pragma unroll
+    for (int e = 0; e < CH; e++) v[e] = (float)(int8_t)(w >> (8 * e));
+}
+
+// TT: the table's type, int8_t for rows of codes.
+template <typename TT, typename T>
+__global__ __launch_bounds__(256) void embedding_kernel(EmbArgs a) {
+    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = (int64_t)(i / a.ppr);
+    if (m >= a.M) return;
+    const int c = (int)(i % a.ppr) * CH, D = (int)a.D;
+    const int tok = a.tokens[m];
+    const bool in = (uint32_t)tok < (uint64_t)a.V;   // (negative ones are above every V)
+    const TT* row = (const TT*)a.table + (in ? tok : 0) * a.ldt;
+    float v[CH], f = a.alpha;
+    if constexpr (__is_same(TT, int8_t)) {
+        f *= a.scale[in ? tok : 0];
+        if (D >= CH) {
+            load_codes(row, c, D, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < CH; e++) v[e] = (float)row[min(c + e, D - 1)];
+        }
+    } else if (D >= CH) {
+        piece_values<TT, false>(load_piece<TT, false>(row, c, D), c, D, v);
+    } else {
+        load_some(row + c, D - c, v);
+    }
+#pragma unroll
+    for (int e = 0; e < CH; e++) v[e] = in ? v[e] * f : 0.f;
+    store_some((T*)a.out + m * a.ldo + c, D - c, v);
+}
+
+// ---------------------------------------------------------------- gradient
+struct EmbBwdArgs {
+    const void* dy;
+    const int32_t* tokens;
+    void* dtable;
+    int64_t lddy, ldt, M, V, D;
+    float alpha;
+    int32_t accumulate, passes;   // passes of the sort
+    int32_t sorters;              // workgroups that sort, ahead of those that write zeros
+    int32_t *order, *key;         // [M]: rows by token, and their tokens (V for those outside the table)
+    int32_t *order1, *key1;       // the same of each chunk, where there are several
+    float* part;                  // [stretches][2][D]
+};
+
+// (1) LDS: the chunk's tokens, two lists of places, the waves' counters.
+template <typename TG>
+__global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int t = threadIdx.x;
+    if ((int)blockIdx.x >= a.sorters) {   // zeros of every n-th row
+        const float zero[CH] = {};
+        for (int64_t r = (int64_t)blockIdx.x - a.sorters; r < a.V; r += (int64_t)gridDim.x - a.sorters) {
+            TG* row = (TG*)a.dtable + r * a.ldt;
+            for (int c = t * CH; c < a.D; c += kSortThreads * CH) store_some(row + c, (int)(a.D - c), zero);
+        }
+        return;
+    }
+    const int64_t base = (int64_t)blockIdx.x * kSortMax;
+    const int n = (int)min((int64_t)kSortMax, a.M - base);
+    const int rounds = (n + kSortThreads - 1) / kSortThreads, room = rounds * kSortThreads;
+    uint32_t* key = (uint32_t*)lds;
+    uint16_t* src = (uint16_t*)(key + room);
+    uint16_t* dst = src + room;
+    volatile uint32_t* bins = (volatile uint32_t*)(dst + room);   // [wave][bin]
+    volatile uint32_t* totals = bins + kSortWaves * kBins;        // of the four waves that scan
+    for (int i = t; i < n; i += kSortThreads) {
+        const int tok = a.tokens[base + i];
+        key[i] = (uint32_t)tok < (uint64_t)a.V ? (uint32_t)tok : (uint32_t)a.V;
+        src[i] = (uint16_t)i;
+    }
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    for (int pass = 0; pass < a.passes; pass++) {
+        const int shift = 8 * pass;
+        for (int i = t; i < kSortWaves * kBins; i += kSortThreads) bins[i] = 0;
+        __syncthreads();
+        // A wave's places are consecutive: each counts those of its digit before it, in this wave.
+        uint32_t rank[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; r++) {
+            if (r >= rounds) break;
+            const int i = (wave * rounds + r) * 64 + lane;
+            const bool in = i < n;
+            const uint32_t d = in ? key[src[i]] >> shift & (kBins - 1) : 0u;
+            uint64_t peers = __ballot(in);
+#pragma unroll
+            for (int b = 0; b < 8; b++) {
+                const uint64_t ones = __ballot(d >> b & 1);
+                peers &= d >> b & 1 ? ones : ~ones;
+            }
+            volatile uint32_t* bin = bins + wave * kBins + d;
+            const uint32_t old = *bin;
+            rank[r] = old + (uint32_t)__popcll(peers & below);
+            __builtin_amdgcn_wave_barrier();
+            if (in && (peers & below) == 0) *bin = old + (uint32_t)__popcll(peers);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        // bins[wave][d] = places of smaller digits, and of this one in the waves before
+        uint32_t sum = 0, incl = 0;
+        if (t < kBins) {
+#pragma unroll
+            for (int w = 0; w < kSortWaves; w++) {
+                const uint32_t c = bins[w * kBins + t];
+                bins[w * kBins + t] = sum;
+                sum += c;
+            }
+            incl = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const uint32_t u = (uint32_t)__shfl_up((int)incl, o, kWave);
+                incl += lane >= o ? u : 0u;
+            }
+            if (lane == 63) totals[wave] = incl;
+        }
+        __syncthreads();
+        if (t < kBins) {
+            uint32_t before = incl - sum;
+            for (int w = 0; w < wave; w++) before += totals[w];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; w++) bins[w * kBins + t] = bins[w * kBins + t] + before;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; r++) {
+            if (r >= rounds) break;
+            const int i = (wave * rounds + r) * 64 + lane;
+            if (i < n) {
+                const uint16_t p = src[i];
+                dst[bins[wave * kBins + (key[p] >> shift & (kBins - 1))] + rank[r]] = p;
+            }
+        }
+        __syncthreads();
+        uint16_t* x = src;
+        src = dst, dst = x;
+    }
+    __syncthreads();   // (of no pass)
+    int32_t *order = a.order1 ? a.order1 : a.order, *keys = a.key1 ? a.key1 : a.key;
+    for (int i = t; i < n; i += kSortThreads) {
+        const int p = src[i];
+        order[base + i] = (int32_t)(base + p);
+        keys[base + i] = (int32_t)key[p];
+    }
+}
+
+// Number of keys below k (or up to k) of n in order.
+__device__ __forceinline__ int64_t count_below(const int32_t* key, int64_t n, int32_t k, bool equal) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        const int32_t v = key[mid];
+        if (v < k || (equal && v == k)) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Several chunks: an element's place is its own in its chunk and, in every other, the
+// number of smaller tokens, equal ones among them in the chunks before.
+__global__ __launch_bounds__(256) void token_merge_kernel(EmbBwdArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.M) return;
+    const int32_t k = a.key1[i];
+    const int64_t mine = i / kSortMax;
+    int64_t at = i - mine * kSortMax;
+    for (int64_t c = 0; c * kSortMax < a.M; c++)
+        if (c != mine) at += count_below(a.key1 + c * kSortMax, min((int64_t)kSortMax, a.M - c * kSortMax), k, c < mine);
+    a.order[at] = a.order1[i];
+    a.key[at] = k;
+}
+
+constexpr int kSumThreads = 256, kSumCols = kSumThreads * CH;
+
+// (2) A stretch of sorted rows, 2048 columns.  KIND: the number of columns is at least 8 (1), or not (0).
+template <typename T, typename TG, int KIND>
+__global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, int slices) {
+    constexpr int AHEAD = sizeof(T) == 4 ? 8 : 16;   // rows in flight
+    const int64_t s = blockIdx.x / (uint32_t)slices;
+    const int D = (int)a.D, c = (int)(blockIdx.x % (uint32_t)slices) * kSumCols + (int)threadIdx.x * CH;
+    const int64_t i0 = s * kRun;
+    const int n = (int)min((int64_t)kRun, a.M - i0);
+    const int32_t* key = a.key + i0;
+    const int32_t* order = a.order + i0;
+    const int32_t before = i0 > 0 ? key[-1] : -1, after = i0 + n < a.M ? key[n] : -1;
+    float sum[CH] = {};
+    bool first = true;    // no row of this stretch has ended a token yet
+    int32_t k = key[0];
+#pragma unroll 1
+    for (int j0 = 0; j0 < n; j0 += AHEAD) {
+        Piece<T> p[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            const T* row = (const T*)a.dy + (int64_t)order[min(j0 + j, n - 1)] * a.lddy;
+            if constexpr (KIND) p[j] = load_piece<T, false>(row, c, D);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            const int at = j0 + j;
+            if (at >= n) break;
+            float v[CH];
+            if constexpr (KIND) piece_values<T, false>(p[j], c, D, v);
+            else load_some((const T*)a.dy + (int64_t)order[at] * a.lddy + c, D - c, v);
+#pragma unroll
+            for (int e = 0; e < CH; e++) sum[e] += v[e];
+            const int32_t next = at + 1 < n ? key[at + 1] : after;
+            if (next == k && at + 1 < n) continue;
+            // the last row of token k here
+            const bool from = first && before == k, on = at + 1 == n && next == k;
+            if (c < D && k < a.V) {
+                if (from || on) {
+                    store_some(a.part + (2 * s + (from ? 0 : 1)) * a.D + c, D - c, sum);
+                } else {
+                    TG* row = (TG*)a.dtable + k * a.ldt + c;
+                    float old[CH];
+                    load_some(row, a.accumulate ? D - c : 0, old);
+#pragma unroll
+                    for (int e = 0; e < CH; e++) old[e] = __builtin_fmaf(a.alpha, sum[e], old[e]);
+                    store_some(row, D - c, old);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < CH; e++) sum[e] = 0.f;
+            first = false;
+            k = next;
+        }
+    }
+}
+
+// (3) The token that crosses the end of a stretch that it begins in: its partial sums in order.
+template <typename TG>
+__global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slices) {
+    const int64_t s = blockIdx.x / (uint32_t)slices;
+    const int c = (int)(blockIdx.x % (uint32_t)slices) * 1024 + (int)threadIdx.x * 4;
+    const int64_t i0 = s * kRun, end = i0 + kRun;   // (the last stretch crosses nothing)
+    if (end >= a.M) return;
+    const int32_t k = a.key[end];
+    if (a.key[end - 1] != k || k >= a.V || (i0 > 0 && a.key[i0 - 1] == k)) return;
+    const int64_t last = (end + count_below(a.key + end, a.M - end, k, true) - 1) / kRun;
+    if (c >= a.D) return;
+    const int left = (int)(a.D - c);
+    float sum[4];
+    load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
+    for (int64_t p = s + 1; p <= last; p += 8) {
+        float v[8][4];
+#pragma unroll
+        for (int i = 0; i < 8; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += p + i <= last ? v[i][e] : 0.f;
+    }
+    TG* row = (TG*)a.dtable + k * a.ldt + c;
+    float old[4];
+    load_some(row, a.accumulate ? left : 0, old);
+#pragma unroll
+    for (int e = 0; e < 4; e++) old[e] = __builtin_fmaf(a.alpha, sum[e], old[e]);
+    store_some(row, left, old);
+}
+
+// ---------------------------------------------------------------- launches
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+
+struct EmbSpace {
+    int64_t order, key, order1, key1, part, total;
+};
+EmbSpace emb_space(int64_t M, int64_t D) {
+    EmbSpace s{};
+    const bool chunks = M > kSortMax;
+    s.order = 0;
+    s.key = s.order + up256(M * 4);
+    s.order1 = s.key + up256(M * 4);
+    s.key1 = s.order1 + (chunks ? up256(M * 4) : 0);
+    s.part = s.key1 + (chunks ? up256(M * 4) : 0);
+    s.total = s.part + up256(ceil_div(M, kRun) * 2 * D * 4);
+    return s;
+}
+
+int sort_passes(int64_t V) {   // bytes of the largest key, V
+    int p = 1;
+    while (p < 4 && (V >> (8 * p)) > 0) p++;
+    return p;
+}
+
+constexpr int kSortLds = kSortMax * 8 + kSortWaves * kBins * 4 + 64;
+
+// Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
+template <auto kernel, int LDS>
+hipError_t allow_lds() {
+    static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
+template <typename TG>
+hipError_t run_sort(EmbBwdArgs& a, hipStream_t stream) {
+    const hipError_t e = allow_lds<token_sort_kernel<TG>, kSortLds>();
+    if (e != hipSuccess) return e;
+    a.sorters = (int32_t)ceil_div(a.M, kSortMax);
+    const int64_t n = a.M < kSortMax ? a.M : kSortMax;
+    const unsigned lds = (unsigned)(ceil_div(n, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 4 + 64);
+    const int64_t zeros = a.accumulate ? 0 : (a.V < 512 ? a.V : 512);
+    hipLaunchKernelGGL((token_sort_kernel<TG>), dim3((unsigned)(a.sorters + zeros)), dim3(kSortThreads), lds, stream, a);
+    return hipGetLastError();
+}
+
+template <typename T, typename TG>
+hipError_t run_sums(const EmbBwdArgs& a, hipStream_t stream) {
+    const int64_t runs = ceil_div(a.M, kRun);
+    const int slices = (int)ceil_div(a.D, kSumCols);
+    if (a.D >= CH)
+        hipLaunchKernelGGL((token_sum_kernel<T, TG, 1>), dim3((unsigned)(runs * slices)), dim3(kSumThreads), 0, stream, a, slices);
+    else
+        hipLaunchKernelGGL((token_sum_kernel<T, TG, 0>), dim3((unsigned)(runs * slices)), dim3(kSumThreads), 0, stream, a, slices);
+    return hipGetLastError();
+}
+
+template <typename TG>
+hipError_t run_join(const EmbBwdArgs& a, hipStream_t stream) {
+    const int64_t runs = ceil_div(a.M, kRun);
+    if (runs < 2) return hipSuccess;
+    const int slices = (int)ceil_div(a.D, 1024);
+    hipLaunchKernelGGL((token_join_kernel<TG>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices);
+    return hipGetLastError();
+}
+
+template <typename TT, typename T>
+hipError_t run_embedding(EmbArgs a, hipStream_t stream) {
+    // a launch holds fewer than 2^32 threads: very many rows go in slabs
+    const int64_t M = a.M, slab = ((int64_t)1 << 31) / a.ppr;
+    for (int64_t m0 = 0; m0 < M; m0 += slab) {
+        a.M = M - m0 < slab ? M - m0 : slab;
+        hipLaunchKernelGGL((embedding_kernel<TT, T>), dim3((unsigned)ceil_div(a.M * a.ppr, 256)), dim3(256), 0, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.tokens += slab;
+        a.out = (T*)a.out + slab * a.ldo;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t embedding_bwd_workspace(int64_t M, int64_t V, int64_t D) {
+    return M > 0 && V > 0 && D > 0 && M <= kMaxTokens && V < kMaxDim && D < kMaxLd ? (size_t)emb_space(M, D).total : 0;
+}
+
+}  // namespace niti
+
+using namespace niti;
+
+extern "C" {
+
+niti_status niti_embedding_fwd(const void* table, int64_t ldt, int table_type, const float* table_scale, const int32_t* tokens,
+                               void* out, int64_t ldout, int64_t M, int64_t V, int64_t D, float alpha, int type, void* stream) {
+    if (M < 0 || V < 1 || D < 1) return NITI_ERR_SHAPE;
+    if (!valid_type(type) || (table_type != NITI_I8 && !valid_type(table_type)) || !(alpha - alpha == 0.f)) return NITI_ERR_ARG;
+    if (M >= kMaxDim || V >= kMaxDim || D >= kMaxLd) return NITI_ERR_UNSUPPORTED;
+    if (M == 0) return NITI_OK;
+    if (!table || !tokens || !out || (table_type == NITI_I8) != (table_scale != nullptr)) return NITI_ERR_NULL;
+    if (bad_ld(V > 1 ? ldt : D, D, false) || bad_ld(M > 1 ? ldout : D, D, true)) return NITI_ERR_SHAPE;
+    const EmbArgs a{table, table_scale, tokens, out, V > 1 ? ldt : D, M > 1 ? ldout : D, M, V, D, (uint32_t)((D + CH - 1) / CH), alpha};
+    hipStream_t s = (hipStream_t)stream;
+    const hipError_t e = by_type(type, [&](auto t) {
+        using T = decltype(t);
+        if (table_type == NITI_I8) return run_embedding<int8_t, T>(a, s);
+        return by_type(table_type, [&](auto tt) { return run_embedding<decltype(tt), T>(a, s); });
+    });
+    return e == hipSuccess ? NITI_OK : NITI_ERR_HIP;
+}
+
+niti_status niti_embedding_bwd(const void* dy, int64_t lddy, int type, const int32_t* tokens, void* dtable, int64_t ldt, int dtable_type,
+                               int64_t M, int64_t V, int64_t D, float alpha, int accumulate, void* ws, size_t ws_bytes, void* stream) {
+    if (M < 0 || V < 1 || D < 1) return NITI_ERR_SHAPE;
+    if (!valid_type(type) || !valid_type(dtable_type) || !(alpha - alpha == 0.f)) return NITI_ERR_ARG;
+    if (M > kMaxTokens || V >= kMaxDim || D >= kMaxLd) return NITI_ERR_UNSUPPORTED;
+    if (M == 0 && accumulate) return NITI_OK;
+    if (!dtable || (M > 0 && (!dy || !tokens))) return NITI_ERR_NULL;
+    if ((M > 0 && bad_ld(M > 1 ? lddy : D, D, false)) || bad_ld(V > 1 ? ldt : D, D, true)) return NITI_ERR_SHAPE;
+    const EmbSpace w = emb_space(M, D);
+    if (M > 0 && (!ws || ws_bytes < (size_t)w.total)) return NITI_ERR_WORKSPACE;
+    if (M > 0 && ((uintptr_t)ws & 15)) return NITI_ERR_ARG;
+    char* base = (char*)ws;
+    const bool chunks = M > kSortMax;
+    hipStream_t s = (hipStream_t)stream;
+    EmbBwdArgs a{dy, tokens, dtable, M > 1 ? lddy : D, V > 1 ? ldt : D, M, V, D, alpha, accumulate != 0, sort_passes(V), 0,
+                 (int32_t*)(base + w.order), (int32_t*)(base + w.key), chunks ? (int32_t*)(base + w.order1) : nullptr,
+                 chunks ? (int32_t*)(base + w.key1) : nullptr, (float*)(base + w.part)};
+    hipError_t e = by_type(dtable_type, [&](auto g) { return run_sort<decltype(g)>(a, s); });
+    if (e == hipSuccess && chunks) {
+        hipLaunchKernelGGL(token_merge_kernel, dim3((unsigned)ceil_div(M, 256)), dim3(256), 0, s, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && M > 0)
+        e = by_type(dtable_type, [&](auto g) {
+            return by_type(type, [&](auto t) { return run_sums<decltype(t), decltype(g)>(a, s); });
+        });
+    if (e == hipSuccess && M > 0) e = by_type(dtable_type, [&](auto g) { return run_join<decltype(g)>(a, s); });
+    return e == hipSuccess ? NITI_OK : NITI_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,127 @@
+// Gated product of int8 rows: both projections of a feed-forward block, the
+// activation and the product in one kernel.
+//
+//   z[m][n] = s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n],  n < 2 F,   out[m][n] = act(z[m][n]) z[m][F + n]
+//
+// The kernels are those of the plain product with weight rows paired (see linear_tiles.h): the sums are
+// exact in int32, a is read once for both projections, and z reaches memory only where it is asked for.
+#include "linear_tiles.h"
+
+namespace niti {
+
+namespace {
+
+// What a call takes in each kernel (see the forms), N counting the weight rows.
+constexpr Cost kPair12{16, 32, kSpread, 1.92f, 0.61f, 0.95f, 1.33f};
+constexpr Cost kPair22{32, 32, kSpread, 2.06f, 0.75f, 1.18f, 1.90f};
+constexpr Cost kPairBytes12{16, 32, kSpread, 2.01f, 0.59f, 1.23f, 2.45f};
+constexpr Cost kPairBytes22{32, 32, kSpread, 2.02f, 0.86f, 1.39f, 3.48f};
+constexpr Cost kPair64{64, 128, kTwo, 2.09f, 1.8f, 1.6f, 2.6f};
+constexpr Cost kPairAny64{64, 64, kSpread, 2.84f, 1.02f, 3.38f, 4.07f};
+constexpr Cost kPair128{128, 128, kTwo, 0.96f, 3.17f, 3.79f, 3.45f};
+constexpr Cost kPairDeep128{128, 128, kRounds, 0.12f, 4.49f, 3.72f, 2.33f};
+constexpr Cost kPair256{256, 256, kRounds, 0.41f, 11.1f, 9.31f, 5.98f};
+
+struct Choice {
+    enum { kS12, kS22, k64, k128, k128d, k256 } kernel;
+    float time;
+    bool pack;   // the operands are copied to whole aligned pieces first
+};
+
+Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room) {
+    // columns of whole tiles: a half's last tile is not filled by the other half
+    const bool whole = rows == kOfPieces, words = rows != kOfBytes;
+    auto at = [&](const Cost& c) { return cost(c, M, (F + c.bn / 2 - 1) / (c.bn / 2) * c.bn, K); };
+    Choice c{Choice::kS12, at(words ? kPair12 : kPairBytes12), false};
+    auto take = [&](decltype(c.kernel) kernel, float time) {
+        if (time < c.time) c = Choice{kernel, time, false};
+    };
+    take(Choice::kS22, at(words ? kPair22 : kPairBytes22));
+    take(Choice::k64, at(whole ? kPair64 : kPairAny64));
+    if (whole) {
+        take(Choice::k128, at(kPair128));
+        take(Choice::k128d, at(kPairDeep128) * (M * F > 128 * 128 * 128 ? 1.08f : 1.f));
+        take(Choice::k256, at(kPair256));
+    }
+    const size_t copies = whole ? 0 : pack_bytes(M, 2 * F, K);
+    if (copies > 0 && copies <= room) {
+        Choice p = choose(M, F, up16(K), kOfPieces, 0);
+        p.time += 2.3f + (float)((double)copies * 2. / 3e6);   // (3 TB/s)
+        p.pack = true;
+        if (p.time < c.time) c = p;
+    }
+    return c;
+}
+
+template <typename T>
+hipError_t run_gated(const LinArgs& A, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const bool whole = ring_takes(A);
+    const Choice c = choose(A.M, A.N, A.K, whole ? kOfPieces : (word_rows(A) ? kOfWords : kOfBytes), ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0);
+    if (c.pack) {
+        const int64_t Kp = up16(A.K);
+        const uint32_t ppr = (uint32_t)(Kp / 16), pieces = (uint32_t)(A.M + 2 * A.N) * ppr;
+        hipLaunchKernelGGL(linear_pack_kernel, dim3((pieces + 255) / 256), dim3(256), 0, stream, A, ppr, pieces, (int8_t*)ws);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        LinArgs P = A;
+        P.a = (const int8_t*)ws, P.b = P.a + A.M * Kp;
+        P.lda = P.ldb = P.K = Kp;
+        return run_gated<T>(P, nullptr, 0, stream);
+    }
+    switch (c.kernel) {
+        case Choice::kS12: return run_small<T, 1, 2, true>(A, stream);
+        case Choice::kS22: return run_small<T, 2, 2, true>(A, stream);
+        case Choice::k64: return whole ? run_ring<T, 64, 128, 3, 2, 2, 128, true>(A, stream) : run_any<T, true>(A, stream);
+        case Choice::k128: return run_ring<T, 128, 128, 2, 4, 2, 128, true>(A, stream);
+        case Choice::k128d: return run_ring<T, 128, 128, 4, 4, 2, 128, true>(A, stream);
+        default: return run_ring<T, 256, 256, 4, 2, 4, 64, true>(A, stream);
+    }
+}
+
+}  // namespace
+
+// For copies of the operands, if that is how this product would go with room for them.
+size_t gated_fwd_workspace(int64_t M, int64_t F, int64_t K) {
+    if (M < 1 || F < 1 || K < 1 || M >= kMaxDim || F >= kMaxLd / 2 || K >= kMaxSum) return 0;
+    const bool pack = choose(M, F, K, kOfBytes, SIZE_MAX).pack || choose(M, F, K, kOfWords, SIZE_MAX).pack;
+    return pack ? pack_bytes(M, 2 * F, K) : 0;
+}
+
+}  // namespace niti
+
+using namespace niti;
+
+extern "C" {
+
+niti_status niti_gated_fwd(const int8_t* a, int64_t lda, const float* s_a, int64_t s_a_n, const int8_t* b, int64_t ldb, const float* s_b,
+                           int64_t s_b_n, const void* bias, int bias_type, int act, void* z, int64_t ldz, void* out, int64_t ldout,
+                           int64_t M, int64_t F, int64_t K, int type, void* ws, size_t ws_bytes, void* stream) {
+    if (M < 0 || F < 0 || K < 0) return NITI_ERR_SHAPE;
+    if (!valid_type(type) || (bias && !valid_type(bias_type)) || act < NITI_ACT_NONE || act > NITI_ACT_SILU) return NITI_ERR_ARG;
+    if (M >= kMaxDim || F >= kMaxLd / 2 || K >= kMaxSum) return NITI_ERR_UNSUPPORTED;
+    if (M == 0 || F == 0) return NITI_OK;
+    if (!s_a || !s_b || !out || (K > 0 && (!a || !b))) return NITI_ERR_NULL;
+    if ((s_a_n != 1 && s_a_n != M) || (s_b_n != 1 && s_b_n != 2 * F)) return NITI_ERR_SHAPE;
+    if (bad_ld(M > 1 ? lda : K, K, false) || bad_ld(ldb, K, false) || (z && bad_ld(M > 1 ? ldz : 2 * F, 2 * F, true)) ||
+        bad_ld(M > 1 ? ldout : F, F, true))
+        return NITI_ERR_SHAPE;
+    if (ws_bytes > 0 && !ws) return NITI_ERR_WORKSPACE;
+    LinArgs A{a, b, s_a, s_b, bias, nullptr, z, out, M > 1 ? lda : K, ldb, 0, ldz, ldout, M, F, K, s_a_n == 1 ? 0 : 1, s_b_n == 1 ? 0 : 1,
+              bias_type, act, 0, 0, 0};
+    // Very many rows go in slabs, so that a launch stays below 2^32 threads.
+    const int64_t size = (int64_t)type_size(type), tn = (F + 31) / 32;
+    int64_t slab = ((int64_t)1 << 22) / tn * 64;
+    if (slab < 64) slab = 64;
+    for (int64_t left = M; left > 0; left -= slab) {
+        A.M = left < slab ? left : slab;
+        const hipError_t e = by_type(type, [&](auto t) { return run_gated<decltype(t)>(A, ws, ws_bytes, (hipStream_t)stream); });
+        if (e != hipSuccess) return NITI_ERR_HIP;
+        A.a += slab * A.lda;
+        if (A.a_step) A.s_a += slab;
+        if (A.z) A.z = (char*)A.z + slab * A.ldz * size;
+        A.out = (char*)A.out + slab * A.ldout * size;
+    }
+    return NITI_OK;
+}
+
+}  // extern "C"

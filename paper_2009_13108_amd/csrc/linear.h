@@ -1,5 +1,5 @@
 // Internal interface of the product of int8 rows (linear.hip), which its
-// backward pass (linear_bwd.hip) calls too.
+// backward pass (linear_bwd.hip) calls too, and the workspaces of the row-wise operators.
 #pragma once
 
 #include "scaled.h"
@@ -8,7 +8,7 @@ namespace niti {
 
 struct LinArgs {
     const int8_t* a;     // [M][K]
-    const int8_t* b;     // [N][K]
+    const int8_t* b;     // [N][K]; of a gated product [2 N][K], and s_b, bias and z's columns likewise
     const float* s_a;    // scale of row m at s_a[m * a_step]; NULL: 1
     const float* s_b;
     const void* bias;    // [N] or NULL
@@ -31,5 +31,10 @@ hipError_t linear_run_pair(const LinArgs& a, const LinArgs& b, int type, void* w
 size_t linear_fwd_workspace(int64_t M, int64_t N, int64_t K);
 size_t linear_bwd_workspace(int64_t M, int64_t N, int64_t K);
 size_t rmsnorm_bwd_workspace(int64_t M, int64_t D);
+size_t gated_fwd_workspace(int64_t M, int64_t F, int64_t K);
+size_t gated_bwd_workspace(int64_t M, int64_t F, int64_t K);
+size_t embedding_bwd_workspace(int64_t M, int64_t V, int64_t D);
+size_t logprobs_workspace(int64_t M, int64_t V, int64_t top);
+size_t distill_workspace(int64_t M, int64_t V);
 
 }  // namespace niti

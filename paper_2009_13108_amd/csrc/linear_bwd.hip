@@ -6,6 +6,9 @@
 // Folding b's scale into the rows (it varies along their sum) and a's into the
 // columns leaves both sums with integers only.
 //
+// A gated product out = act(gate) up has dz in two halves, dy up act'(gate) and dy act(gate),
+// and goes the same way with both in one tile: dy and the halves of z are read once a pass.
+//
 // Up to five launches.  (1) Tiles of 16 x 256 of dz leave the maxima of their rows and
 // the maxima and sums of their columns; (2) those are joined, in a fixed order:
 // r, c and dbias; (3) dz is formed again, in tiles of 128 x 128, for the codes of
@@ -41,7 +44,8 @@ struct DzArgs {
     const float* s_a;
     const float* s_b;
     int64_t lddy, ldz;
-    int64_t M, N, Mp, Np;
+    int64_t M, N, Mp, Np;       // N: columns of dz
+    int64_t W;                  // columns of dy: N, or N / 2 of a gated product
     int64_t tiles_m, tiles_n;   // of step 1
     int32_t a_step, b_step;
     int32_t act, sr;
@@ -60,38 +64,55 @@ struct DzArgs {
 
 // dz of 8 columns from c on of rows m, m + step, ...; zeros past the edges.  All
 // loads go out before the first is used (see load_piece).  KIND: the number of
-// columns is a multiple of 8 (2), is at least 8 (1), or neither (0).
-template <typename T, int KIND, int ROWS>
+// columns of dy is a multiple of 8 (2), is at least 8 (1), or neither (0).
+// G: a gated product's two halves, dy up act'(gate) and dy act(gate), from three loads.
+template <typename T, int KIND, int ROWS, bool G>
 struct DzRows {
-    Piece<T> y[KIND ? ROWS : 1], z[KIND ? ROWS : 1];
+    static constexpr int H = G ? 2 : 1;
+    Piece<T> y[KIND ? ROWS : 1], z[KIND ? ROWS : 1], u[KIND && G ? ROWS : 1];
     __device__ __forceinline__ void load(const DzArgs& a, int64_t m, int64_t step, int c) {
         if constexpr (KIND > 0) {
 #pragma unroll
             for (int i = 0; i < ROWS; i++) {
                 const int64_t r = min(m + i * step, a.M - 1);
-                y[i] = load_piece<T, KIND == 2>((const T*)a.dy + r * a.lddy, c, (int)a.N);
-                z[i] = load_piece<T, KIND == 2>((const T*)a.z + r * a.ldz, c, (int)a.N);
+                y[i] = load_piece<T, KIND == 2>((const T*)a.dy + r * a.lddy, c, (int)a.W);
+                z[i] = load_piece<T, KIND == 2>((const T*)a.z + r * a.ldz, c, (int)a.W);
+                if constexpr (G) u[i] = load_piece<T, KIND == 2>((const T*)a.z + r * a.ldz + a.W, c, (int)a.W);
             }
         }
     }
-    __device__ __forceinline__ void get(const DzArgs& a, int i, int64_t m, int c, float (&d)[CH]) {
-        const int N = (int)a.N;
-        float s[CH];
+    __device__ __forceinline__ void get(const DzArgs& a, int i, int64_t m, int c, float (&d)[H][CH]) {
+        const int W = (int)a.W;
+        float s[CH], v[CH];
         if constexpr (KIND > 0) {
-            piece_values<T, KIND == 2>(y[i], c, N, d);
-            piece_values<T, KIND == 2>(z[i], c, N, s);
+            piece_values<T, KIND == 2>(y[i], c, W, d[0]);
+            piece_values<T, KIND == 2>(z[i], c, W, s);
+            if constexpr (G) piece_values<T, KIND == 2>(u[i], c, W, v);
         } else {
             const int64_t r = min(m, a.M - 1);
-            load_some((const T*)a.dy + r * a.lddy + c, N - c, d);
-            if (a.act != NITI_ACT_NONE) load_some((const T*)a.z + r * a.ldz + c, N - c, s);
+            load_some((const T*)a.dy + r * a.lddy + c, W - c, d[0]);
+            if (G || a.act != NITI_ACT_NONE) load_some((const T*)a.z + r * a.ldz + c, W - c, s);
+            if constexpr (G) load_some((const T*)a.z + r * a.ldz + a.W + c, W - c, v);
+        }
+        if constexpr (G) {
+#pragma unroll
+            for (int e = 0; e < CH; e++) d[1][e] = s[e];
+            act_values(a.act, d[1]);
+#pragma unroll
+            for (int e = 0; e < CH; e++) {
+                d[1][e] *= d[0][e];
+                d[0][e] *= v[e];
+            }
         }
         if (a.act != NITI_ACT_NONE) {
             act_slopes(a.act, s);
 #pragma unroll
-            for (int e = 0; e < CH; e++) d[e] *= s[e];
+            for (int e = 0; e < CH; e++) d[0][e] *= s[e];
         }
 #pragma unroll
-        for (int e = 0; e < CH; e++) d[e] = m < a.M ? d[e] : 0.f;
+        for (int h = 0; h < H; h++)
+#pragma unroll
+            for (int e = 0; e < CH; e++) d[h][e] = m < a.M ? d[h][e] : 0.f;
     }
 };
 
@@ -110,51 +131,62 @@ __device__ __forceinline__ void load_cols(const float* p, int step, int c, int N
 }
 
 // Step 1.  A thread takes 8 columns of 2 rows; 32 lanes a row, 8 threads a column group.
-template <typename T, int KIND>
+template <typename T, int KIND, bool G>
 __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
-    __shared__ float ssum[8][SC + 8];
-    __shared__ uint32_t smax[8][SC + 8];
+    constexpr int H = G ? 2 : 1;
+    __shared__ float ssum[H][8][SC + 8];
+    __shared__ uint32_t smax[H][8][SC + 8];
     const int64_t tm = blockIdx.x / (uint32_t)a.tiles_n, tn = blockIdx.x % (uint32_t)a.tiles_n;
     const int col = (threadIdx.x & 31) * CH, grp = threadIdx.x >> 5;
     const int c = (int)(tn * SC + col);
-    DzRows<T, KIND, SR / 8> rows;
+    DzRows<T, KIND, SR / 8, G> rows;
     rows.load(a, tm * SR + grp, 8, c);
-    float sb[CH], sum[CH], sa[SR / 8];
-    uint32_t mx[CH];
+    float sb[H][CH], sum[H][CH], sa[SR / 8];
+    uint32_t mx[H][CH];
 #pragma unroll
     for (int i = 0; i < SR / 8; i++) sa[i] = a.s_a[a.a_step ? min(tm * SR + i * 8 + grp, a.M - 1) : 0];
-    load_cols<KIND>(a.s_b, a.b_step, c, (int)a.N, sb);
 #pragma unroll
-    for (int e = 0; e < CH; e++) sum[e] = 0.f, mx[e] = 0;
+    for (int h = 0; h < H; h++) {
+        load_cols<KIND>(a.s_b + (a.b_step ? h * a.W : 0), a.b_step, c, (int)a.W, sb[h]);
+#pragma unroll
+        for (int e = 0; e < CH; e++) sum[h][e] = 0.f, mx[h][e] = 0;
+    }
 #pragma unroll
     for (int i = 0; i < SR / 8; i++) {
         const int64_t m = tm * SR + i * 8 + grp;
-        float d[CH];
+        float d[H][CH];
         rows.get(a, i, m, c, d);
         uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < CH; e++) {
-            sum[e] += d[e];
-            mx[e] = max(mx[e], mag_bits(d[e] * sa[i]));
-            top = max(top, mag_bits(d[e] * sb[e]));   // (zeros past the edges)
-        }
+        for (int h = 0; h < H; h++)
+#pragma unroll
+            for (int e = 0; e < CH; e++) {
+                sum[h][e] += d[h][e];
+                mx[h][e] = max(mx[h][e], mag_bits(d[h][e] * sa[i]));
+                top = max(top, mag_bits(d[h][e] * sb[h][e]));   // (zeros past the edges)
+            }
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 32));
         if ((threadIdx.x & 31) == 0 && m < a.M) a.rmax[tn * a.M + m] = top;
     }
 #pragma unroll
-    for (int e = 0; e < CH; e++) ssum[grp][col + e] = sum[e], smax[grp][col + e] = mx[e];
+    for (int h = 0; h < H; h++)
+#pragma unroll
+        for (int e = 0; e < CH; e++) ssum[h][grp][col + e] = sum[h][e], smax[h][grp][col + e] = mx[h][e];
     __syncthreads();
     const int64_t cc = tn * SC + threadIdx.x;
-    if (cc < a.N) {
-        float s = ssum[0][threadIdx.x];
-        uint32_t m = smax[0][threadIdx.x];
-        for (int g = 1; g < 8; g++) {
-            s += ssum[g][threadIdx.x];
-            m = max(m, smax[g][threadIdx.x]);
+    if (cc < a.W) {
+#pragma unroll
+        for (int h = 0; h < H; h++) {
+            float s = ssum[h][0][threadIdx.x];
+            uint32_t m = smax[h][0][threadIdx.x];
+            for (int g = 1; g < 8; g++) {
+                s += ssum[h][g][threadIdx.x];
+                m = max(m, smax[h][g][threadIdx.x]);
+            }
+            a.csum[tm * a.N + h * a.W + cc] = s;
+            a.cmax[tm * a.N + h * a.W + cc] = m;
         }
-        a.csum[tm * a.N + cc] = s;
-        a.cmax[tm * a.N + cc] = m;
     }
 }
 
@@ -282,29 +314,31 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
 }
 
 // Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
-template <typename T, int KIND>
+template <typename T, int KIND, bool G>
 __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int codes, int tiles_c) {
-    __shared__ __attribute__((aligned(16))) int8_t tile[CT][CP];
-    __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[CT];
+    constexpr int H = G ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) int8_t tile[H][CT][CP];
+    __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[H * CT];
     int block = blockIdx.x;
     if (block >= codes) {   // the codes' tiles, which take longest, are first
         block -= codes;
-        if (block < ta.blocks) turn_tile(ta, block, tile);
-        else turn_tile(tb, block - ta.blocks, tile);
+        if (block < ta.blocks) turn_tile(ta, block, tile[0]);
+        else turn_tile(tb, block - ta.blocks, tile[0]);
         return;
     }
     const int64_t m0 = (int64_t)((uint32_t)block / (uint32_t)tiles_c) * CT, n0 = (int64_t)((uint32_t)block % (uint32_t)tiles_c) * CT;
     const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 4;   // 8 columns of 4 rows a thread
     const int c = (int)(n0 + col);
-    float sb[CH], ci[CH], sa[4];
-    DzRows<T, KIND, 4> rows;
+    float sb[H][CH], ci[H][CH], sa[4];
+    DzRows<T, KIND, 4, G> rows;
     rows.load(a, m0 + row0, 1, c);
 #pragma unroll
     for (int i = 0; i < 4; i++) sa[i] = a.s_a[a.a_step ? min(m0 + row0 + i, a.M - 1) : 0];
-    load_cols<KIND>(a.s_b, a.b_step, c, (int)a.N, sb);
-    {   // the tile's factors: 128 threads a row each, 128 a column
-        const int i = threadIdx.x & (CT - 1);
-        const int64_t m = min(m0 + i, a.M - 1), n = min(n0 + i, a.N - 1);
+#pragma unroll
+    for (int h = 0; h < H; h++) load_cols<KIND>(a.s_b + (a.b_step ? h * a.W : 0), a.b_step, c, (int)a.W, sb[h]);
+    {   // the tile's factors: 128 threads a row each, 128 a column (of each half)
+        const int i = threadIdx.x & (CT - 1), half = G ? (int)threadIdx.x / CT - 1 : 0;
+        const int64_t m = min(m0 + i, a.M - 1), n = half * a.W + min(n0 + i, a.W - 1);
         if (threadIdx.x < CT) {
             float inv;
             if (a.join) {
@@ -315,7 +349,7 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
                 inv = a.r[a.M + m];
             }
             rinv[i] = inv;
-        } else if (threadIdx.x < 2 * CT) {
+        } else if (threadIdx.x < (1 + H) * CT) {
             float inv;
             if (a.join) {
                 float s = 0.f;
@@ -330,7 +364,7 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
                     mx = max(mx, max(a.cmax[g * a.N + n], a.cmax[two * a.N + n]));
                 }
                 const RowScale rs = row_scale(mx);
-                if (m0 == 0 && n0 + i < a.N) {
+                if (m0 == 0 && n0 + i < a.W) {
                     a.c[n] = rs.scale;
                     if (a.dbias) a.dbias[n] = s;
                 }
@@ -338,79 +372,98 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
             } else {
                 inv = a.c[a.N + n];
             }
-            cinv[i] = n0 + i < a.N ? inv : 0.f;
+            cinv[half * CT + i] = n0 + i < a.W ? inv : 0.f;
         }
     }
     __syncthreads();
+    uint32_t cmask[H][2] = {};
 #pragma unroll
-    for (int e = 0; e < CH; e++) ci[e] = cinv[col + e];
-    uint32_t cmask[2] = {0, 0};
+    for (int h = 0; h < H; h++)
 #pragma unroll
-    for (int e = 0; e < CH; e++) cmask[e >> 2] |= (code_mask(ci[e]) & 0xFFu) << (8 * (e & 3));
-    uint32_t qc[4][2];   // codes of the columns: four rows of eight bytes
+        for (int e = 0; e < CH; e++) {
+            ci[h][e] = cinv[h * CT + col + e];
+            cmask[h][e >> 2] |= (code_mask(ci[h][e]) & 0xFFu) << (8 * (e & 3));
+        }
+    uint32_t qc[H][4][2];   // codes of the columns: four rows of eight bytes
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const int64_t m = m0 + row0 + i;
         const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
-        float d[CH], pc[CH], cc[CH];
+        float d[H][CH];
         rows.get(a, i, m, c, d);
         const float ri = rinv[row0 + i];
-        if (a.sr) {
-            DrawStream r(a.seed, a.call, (uint64_t)(m * a.N + c));
 #pragma unroll
-            for (int e = 0; e < CH; e++) {
-                const uint64_t u = r.next();
-                pc[e] = code_sr(d[e] * sb[e], ri, draw_hi(u));
-                cc[e] = code_sr(d[e] * sa[i], ci[e], draw_lo(u));
-            }
-        } else {
+        for (int h = 0; h < H; h++) {
+            float pc[CH], cc[CH];
+            if (a.sr) {
+                DrawStream r(a.seed, a.call, (uint64_t)(m * a.N + h * a.W + c));
 #pragma unroll
-            for (int e = 0; e < CH; e++) {
-                pc[e] = code_rtn(d[e] * sb[e], ri);
-                cc[e] = code_rtn(d[e] * sa[i], ci[e]);
+                for (int e = 0; e < CH; e++) {
+                    const uint64_t u = r.next();
+                    pc[e] = code_sr(d[h][e] * sb[h][e], ri, draw_hi(u));
+                    cc[e] = code_sr(d[h][e] * sa[i], ci[h][e], draw_lo(u));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < CH; e++) {
+                    pc[e] = code_rtn(d[h][e] * sb[h][e], ri);
+                    cc[e] = code_rtn(d[h][e] * sa[i], ci[h][e]);
+                }
             }
+            // (past the edges dz is 0, and so are the codes: a draw is below 1)
+            if (a.p && in) {
+                const uint32_t mask = code_mask(ri);
+                const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
+                // a gate's row of codes ends where its partner's begins, that one's (or the only one) where the padding does
+                const int end = G && h == 0 ? (int)a.W : (int)(a.Np - h * a.W);
+                int8_t* dst = a.p + m * a.Np + h * a.W + c;
+                if (!G || c + CH <= end) {
+                    if (c < end) __builtin_memcpy(dst, w, CH);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < CH; e++)
+                        if (c + e < end) dst[e] = (int8_t)(w[e >> 2] >> (8 * (e & 3)));
+                }
+            }
+            qc[h][i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[h][0];
+            qc[h][i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[h][1];
         }
-        // (past the edges dz is 0, and so are the codes: a draw is below 1)
-        if (a.p && in && c < a.Np) {
-            const uint32_t mask = code_mask(ri);
-            const uint32_t w[2] = {pack4(pc[0], pc[1], pc[2], pc[3]) & mask, pack4(pc[4], pc[5], pc[6], pc[7]) & mask};
-            __builtin_memcpy(a.p + m * a.Np + c, w, CH);
-        }
-        qc[i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[0];
-        qc[i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[1];
     }
 #pragma unroll
-    for (int g = 0; g < 2; g++) {
-        uint32_t w[4] = {qc[0][g], qc[1][g], qc[2][g], qc[3][g]};
-        turn4(w);
+    for (int h = 0; h < H; h++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) *(uint32_t*)&tile[col + 4 * g + i][row0] = w[i];
-    }
+        for (int g = 0; g < 2; g++) {
+            uint32_t w[4] = {qc[h][0][g], qc[h][1][g], qc[h][2][g], qc[h][3][g]};
+            turn4(w);
+#pragma unroll
+            for (int i = 0; i < 4; i++) *(uint32_t*)&tile[h][col + 4 * g + i][row0] = w[i];
+        }
     if (!a.q) return;
     __syncthreads();
-    store_turned(tile, a.q, a.Mp, n0, a.N, m0, a.Mp);
+#pragma unroll
+    for (int h = 0; h < H; h++) store_turned(tile[h], a.q, a.Mp, h * a.W + n0, (h + 1) * a.W, m0, a.Mp);
 }
 
 // Calls f with the column count's KIND.
 template <typename F>
-hipError_t by_kind(int64_t N, F f) {
-    if (N % CH == 0) return f(std::integral_constant<int, 2>());
-    if (N > CH) return f(std::integral_constant<int, 1>());
+hipError_t by_kind(int64_t W, F f) {
+    if (W % CH == 0) return f(std::integral_constant<int, 2>());
+    if (W > CH) return f(std::integral_constant<int, 1>());
     return f(std::integral_constant<int, 0>());
 }
 
-template <typename T>
+template <typename T, bool G>
 hipError_t run_stats(const DzArgs& a, hipStream_t stream) {
-    return by_kind(a.N, [&](auto k) {
-        hipLaunchKernelGGL((dz_stats_kernel<T, decltype(k)::value>), dim3((unsigned)(a.tiles_m * a.tiles_n)), dim3(256), 0, stream, a);
+    return by_kind(a.W, [&](auto k) {
+        hipLaunchKernelGGL((dz_stats_kernel<T, decltype(k)::value, G>), dim3((unsigned)(a.tiles_m * a.tiles_n)), dim3(256), 0, stream, a);
         return hipGetLastError();
     });
 }
 
-template <typename T>
+template <typename T, bool G>
 hipError_t run_codes(const DzArgs& a, const Turn& ta, const Turn& tb, int64_t tiles, int tiles_c, hipStream_t stream) {
-    return by_kind(a.N, [&](auto k) {
-        hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(CTH), 0,
+    return by_kind(a.W, [&](auto k) {
+        hipLaunchKernelGGL((dz_codes_kernel<T, decltype(k)::value, G>), dim3((unsigned)(ta.blocks + tb.blocks + tiles)), dim3(CTH), 0,
                            stream, a, ta, tb, (int)tiles, tiles_c);
         return hipGetLastError();
     });
@@ -421,12 +474,13 @@ struct BwdSpace {
     int64_t p, q, at, bt, r, c, rmax, cmax, csum, sums, sums_bytes, total;
 };
 
-BwdSpace space(int64_t M, int64_t N, int64_t K) {
+// W: columns of dy.
+BwdSpace space(int64_t M, int64_t N, int64_t W, int64_t K) {
     BwdSpace s;
     s.Mp = up(M, kPad);
     s.Np = up(N, kPad);
     s.tiles_m = (M + SR - 1) / SR;
-    s.tiles_n = (N + SC - 1) / SC;
+    s.tiles_n = (W + SC - 1) / SC;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t o = at;
@@ -453,16 +507,17 @@ BwdSpace space(int64_t M, int64_t N, int64_t K) {
 }  // namespace
 
 size_t linear_bwd_workspace(int64_t M, int64_t N, int64_t K) {
-    return M > 0 && N > 0 && K >= 0 && M < kMaxSum && N < kMaxSum && K < kMaxLd ? (size_t)space(M, N, K).total : 0;
+    return M > 0 && N > 0 && K >= 0 && M < kMaxSum && N < kMaxSum && K < kMaxLd ? (size_t)space(M, N, N, K).total : 0;
+}
+size_t gated_bwd_workspace(int64_t M, int64_t F, int64_t K) {
+    return M > 0 && F > 0 && K >= 0 && M < kMaxSum && F < kMaxSum / 2 && K < kMaxLd ? (size_t)space(M, 2 * F, F, K).total : 0;
 }
 
-}  // namespace niti
+namespace {
 
-using namespace niti;
-
-extern "C" {
-
-niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, const int8_t* a,
+// G: N counts the columns of dz, gates and their partners.
+template <bool G>
+niti_status linear_backward(const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, const int8_t* a,
                             int64_t lda, const float* s_a, int64_t s_a_n, const int8_t* b, int64_t ldb,
                             const float* s_b, int64_t s_b_n, void* da, int64_t ldda, void* db, int64_t lddb,
                             float* dbias, int64_t M, int64_t N, int64_t K, niti_round_mode mode, uint64_t seed,
@@ -471,6 +526,7 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     if (!valid_type(type) || act < NITI_ACT_NONE || act > NITI_ACT_SILU) return NITI_ERR_ARG;
     if (mode != NITI_ROUND_RTN && mode != NITI_ROUND_SR) return NITI_ERR_ARG;
     if (M >= kMaxSum || N >= kMaxSum || K >= kMaxLd) return NITI_ERR_UNSUPPORTED;
+    const int64_t W = G ? N / 2 : N;   // columns of dy
     hipStream_t s = (hipStream_t)stream;
     if (K == 0) da = db = nullptr;
     if (M == 0 || N == 0) {   // sums of nothing
@@ -494,22 +550,23 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
         }
         return NITI_OK;
     }
-    if (!dy || !s_a || !s_b || (act != NITI_ACT_NONE && !z) || (db && !a) || (da && !b)) return NITI_ERR_NULL;
+    const bool has_z = G || act != NITI_ACT_NONE;
+    if (!dy || !s_a || !s_b || (has_z && !z) || (db && !a) || (da && !b)) return NITI_ERR_NULL;
     if ((s_a_n != 1 && s_a_n != M) || (s_b_n != 1 && s_b_n != N)) return NITI_ERR_SHAPE;
-    if (bad_ld(M > 1 ? lddy : N, N, false) || (act != NITI_ACT_NONE && bad_ld(M > 1 ? ldz : N, N, false)) ||
+    if (bad_ld(M > 1 ? lddy : W, W, false) || (has_z && bad_ld(M > 1 ? ldz : N, N, false)) ||
         (db && bad_ld(M > 1 ? lda : K, K, false)) || (da && bad_ld(N > 1 ? ldb : K, K, false)) ||
         (da && bad_ld(M > 1 ? ldda : K, K, true)) || (db && bad_ld(N > 1 ? lddb : K, K, true)))
         return NITI_ERR_SHAPE;
-    const BwdSpace w = space(M, N, K);
+    const BwdSpace w = space(M, N, W, K);
     if (!ws || ws_bytes < (size_t)w.total) return NITI_ERR_WORKSPACE;
     if ((uintptr_t)ws & 15) return NITI_ERR_ARG;
     if (!da && !db && !dbias) return NITI_OK;
     char* base = (char*)ws;
     DzArgs d{};
     // without an activation dy stands for z, so that the kernels' loads need no branch
-    d.dy = dy, d.z = act != NITI_ACT_NONE ? z : dy, d.s_a = s_a, d.s_b = s_b;
-    d.lddy = lddy, d.ldz = act != NITI_ACT_NONE ? ldz : lddy;
-    d.M = M, d.N = N, d.Mp = w.Mp, d.Np = w.Np;
+    d.dy = dy, d.z = has_z ? z : dy, d.s_a = s_a, d.s_b = s_b;
+    d.lddy = lddy, d.ldz = has_z ? ldz : lddy;
+    d.M = M, d.N = N, d.W = W, d.Mp = w.Mp, d.Np = w.Np;
     d.a_step = s_a_n == 1 ? 0 : 1, d.b_step = s_b_n == 1 ? 0 : 1;
     d.act = act, d.sr = mode == NITI_ROUND_SR, d.seed = seed, d.call = call;
     d.tiles_m = w.tiles_m, d.tiles_n = w.tiles_n;
@@ -521,7 +578,7 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
     d.rmax = (uint32_t*)(base + w.rmax);
     d.cmax = (uint32_t*)(base + w.cmax);
     d.csum = (float*)(base + w.csum);
-    if (by_type(type, [&](auto t) { return run_stats<decltype(t)>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
+    if (by_type(type, [&](auto t) { return run_stats<decltype(t), G>(d, s); }) != hipSuccess) return NITI_ERR_HIP;
     // Tiles of step 3 read those of step 1 that they lie in, each again: up to 32 by 40 of them (512 x 10240) that takes
     // less than a launch (250 x 4096 x 512 26.3 -> 24.5 us, 200 x 9000 x 1024 45.2 -> 42.9, 400 x 1024 x 512 18.2 -> 16.5,
     // 512 x 10240 x 512 44.6 -> 42.7).
@@ -532,10 +589,11 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
         if (hipGetLastError() != hipSuccess) return NITI_ERR_HIP;
     }
     if (!da && !db) return NITI_OK;
-    const int64_t tr = (M + CT - 1) / CT, tc = (N + CT - 1) / CT, tk = (K + CT - 1) / CT;
+    // (a gated product's last columns are followed by the padding of the rows of codes)
+    const int64_t tr = (M + CT - 1) / CT, tn = (N + CT - 1) / CT, tc = G ? (w.Np - W + CT - 1) / CT : tn, tk = (K + CT - 1) / CT;
     Turn ta{a, (int8_t*)(base + w.at), lda, M, w.Mp, K, db ? (int32_t)(tr * tk) : 0, (int32_t)tk};
-    Turn tb{b, (int8_t*)(base + w.bt), ldb, N, w.Np, K, da ? (int32_t)(tc * tk) : 0, (int32_t)tk};
-    if (by_type(type, [&](auto t) { return run_codes<decltype(t)>(d, ta, tb, tr * tc, (int)tc, s); }) != hipSuccess)
+    Turn tb{b, (int8_t*)(base + w.bt), ldb, N, w.Np, K, da ? (int32_t)(tn * tk) : 0, (int32_t)tk};
+    if (by_type(type, [&](auto t) { return run_codes<decltype(t), G>(d, ta, tb, tr * tc, (int)tc, s); }) != hipSuccess)
         return NITI_ERR_HIP;
     const LinArgs B{d.q, ta.t, d.c, nullptr, nullptr, nullptr, nullptr, db, w.Mp, w.Mp, 0, 0, lddb, N, K, w.Mp, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
     const LinArgs A{d.p, tb.t, d.r, nullptr, nullptr, nullptr, nullptr, da, w.Np, w.Np, 0, 0, ldda, M, K, w.Np, 1, 0, 0, NITI_ACT_NONE, 0, 0, 0};
@@ -544,6 +602,32 @@ niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t
                                   : linear_run(da ? A : B, type, sums, (size_t)w.sums_bytes, s);
     if (e != hipSuccess) return NITI_ERR_HIP;
     return NITI_OK;
+}
+
+}  // namespace
+
+}  // namespace niti
+
+using namespace niti;
+
+extern "C" {
+
+niti_status niti_linear_bwd(const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, const int8_t* a,
+                            int64_t lda, const float* s_a, int64_t s_a_n, const int8_t* b, int64_t ldb,
+                            const float* s_b, int64_t s_b_n, void* da, int64_t ldda, void* db, int64_t lddb,
+                            float* dbias, int64_t M, int64_t N, int64_t K, niti_round_mode mode, uint64_t seed,
+                            uint32_t call, int type, void* ws, size_t ws_bytes, void* stream) {
+    return linear_backward<false>(dy, lddy, z, ldz, act, a, lda, s_a, s_a_n, b, ldb, s_b, s_b_n, da, ldda, db, lddb, dbias, M, N, K,
+                                  mode, seed, call, type, ws, ws_bytes, stream);
+}
+
+niti_status niti_gated_bwd(const void* dy, int64_t lddy, const void* z, int64_t ldz, int act, const int8_t* a, int64_t lda,
+                           const float* s_a, int64_t s_a_n, const int8_t* b, int64_t ldb, const float* s_b, int64_t s_b_n, void* da,
+                           int64_t ldda, void* db, int64_t lddb, float* dbias, int64_t M, int64_t F, int64_t K, niti_round_mode mode,
+                           uint64_t seed, uint32_t call, int type, void* ws, size_t ws_bytes, void* stream) {
+    if (F >= kMaxSum / 2) return NITI_ERR_UNSUPPORTED;
+    return linear_backward<true>(dy, lddy, z, ldz, act, a, lda, s_a, s_a_n, b, ldb, s_b, s_b_n, da, ldda, db, lddb, dbias, M, 2 * F, K,
+                                 mode, seed, call, type, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

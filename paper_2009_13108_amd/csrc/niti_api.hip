@@ -202,6 +202,16 @@ size_t niti_workspace_bytes(int op, const niti_conv_desc* d, int64_t M, int64_t 
             return linear_fwd_workspace(M, N, K);
         case NITI_OP_LINEAR_BWD:
             return linear_bwd_workspace(M, N, K);
+        case NITI_OP_GATED_FWD:
+            return gated_fwd_workspace(M, N, K);
+        case NITI_OP_GATED_BWD:
+            return gated_bwd_workspace(M, N, K);
+        case NITI_OP_EMBEDDING_BWD:
+            return embedding_bwd_workspace(M, N, K);
+        case NITI_OP_TOKEN_LOGPROBS:
+            return logprobs_workspace(M, N, K);
+        case NITI_OP_DISTILL_FWD:
+            return distill_workspace(M, N);
         default:
             return 0;
     }

@@ -34,10 +34,16 @@ OP_INT_CE_LOSS = 4
 OP_RMSNORM_BWD = 5
 OP_LINEAR_FWD = 6
 OP_LINEAR_BWD = 7
+OP_GATED_FWD = 8
+OP_GATED_BWD = 9
+OP_EMBEDDING_BWD = 10
+OP_TOKEN_LOGPROBS = 11
+OP_DISTILL_FWD = 12
 
 F32 = 0
 BF16 = 1
 F16 = 2
+I8 = 3
 
 ACT_NONE = 0
 ACT_RELU = 1
@@ -100,7 +106,8 @@ EXPORTS = [
     "niti_status_str", "niti_quantize_u8", "niti_maxpool2_fwd", "niti_maxpool2_bwd",
     "niti_relu_mask", "niti_dropout_fwd", "niti_dropout_bwd", "niti_stats_bytes", "niti_timing_enable", "niti_timing_read", "niti_timing_record",
     "niti_mfma_loop", "niti_rmsnorm_fwd", "niti_rmsnorm_bwd", "niti_quantize_rows", "niti_linear_fwd",
-    "niti_linear_bwd", "niti_adamw_step", "niti_adamw_read",
+    "niti_linear_bwd", "niti_adamw_step", "niti_adamw_read", "niti_gated_fwd", "niti_gated_bwd", "niti_embedding_fwd",
+    "niti_embedding_bwd", "niti_token_logprobs", "niti_distill_fwd", "niti_distill_bwd",
 ]
 
 TIMING_IGEMM = 0
@@ -148,6 +155,14 @@ def lib():
                                     P],
                 "niti_linear_bwd": [P, I64, P, I64, I, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I,
                                     ctypes.c_uint64, ctypes.c_uint32, I, P, Z, P],
+                "niti_gated_fwd": [P, I64, P, I64, P, I64, P, I64, P, I, I, P, I64, P, I64, I64, I64, I64, I, P, Z, P],
+                "niti_gated_bwd": [P, I64, P, I64, I, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, P, I64, I64, I64, I,
+                                   ctypes.c_uint64, ctypes.c_uint32, I, P, Z, P],
+                "niti_embedding_fwd": [P, I64, I, P, P, P, I64, I64, I64, I64, ctypes.c_float, I, P],
+                "niti_embedding_bwd": [P, I64, I, P, P, I64, I, I64, I64, I64, ctypes.c_float, I, P, Z, P],
+                "niti_token_logprobs": [P, I64, P, P, P, P, P, P, I64, I64, I64, ctypes.c_float, I, P, Z, P],
+                "niti_distill_fwd": [P, I64, P, I64, I, P, I64, P, P, P, I64, P, I64, I64, I64, I64, ctypes.c_float, I, P, Z, P],
+                "niti_distill_bwd": [P, I64, P, I64, I, P, I64, P, P, I64, P, I64, I64, I64, I64, ctypes.c_float, I, P],
                 "niti_adamw_step": [P, I64, I, I, I, I64, D, D, D, D, D, P, I, ctypes.c_uint64, P],
                 "niti_adamw_read": [P, I64, I, P],
             }
@@ -777,6 +792,142 @@ def linear_bwd(dy, a, b, s_a, s_b, ws, z=None, act=ACT_NONE, da=None, db=None, d
     pws, nws = _ws_args(ws, dev)
     _run("niti_linear_bwd", pdy, lddy, pz, ldz, act, pa, lda, psa, nsa, pb, ldb, psb, nsb, pda, ldda, pdb, lddb,
          _vec(dbias, dev, N, "dbias", f32), M, N, K, mode, seed & 0xFFFFFFFFFFFFFFFF, call & 0xFFFFFFFF, kind, pws, nws,
+         _stream(stream))
+
+
+def gated_fwd(a, b, out, s_a, s_b, act=ACT_SILU, bias=None, z=None, ws=None, stream=None):
+    """out = act(gate) * up, where b [2F][K] holds the rows of both projections, the gates' first:
+    [gate up] = z = s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n]; ws as
+    workspace_bytes(OP_GATED_FWD, None, M, F, K), or None (niti_gated_fwd)."""
+    (M, K), dev = _matrix(a, "a")
+    F = _width(out, 1, "out")
+    i8, dt = _torch_mod.int8, out.dtype
+    kind = _type_of(dt, "out")
+    pa, lda = _mat(a, dev, i8, (M, K), "a")
+    pb, ldb = _mat(_given(b, "b"), dev, i8, (2 * F, K), "b")
+    po, ldo = _mat(out, dev, dt, (M, F), "out", True)
+    pz, ldz = _mat(z, dev, dt, (M, 2 * F), "z", True)
+    psa, nsa = _scales(s_a, dev, M, "s_a")
+    psb, nsb = _scales(s_b, dev, 2 * F, "s_b")
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_gated_fwd", pa, lda, psa, nsa, pb, ldb, psb, nsb, _vec(bias, dev, 2 * F, "bias"),
+         F32 if bias is None else _type_of(bias.dtype, "bias"), act, pz, ldz, po, ldo, M, F, K, kind, pws, nws, _stream(stream))
+
+
+def gated_bwd(dy, z, a, b, s_a, s_b, ws, act=ACT_SILU, da=None, db=None, dbias=None, mode=RTN, seed=0, call=0, stream=None):
+    """Gradients of the values that a and b [2F][K] stand for and of the bias [2F], from gated_fwd's z,
+    by int8 products; ws as workspace_bytes(OP_GATED_BWD, None, M, F, K) (niti_gated_bwd)."""
+    (M, F), dev = _matrix(dy, "dy")
+    K = _width(a, 1, "a")
+    i8, f32, dt = _torch_mod.int8, _torch_mod.float32, dy.dtype
+    kind = _type_of(dt, "dy")
+    pdy, lddy = _mat(dy, dev, dt, (M, F), "dy")
+    pz, ldz = _mat(_given(z, "z"), dev, dt, (M, 2 * F), "z")
+    pa, lda = _mat(a, dev, i8, (M, K), "a")
+    pb, ldb = _mat(_given(b, "b"), dev, i8, (2 * F, K), "b")
+    pda, ldda = _mat(da, dev, dt, (M, K), "da", True)
+    pdb, lddb = _mat(db, dev, dt, (2 * F, K), "db", True)
+    psa, nsa = _scales(s_a, dev, M, "s_a")
+    psb, nsb = _scales(s_b, dev, 2 * F, "s_b")
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_gated_bwd", pdy, lddy, pz, ldz, act, pa, lda, psa, nsa, pb, ldb, psb, nsb, pda, ldda, pdb, lddb,
+         _vec(dbias, dev, 2 * F, "dbias", f32), M, F, K, mode, seed & 0xFFFFFFFFFFFFFFFF, call & 0xFFFFFFFF, kind, pws, nws,
+         _stream(stream))
+
+
+# ------------------------------------------------------------------ tokens and logits
+def _given(t, what):
+    """An operand that a call cannot go without."""
+    if not isinstance(t, _Tensor):
+        raise TypeError("%s must be a device tensor" % what)
+    return t
+
+
+def embedding_fwd(table, tokens, out, table_scale=None, alpha=1.0, stream=None):
+    """out[m] = alpha * table[tokens[m]]; an int8 table has its rows' scales in table_scale.
+    Tokens (int32) outside the table give rows of zeros (niti_embedding_fwd)."""
+    (V, D), dev = _matrix(table, "table")
+    dt = _dtype(out, "out")
+    kind = _type_of(dt, "out")
+    codes = table.dtype is _torch_mod.int8
+    if codes != (table_scale is not None):
+        raise ValueError("table_scale belongs to an int8 table")
+    t_type = I8 if codes else _type_of(table.dtype, "table")
+    M = _given(tokens, "tokens").numel()
+    pt, ldt = _mat(table, dev, table.dtype, (V, D), "table")
+    po, ldo = _mat(out, dev, dt, (M, D), "out", True)
+    _run("niti_embedding_fwd", pt, ldt, t_type, _vec(table_scale, dev, V, "table_scale", _torch_mod.float32),
+         _vec(tokens, dev, M, "tokens", _torch_mod.int32), po, ldo, M, V, D, alpha, kind, _stream(stream))
+
+
+def embedding_bwd(dy, tokens, dtable, ws, alpha=1.0, accumulate=False, stream=None):
+    """dtable[v] = alpha * the sum of dy[m] over the m with tokens[m] = v (accumulate: added to what
+    dtable holds, other rows left as they are); ws as workspace_bytes(OP_EMBEDDING_BWD, None, M, V, D)
+    (niti_embedding_bwd)."""
+    (M, D), dev = _matrix(dy, "dy")
+    V = _width(dtable, 0, "dtable")
+    dt, gt = dy.dtype, dtable.dtype
+    kind, gkind = _type_of(dt, "dy"), _type_of(gt, "dtable")
+    pdy, lddy = _mat(dy, dev, dt, (M, D), "dy")
+    pg, ldg = _mat(dtable, dev, gt, (V, D), "dtable", True)
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_embedding_bwd", pdy, lddy, kind, _vec(_given(tokens, "tokens"), dev, M, "tokens", _torch_mod.int32), pg, ldg, gkind,
+         M, V, D, alpha, 1 if accumulate else 0, pws, nws, _stream(stream))
+
+
+def token_logprobs(logits, tokens=None, logp=None, lse=None, entropy=None, top_logp=None, top_idx=None, scale=1.0, ws=None,
+                   stream=None):
+    """Log probabilities of softmax(scale * logits) by rows: logp of the given tokens (int32), lse, entropy, and
+    the largest, with their columns, in top_logp [M][top] and top_idx (int32), equal ones by column; ws as
+    workspace_bytes(OP_TOKEN_LOGPROBS, None, M, V, top) where that is not 0 (niti_token_logprobs)."""
+    (M, V), dev = _matrix(logits, "logits")
+    dt, f32, i32 = logits.dtype, _torch_mod.float32, _torch_mod.int32
+    kind = _type_of(dt, "logits")
+    if (tokens is None) != (logp is None):
+        raise ValueError("token_logprobs: tokens and logp belong together")
+    px, ldx = _mat(logits, dev, dt, (M, V), "logits")
+    top = 0 if top_logp is None and top_idx is None else _width(top_idx if top_logp is None else top_logp, 1, "top_logp")
+    pv, pi = (None if t is None else _vec(t, dev, M * top, n, d) if _given(t, n).shape == (M, top) else _misshapen(t, (M, top), n)
+              for t, n, d in ((top_logp, "top_logp", f32), (top_idx, "top_idx", i32)))
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_token_logprobs", px, ldx, _vec(tokens, dev, M, "tokens", i32), _vec(logp, dev, M, "logp", f32),
+         _vec(lse, dev, M, "lse", f32), _vec(entropy, dev, M, "entropy", f32), pv, pi, M, V, top, scale, kind, pws, nws,
+         _stream(stream))
+
+
+def _misshapen(t, shape, what):
+    raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+
+
+def _distill_args(logits, t_val, t_idx, dloss, dlogits):
+    (M, V), dev = _matrix(logits, "logits")
+    dt = logits.dtype
+    kind = _type_of(dt, "logits")
+    top = _width(t_val, 1, "t_val")
+    px, ldx = _mat(logits, dev, dt, (M, V), "logits")
+    pv, ldv = _mat(t_val, dev, t_val.dtype, (M, top), "t_val")
+    pi, ldi = _mat(_given(t_idx, "t_idx"), dev, _torch_mod.int32, (M, top), "t_idx")
+    pd, ldd = _mat(dlogits, dev, dt, (M, V), "dlogits", True)
+    pg, ng = (None, 0) if dloss is None else _scales(dloss, dev, M, "dloss")
+    return M, V, top, dev, kind, (px, ldx, pv, ldv, _type_of(t_val.dtype, "t_val"), pi, ldi), (pg, ng, pd, ldd)
+
+
+def distill_fwd(logits, t_val, t_idx, loss, lse=None, dlogits=None, dloss=None, scale=1.0, ws=None, stream=None):
+    """loss[m] = KL(p || softmax(scale * logits)), p = softmax(scale * t_val) over the teacher's columns t_idx
+    (int32; -1: none).  dlogits: the gradient, times dloss (one or M; None: 1), in the same pass; it may be logits.
+    ws as workspace_bytes(OP_DISTILL_FWD, None, M, V) where that is not 0 (niti_distill_fwd)."""
+    M, V, top, dev, kind, operands, grad = _distill_args(logits, t_val, t_idx, dloss, dlogits)
+    f32 = _torch_mod.float32
+    pws, nws = _ws_args(ws, dev)
+    _run("niti_distill_fwd", *operands, _vec(_given(loss, "loss"), dev, M, "loss", f32), _vec(lse, dev, M, "lse", f32), *grad, M, V,
+         top, scale, kind, pws, nws, _stream(stream))
+
+
+def distill_bwd(logits, t_val, t_idx, lse, dloss, dlogits, scale=1.0, stream=None):
+    """The gradient of distill_fwd from the lse that it kept, times dloss (one or M; None: 1); dlogits may be
+    logits (niti_distill_bwd)."""
+    M, V, top, dev, kind, operands, grad = _distill_args(logits, t_val, t_idx, dloss, _given(dlogits, "dlogits"))
+    _run("niti_distill_bwd", *operands, _vec(_given(lse, "lse"), dev, M, "lse", _torch_mod.float32), *grad, M, V, top, scale, kind,
          _stream(stream))
 
 
