@@ -29,58 +29,93 @@ namespace {
 constexpr int kTopMax = 64;     // alternatives of a row
 constexpr int kListMax = 256;   // teacher's logits of a row
 constexpr int kCand = 512;      // collected logits of a row
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr uint32_t kNegInf = 0xFF800000u;
 
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(kNegInf); }
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
 
-// Integers of the order of floats (no NaN among them; both zeros alike).
+// Integers of the order of floats (no NaN among them; both zeros alike), and the float of one.
 __device__ __forceinline__ uint32_t order_key(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);
     return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+// Of two logits the one with the larger rank stands first: by value, then by column.
+__device__ __forceinline__ uint64_t rank_of(float v, int col) { return (uint64_t)order_key(v) << 32 | (uint32_t)~col; }
+__device__ __forceinline__ int rank_col(uint64_t r) { return (int)~(uint32_t)r; }
 
-// Eight logits from column c on, as they are loaded (in no branch where a row has eight).
-template <typename T>
+// ---------------------------------------------------------------- reductions
+// Row-local steps of a wave: after the first two, four neighbouring lanes have the same, after four, sixteen.
+template <int CTRL>
+__device__ __forceinline__ float lane_step(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); }
+__device__ __forceinline__ float max_of_4(float v) {
+    v = fmaxf(v, lane_step<0xB1>(v));
+    return fmaxf(v, lane_step<0x4E>(v));
+}
+__device__ __forceinline__ float max_of_16(float v) {
+    v = max_of_4(v);
+    v = fmaxf(v, lane_step<0x141>(v));
+    return fmaxf(v, lane_step<0x140>(v));
+}
+__device__ __forceinline__ float max_of_rows(float v) {   // sixteen lanes have the same
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+__device__ __forceinline__ float wave_max(float v) { return max_of_rows(max_of_16(v)); }
+__device__ __forceinline__ float wave_sum(float v) {
+    v += lane_step<0xB1>(v);
+    v += lane_step<0x4E>(v);
+    v += lane_step<0x141>(v);
+    v += lane_step<0x140>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+// Of the NW values that the waves left in LDS.
+template <int NW>
+__device__ __forceinline__ float join_max(const float* red) {
+    float v = red[0];
+#pragma unroll
+    for (int i = 1; i < NW; i++) v = fmaxf(v, red[i]);
+    return v;
+}
+template <int NW>
+__device__ __forceinline__ float join_sum(const float* red) {
+    float v = red[0];
+#pragma unroll
+    for (int i = 1; i < NW; i++) v += red[i];
+    return v;
+}
+
+// ---------------------------------------------------------------- a row in registers
+// Eight logits of column c on, as they are loaded.  No load is in a branch, where it would be waited for: the
+// row's last piece is loaded from eight columns before its end, and its first `down` elements, which belong to the piece before it
+// (past the row: all eight), count for nothing.  TINY: rows of fewer than eight.
+template <bool TINY>
+struct Place {
+    int from, down, end;   // elements down .. end - 1 are the piece's own, of columns from + e
+    __device__ __forceinline__ Place(int c, int V) {
+        from = TINY ? c : min(c, V - CH);
+        down = TINY ? 0 : c - from;
+        end = TINY ? V - c : CH;
+    }
+    __device__ __forceinline__ bool own(int e) const { return e >= down && (!TINY || e < end); }
+    __device__ __forceinline__ bool whole() const { return !TINY && down == 0; }
+};
+
+template <typename T, bool TINY>
 __device__ __forceinline__ Piece<T> load_logits(const T* row, int c, int V) {
     Piece<T> p;
-    if (V >= CH) {
-        const int from = min(c, V - CH);
-        __builtin_memcpy(p.w, row + from, sizeof(p.w));
-        return p;
-    }
-    T t[CH];
-#pragma unroll
-    for (int e = 0; e < CH; e++) t[e] = row[min(c + e, V - 1)];
-    __builtin_memcpy(p.w, t, sizeof(t));
-    return p;
-}
-// Set right where the row ends: minus infinity past it.
-template <typename T>
-__device__ __forceinline__ void end_logits(Piece<T>& p, int c, int V) {
-    if (c + CH <= V) return;
-    constexpr int W = CH * sizeof(T) / 4, PER = 4 / sizeof(T);
-    const uint32_t none = sizeof(T) == 4 ? kNegInf : (__is_same(T, bf16) ? 0xFF80FF80u : 0xFC00FC00u);
-    const int down = V < CH ? 0 : min(c - (V - CH), CH);   // elements to move down; CH: the whole piece is past the row
-    if (PER == 2 && (down & 1)) {
-#pragma unroll
-        for (int i = 0; i < W; i++) p.w[i] = p.w[i] >> 16 | (i + 1 < W ? p.w[i + 1 < W ? i + 1 : i] : none) << 16;
-    }
-#pragma unroll
-    for (int b = 1; b <= W; b *= 2) {
-        const bool move = (down / PER) & b;
-#pragma unroll
-        for (int i = 0; i < W; i++) p.w[i] = move ? (i + b < W ? p.w[i + b < W ? i + b : i] : none) : p.w[i];
-    }
-    if (V < CH) {
+    if constexpr (TINY) {
         T t[CH];
-        __builtin_memcpy(t, p.w, sizeof(t));
 #pragma unroll
-        for (int e = 0; e < CH; e++)
-            if (c + e >= V) t[e] = from_f<T>(neg_inf());
+        for (int e = 0; e < CH; e++) t[e] = row[min(c + e, V - 1)];
         __builtin_memcpy(p.w, t, sizeof(t));
+    } else {
+        __builtin_memcpy(p.w, row + min(c, V - CH), sizeof(p.w));
     }
+    return p;
 }
 template <typename T>
 __device__ __forceinline__ void logit_values(const Piece<T>& p, float (&v)[CH]) {
@@ -89,44 +124,97 @@ __device__ __forceinline__ void logit_values(const Piece<T>& p, float (&v)[CH]) 
 #pragma unroll
     for (int e = 0; e < CH; e++) v[e] = to_f(t[e]);
 }
-
-__device__ __forceinline__ float wave_max_f32(float v) {
+// Minus infinity in the place of the elements that are not the piece's own.
+template <typename T, bool TINY>
+__device__ __forceinline__ void mask_logits(Piece<T>& p, int c, int V) {
+    const Place<TINY> at(c, V);
+    if (at.whole()) return;
+    T t[CH];
+    __builtin_memcpy(t, p.w, sizeof(t));
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-    return v;
+    for (int e = 0; e < CH; e++) t[e] = at.own(e) ? t[e] : from_f<T>(neg_inf());
+    __builtin_memcpy(p.w, t, sizeof(t));
 }
-
-// A row's (or a part's) statistics.
-struct Stat {
-    float m, s, w;   // max x, S, W; a row of minus infinities: -inf, 0, 0
-};
-// What exponents are taken from: the maximum, or 0 where there is none.
-__device__ __forceinline__ float base_of(float m) { return m == neg_inf() ? 0.f : m; }
-// A NaN or an infinity in the row leaves a NaN in S.
-__device__ __forceinline__ float log_of(const Stat& st) { return logf(st.s); }
-__device__ __forceinline__ float lse_of(const Stat& st, float scale, float logs) { return st.m == neg_inf() && st.s == 0.f ? neg_inf() : scale * base_of(st.m) + logs; }
-__device__ __forceinline__ float logp_of(const Stat& st, float scale, float logs, float x) {
-    return st.m == neg_inf() && st.s == 0.f ? neg_inf() : scale * (x - base_of(st.m)) - logs;
+template <typename T, bool TINY>
+__device__ __forceinline__ void store_logits(T* row, int c, int V, const float (&v)[CH]) {
+    const Place<TINY> at(c, V);
+    if (at.whole()) {
+        store_n(row + c, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < CH; e++)
+            if (at.own(e)) row[at.from + e] = from_f<T>(v[e]);
+    }
 }
-
-// Sums of exp(scale u) and u exp(scale u) over a thread's pieces.
+// p[want], want uniform, by selects over constant indices: the pieces stay in registers.
 template <typename T, int VPT>
-__device__ __forceinline__ void exp_sums(const Piece<T> (&p)[VPT], float base, float c2, float& s, float& w) {
+__device__ __forceinline__ Piece<T> pick(const Piece<T> (&p)[VPT], int want) {
+    Piece<T> x = p[0];
+#pragma unroll
+    for (int i = 1; i < VPT; i++)
+#pragma unroll
+        for (int w = 0; w < (int)(sizeof(x.w) / 4); w++) x.w[w] = want == i ? p[i].w[w] : x.w[w];
+    return x;
+}
+
+// What exponents of a row are taken from: the maximum, or 0 where there is none.  An element's power is 2^((x - m) c2),
+// c2 = scale log2 e.  (One multiply-add, x c2 - m c2, would do but for rows of a type's lowest value, whose m c2 is no 32-bit number.)
+__device__ __forceinline__ float base_of(float top) { return top == neg_inf() ? 0.f : top; }
+__device__ __forceinline__ float power_of(float x, float base, float c2) { return __builtin_amdgcn_exp2f((x - base) * c2); }
+
+// A row's (or a part's) statistics: the maximum, S = sum 2^u and W = sum u 2^u of u = (x - m) c2.  A row
+// of minus infinities has -inf, 0 and 0; a NaN or an infinity in the row leaves a NaN in S.
+struct Stat {
+    float m, s, w;
+    __device__ __forceinline__ bool empty() const { return m == neg_inf() && s == 0.f; }
+    __device__ __forceinline__ float log() const { return logf(s); }
+    __device__ __forceinline__ float base() const { return base_of(m); }
+    __device__ __forceinline__ float lse(float scale, float logs) const { return empty() ? neg_inf() : scale * base() + logs; }
+    __device__ __forceinline__ float logp(float scale, float logs, float x) const { return empty() ? neg_inf() : scale * (x - base()) - logs; }
+    __device__ __forceinline__ float entropy(float logs) const { return empty() ? 0.f : logs - kLn2 * (w / s); }
+};
+
+// The pieces are converted anew in each pass over them: converted values that stay would take twice the registers.
+template <typename T, int VPT>
+__device__ __forceinline__ void forget_values(Piece<T> (&p)[VPT]) {
+#pragma unroll
+    for (int i = 0; i < VPT; i++)
+#pragma unroll
+        for (int w = 0; w < (int)(sizeof(p[i].w) / 4); w++) asm volatile("" : "+v"(p[i].w[w]));
+}
+// S and W over a thread's pieces; KEEP: the powers stay in e.
+template <typename T, int VPT, bool WANT_W, bool KEEP>
+__device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], float base, float c2, float& s, float& w, float (&e)[KEEP ? VPT : 1][CH]) {
+    if (sizeof(T) == 2) forget_values(p);
     s = w = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         float v[CH];
         logit_values(p[i], v);
 #pragma unroll
-        for (int e = 0; e < CH; e++) {
-            const float u = v[e] - base;
-            const float x = __builtin_amdgcn_exp2f(u * c2);
+        for (int k = 0; k < CH; k++) {
+            const float u = (v[k] - base) * c2, x = __builtin_amdgcn_exp2f(u);
             s += x;
-            w = __builtin_fmaf(x, fmaxf(u, -0x1p100f), w);   // (minus infinity times 0)
+            if (WANT_W) w = __builtin_fmaf(x, fmaxf(u, -0x1p100f), w);   // (minus infinity times 0)
+            if (KEEP) e[i][k] = x;
         }
     }
+    if (sizeof(T) == 2 && !KEEP) forget_values(p);
+}
+template <typename T, int VPT>
+__device__ __forceinline__ float max_of(const Piece<T> (&p)[VPT]) {
+    float mx = neg_inf();
+#pragma unroll
+    for (int i = 0; i < VPT; i++) {
+        float v[CH];
+        logit_values(p[i], v);
+#pragma unroll
+        for (int e = 0; e < CH; e++) mx = fmaxf(mx, v[e]);
+    }
+    return mx;
 }
 
+// ---------------------------------------------------------------- log probabilities
 struct LogArgs {
     const void* x;
     const int32_t* tokens;
@@ -135,199 +223,241 @@ struct LogArgs {
     int64_t ldx, M, V;
     int32_t top, parts;
     float scale, c2;
-    // Parts of split rows: [M][parts] statistics, [M][parts][top] logits and columns in order (past the last: column -1).
+    // Parts of split rows: [M][parts] statistics, [M][parts][top] ranks in order (0: fewer logits than that).
     Stat* stat;
-    float* val;
-    int32_t* col;
+    uint64_t* ranks;
 };
 
 // A row's scalars, by one thread.
 __device__ __forceinline__ void put_scalars(const LogArgs& a, int64_t m, const Stat& st, float logs, int tok, float x) {
-    if (a.logp) a.logp[m] = (uint32_t)tok < (uint64_t)a.V ? logp_of(st, a.scale, logs, x) : 0.f;
-    if (a.lse) a.lse[m] = lse_of(st, a.scale, logs);
-    if (a.entropy) a.entropy[m] = st.m == neg_inf() && st.s == 0.f ? 0.f : logs - a.scale * st.w / st.s;
+    if (a.logp) a.logp[m] = (uint32_t)tok < (uint64_t)a.V ? st.logp(a.scale, logs, x) : 0.f;
+    if (a.lse) a.lse[m] = st.lse(a.scale, logs);
+    if (a.entropy) a.entropy[m] = st.entropy(logs);
 }
-__device__ __forceinline__ void put_top(const LogArgs& a, int64_t m, int r, const Stat& st, float logs, float v, int col) {
-    const bool bad = !(st.s == st.s);
-    if (a.top_logp) a.top_logp[m * a.top + r] = bad ? quiet_nan() : logp_of(st, a.scale, logs, v);
-    if (a.top_idx) a.top_idx[m * a.top + r] = bad ? -1 : col;
+// Alternative r of a row; rank 0: none.
+__device__ __forceinline__ void put_top(const LogArgs& a, int64_t m, int r, const Stat& st, float logs, uint64_t rank) {
+    const bool bad = !(st.s == st.s) || rank == 0;
+    if (a.top_logp) a.top_logp[m * a.top + r] = bad ? quiet_nan() : st.logp(a.scale, logs, key_value((uint32_t)(rank >> 32)));
+    if (a.top_idx) a.top_idx[m * a.top + r] = bad ? -1 : rank_col(rank);
 }
 
-// The bound: the largest of 64 values that at least k of them reach.
-__device__ __forceinline__ float bound_of(float g, int k) {
-    int above = 0;
+// The largest of 64 values (in LDS, 16-byte aligned; each lane's own in g) that at least k of them reach.  By one wave.
+__device__ __forceinline__ float bound_of(const float* values, float g, int k) {
+    int reach = 0;
 #pragma unroll
-    for (int j = 0; j < 64; j++)
-        above += __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(g), j)) >= g ? 1 : 0;
-    return wave_max_f32(above >= k ? g : neg_inf());
+    for (int j = 0; j < 16; j++) {
+        const v4f x = *(const v4f*)(values + 4 * j);
+#pragma unroll
+        for (int i = 0; i < 4; i++) reach += x[i] >= g ? 1 : 0;
+    }
+    return wave_max(reach >= k ? g : neg_inf());
 }
 
-struct Cand {
-    float v[kCand];
-    int col[kCand];
-    int n;
+// Adds n to a counter in LDS for each lane by itself (the compiler would first join the lanes, one after the other).
+__device__ __forceinline__ int lds_add(int* p, int n) {
+    int old;
+    asm volatile("ds_add_rtn_u32 %0, %1, %2\n\ts_waitcnt lgkmcnt(0)" : "=v"(old) : "v"(lds_address(p)), "v"(n) : "memory");
+    return old;
+}
+
+// The top logits of a workgroup's columns: kCand places for the logits that reach a bound, placed by counting.
+template <typename T, int NW, int VPT, bool TINY>
+struct Select {
+    static constexpr int NT = 64 * NW;
+    uint64_t* cand;      // [kCand]
+    int* n;              // zeroed by the caller, who has a barrier after it
+    int (*red)[NW];      // [2][NW]
+    int c0, V;
+
+    // hits(v, e, at): f gets a piece's hits as a mask, its values and its place
+    template <typename Hit, typename F>
+    __device__ __forceinline__ void piece(const Piece<T> (&p)[VPT], int i, Hit hit, F f) {
+        const Piece<T> x = pick(p, i);
+        const Place<TINY> at(c0 + (i * NT + (int)threadIdx.x) * CH, V);
+        float v[CH];
+        logit_values(x, v);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int e = 0; e < CH; e++) mask |= (hit(v[e]) && at.own(e) ? 1u : 0u) << e;
+        f(mask, v, at.from);
+    }
+    // All that hit, in any order; what is past kCand is only counted.
+    template <typename Hit>
+    __device__ __forceinline__ void collect(const Piece<T> (&p)[VPT], Hit hit) {
+#pragma unroll 1
+        for (int i = 0; i < VPT; i++)
+            piece(p, i, hit, [&](uint32_t mask, const float (&v)[CH], int from) {
+                if (!mask) return;
+                int at = lds_add(n, __popc(mask));
+#pragma unroll
+                for (int e = 0; e < CH; e++)
+                    if (mask >> e & 1) {
+                        if (at < kCand) cand[at] = rank_of(v[e], from + e);
+                        at++;
+                    }
+            });
+    }
+    // The `need` equals of tau with the lowest columns, behind the first n0.
+    __device__ __forceinline__ int equals(const Piece<T> (&p)[VPT], float tau, int n0, int need) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        int got = 0;
+#pragma unroll 1
+        for (int i = 0; i < VPT && got < need; i++)   // (the same for all threads)
+            piece(p, i, [&](float v) { return v == tau; }, [&](uint32_t mask, const float (&v)[CH], int from) {
+                int incl = __popc(mask);
+#pragma unroll
+                for (int o = 1; o < 64; o *= 2) {
+                    const int u = __shfl_up(incl, o, kWave);
+                    incl += lane >= o ? u : 0;
+                }
+                int (&r)[NW] = red[i & 1];   // a wave that is a piece ahead writes the other half
+                if (lane == 63) r[wave] = incl;
+                __syncthreads();
+                int at = got + incl - __popc(mask), all = 0;
+#pragma unroll 1
+                for (int w = 0; w < NW; w++) {
+                    at += w < wave ? r[w] : 0;
+                    all += r[w];
+                }
+#pragma unroll
+                for (int e = 0; e < CH; e++)
+                    if (mask >> e & 1) {
+                        if (at < need) cand[n0 + at] = rank_of(v[e], from + e);
+                        at++;
+                    }
+                got += all;
+            });
+        return min(got, need);
+    }
+    // The key of the k-th largest, by bisection on its bits.
+    __device__ __forceinline__ uint32_t kth(const Piece<T> (&p)[VPT], int k) {
+        uint32_t key = 0;
+#pragma unroll 1
+        for (int b = 31; b >= 0; b--) {
+            const uint32_t want = key | 1u << b;
+            int c = 0;
+#pragma unroll 1
+            for (int i = 0; i < VPT; i++)
+                piece(p, i, [&](float v) { return v == v && order_key(v) >= want; },
+                      [&](uint32_t mask, const float (&)[CH], int) { c += __popc(mask); });
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o, kWave);
+            int (&r)[NW] = red[b & 1];
+            if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll 1
+            for (int w = 0; w < NW; w++) c += r[w];
+            if (c >= k) key = want;
+        }
+        return key;
+    }
+    __device__ __forceinline__ int restart() {
+        __syncthreads();
+        if (threadIdx.x == 0) *n = 0;
+        __syncthreads();
+        return 0;
+    }
+    // Number of candidates, among them the top ones; mx: this thread's largest.
+    __device__ __forceinline__ int run(const Piece<T> (&p)[VPT], float mx, float tau, int top) {
+        if (mx >= tau) collect(p, [&](float v) { return v >= tau; });
+        __syncthreads();
+        int count = *n;
+        if (count <= kCand) return count;
+        restart();
+        if (mx > tau) collect(p, [&](float v) { return v > tau; });
+        __syncthreads();
+        count = *n;
+        if (count > kCand) {
+            tau = key_value(kth(p, top));
+            restart();
+            if (mx > tau) collect(p, [&](float v) { return v > tau; });
+            __syncthreads();
+            count = min(*n, kCand);
+        }
+        if (count < top) {
+            count += equals(p, tau, count, top - count);
+            __syncthreads();
+        }
+        return count;
+    }
 };
-// Whether candidate i stands before one of key and column.
-__device__ __forceinline__ bool before(const Cand& c, int i, uint32_t key, int col) {
-    const uint32_t k = order_key(c.v[i]);
-    return k > key || (k == key && c.col[i] < col);
-}
 
-template <typename T, int NW, int VPT>
+// Waves that a SIMD is to hold: two workgroups of sixteen a CU, one loading while the other computes, where 64 registers do.
+template <typename T>
+constexpr int two_a_cu(int nw, int vpt) { return nw == 16 && vpt <= 4 && vpt * (int)sizeof(T) <= 16 ? 8 : 1; }
+
+template <typename T, int NW, int VPT, bool TINY>
 __global__ __launch_bounds__(64 * NW) void logprobs_kernel(LogArgs a) {
     constexpr int NT = 64 * NW, LEN = NT * VPT * CH;
-    __shared__ float red_m[NW], red_s[NW], red_w[NW], group[64], tau_s;
-    __shared__ int red_c[2][NW];
-    __shared__ Cand cand;
+    __shared__ float red_m[NW], red_s[NW], red_w[NW], tau_s;
+    __shared__ __attribute__((aligned(16))) float group[64];
+    __shared__ int red_c[2][NW], n_s;
+    __shared__ uint64_t cand[kCand];
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t m = blockIdx.x / (uint32_t)a.parts;
     const int part = blockIdx.x % (uint32_t)a.parts, V = (int)a.V, c0 = part * LEN;
     const T* row = (const T*)a.x + m * a.ldx;
+    const int tok = a.parts == 1 && a.tokens ? a.tokens[m] : -1;
     Piece<T> p[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; i++) p[i] = load_logits(row, c0 + (i * NT + t) * CH, V);
-    const int tok = a.parts == 1 && a.tokens ? a.tokens[m] : -1;
-    const float x_tok = to_f(row[(uint32_t)tok < (uint32_t)V ? tok : 0]);
-    if (t == 0) cand.n = 0;
-    float mx = neg_inf();
+    for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
+    const T x_tok = row[(uint32_t)tok < (uint32_t)V ? tok : 0];
+    if (t == 0) n_s = 0;
 #pragma unroll
-    for (int i = 0; i < VPT; i++) {
-        end_logits(p[i], c0 + (i * NT + t) * CH, V);
-        float v[CH];
-        logit_values(p[i], v);
-#pragma unroll
-        for (int e = 0; e < CH; e++) mx = fmaxf(mx, v[e]);
-    }
+    for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
+    const float mx = max_of(p);
     // 64 groups of NW neighbouring threads
-    float gm = mx;
-#pragma unroll
-    for (int o = 1; o < NW; o *= 2) gm = fmaxf(gm, __shfl_xor(gm, o, kWave));
-    if (t % NW == 0) group[t / NW] = gm;
-    const float wm = wave_max_f32(gm);
+    const float m4 = max_of_4(mx), m16 = max_of_16(m4);
+    if (t % NW == 0) group[t / NW] = NW == 1 ? mx : (NW == 4 ? m4 : m16);
+    const float wm = max_of_rows(m16);
     if ((t & 63) == 0) red_m[wave] = wm;
     __syncthreads();
     Stat st;
-    st.m = red_m[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) st.m = fmaxf(st.m, red_m[i]);
+    st.m = join_max<NW>(red_m);
     if (a.top && wave == 0) {
-        const float tau = bound_of(group[t], a.top);
+        const float tau = bound_of(group, group[t], a.top);
         if (t == 0) tau_s = tau;
     }
-    exp_sums<T, VPT>(p, base_of(st.m), a.c2, st.s, st.w);
-    st.s = wave_sum_f32(st.s);
-    st.w = wave_sum_f32(st.w);
+    float none[1][CH];
+    row_sums<T, VPT, true, false>(p, st.base(), a.c2, st.s, st.w, none);
+    st.s = wave_sum(st.s);
+    st.w = wave_sum(st.w);
     if ((t & 63) == 0) red_s[wave] = st.s, red_w[wave] = st.w;
     __syncthreads();
-    st.s = red_s[0], st.w = red_w[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) st.s += red_s[i], st.w += red_w[i];
-    const float logs = log_of(st);
+    st.s = join_sum<NW>(red_s);
+    st.w = join_sum<NW>(red_w);
+    const float logs = st.log();
     if (t == 0) {
-        if (a.parts == 1) put_scalars(a, m, st, logs, tok, x_tok);
+        if (a.parts == 1) put_scalars(a, m, st, logs, tok, to_f(x_tok));
         else a.stat[m * a.parts + part] = st;
     }
     if (!a.top) return;
-    const float tau = tau_s;
-    auto each = [&](auto f) {   // f(value, column) of this thread's logits
-#pragma unroll
-        for (int i = 0; i < VPT; i++) {
-            float v[CH];
-            logit_values(p[i], v);
-            const int c = c0 + (i * NT + t) * CH;
-#pragma unroll
-            for (int e = 0; e < CH; e++)
-                if (c + e < V) f(v[e], c + e);
-        }
+    Select<T, NW, VPT, TINY> sel{cand, &n_s, red_c, c0, V};
+    const int n = sel.run(p, mx, tau_s, a.top);
+    auto put = [&](int r, uint64_t rank) {
+        if (a.parts == 1) put_top(a, m, r, st, logs, rank);
+        else a.ranks[(m * a.parts + part) * a.top + r] = rank;
     };
-    auto keep = [&](float v, int c) {
-        const int at = atomicAdd(&cand.n, 1);
-        if (at < kCand) cand.v[at] = v, cand.col[at] = c;
-    };
-    if (mx >= tau) each([&](float v, int c) {
-        if (v >= tau) keep(v, c);
-    });
-    __syncthreads();
-    int n = cand.n;
-    if (n > kCand) {   // (the same for all threads)
-        int turn = 0;
-        auto count = [&](auto pred) {
-            int k = 0;
-            each([&](float v, int c) { k += v == v && pred(order_key(v), c) ? 1 : 0; });
-#pragma unroll
-            for (int o = 32; o >= 1; o >>= 1) k += __shfl_xor(k, o, kWave);
-            if ((t & 63) == 0) red_c[turn][wave] = k;
-            __syncthreads();
-            k = 0;
-#pragma unroll
-            for (int i = 0; i < NW; i++) k += red_c[turn][i];
-            turn ^= 1;   // a wave that is a count ahead writes the other half
-            return k;
-        };
-        uint32_t kth = 0;   // the key of the top-th largest
-        for (int b = 31; b >= 0; b--) {
-            const uint32_t want = kth | 1u << b;
-            if (count([&](uint32_t k, int) { return k >= want; }) >= a.top) kth = want;
-        }
-        const int more = a.top - count([&](uint32_t k, int) { return k > kth; });
-        int last = 0;       // the largest column with fewer than `more` equals before it
-        for (int b = 22; b >= 0; b--) {
-            const int want = last | 1 << b;
-            if (count([&](uint32_t k, int c) { return k == kth && c < want; }) < more) last = want;
-        }
-        if (t == 0) cand.n = 0;
-        __syncthreads();
-        each([&](float v, int c) {
-            const uint32_t k = order_key(v);
-            if (v == v && (k > kth || (k == kth && c <= last))) keep(v, c);
-        });
-        __syncthreads();
-        n = min(cand.n, kCand);
-    }
     for (int j = t; j < n; j += NT) {
-        const float v = cand.v[j];
-        const uint32_t key = order_key(v);
-        const int col = cand.col[j];
+        const uint64_t mine = cand[j];
         int r = 0;
-        for (int i = 0; i < n; i++) r += before(cand, i, key, col) ? 1 : 0;
-        if (r >= a.top) continue;
-        if (a.parts == 1) {
-            put_top(a, m, r, st, logs, v, col);
-        } else {
-            const int64_t at = (m * a.parts + part) * a.top + r;
-            a.val[at] = v;
-            a.col[at] = col;
-        }
+        for (int i = 0; i < n; i++) r += cand[i] > mine ? 1 : 0;
+        if (r < a.top) put(r, mine);
     }
-    for (int r = n + t; r < a.top; r += NT) {   // fewer logits than that in this part, or NaNs among them
-        if (a.parts == 1) {
-            put_top(a, m, r, st, logs, quiet_nan(), -1);
-        } else {
-            const int64_t at = (m * a.parts + part) * a.top + r;
-            a.val[at] = neg_inf();
-            a.col[at] = -1;
-        }
-    }
+    for (int r = n + t; r < a.top; r += NT) put(r, 0);   // fewer logits than that in this part, or NaNs among them
 }
 
 // Statistics of a row from those of its parts, by all 64 lanes of a wave, in an order fixed by the number of parts.
 __device__ __forceinline__ Stat join_stats(const Stat* parts, int n, float c2) {
     const int lane = threadIdx.x & 63;
-    float m = neg_inf();
-    for (int i = lane; i < n; i += 64) m = fmaxf(m, parts[i].m);
+    Stat p = lane < n ? parts[lane] : Stat{neg_inf(), 0.f, 0.f};
     Stat st;
-    st.m = wave_max_f32(m);
-    const float base = base_of(st.m);
-    st.s = st.w = 0.f;
-    for (int i = lane; i < n; i += 64) {
-        const Stat p = parts[i];
-        const float d = base_of(p.m) - base;   // W = f (W_i + d S_i) with f = exp(scale d)
-        const float f = p.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(d * c2);
-        st.s += f * p.s;
-        st.w += f * (p.w + fmaxf(d, -0x1p100f) * p.s);
-    }
-    st.s = wave_sum_f32(st.s);
-    st.w = wave_sum_f32(st.w);
+    st.m = wave_max(p.m);
+    // W = sum f (W_i + d S_i) with f = 2^d; a part of minus infinities (base 0, whatever the row's is) adds nothing
+    const float d = p.s == 0.f ? 0.f : (p.base() - st.base()) * c2, f = __builtin_amdgcn_exp2f(d);
+    st.s = wave_sum(f * p.s);
+    st.w = wave_sum(f * (p.w + fmaxf(d, -0x1p100f) * p.s));
     return st;
 }
 
@@ -337,51 +467,44 @@ constexpr int kPartsMax = 64;   // parts of a row
 // each of j parts with j (r + 1) >= k bounds the k-th of the row.
 template <typename T>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(LogArgs a) {
-    __shared__ float val[kPartsMax * kTopMax];
-    __shared__ int col[kPartsMax * kTopMax];
+    __shared__ uint64_t cand[kPartsMax * kTopMax];
+    __shared__ __attribute__((aligned(16))) float group[64];
     __shared__ float tau_s;
     __shared__ int n_s;
     const int t = threadIdx.x;
     const int64_t m = blockIdx.x;
     const int top = a.top, parts = a.parts;
     const int tok = a.tokens ? a.tokens[m] : -1;
-    const float x_tok = to_f(((const T*)a.x + m * a.ldx)[(uint32_t)tok < (uint32_t)a.V ? tok : 0]);
-    const float* v = a.val + m * parts * top;
-    const int32_t* c = a.col + m * parts * top;
+    const T x_tok = ((const T*)a.x + m * a.ldx)[(uint32_t)tok < (uint32_t)a.V ? tok : 0];
+    const uint64_t* ranks = a.ranks + m * parts * top;
+    const Stat st = join_stats(a.stat + m * parts, parts, a.c2);
     if (t == 0) n_s = 0;
     if (top && t < 64) {
         const int r = (top + parts - 1) / parts - 1, j = (top + r) / (r + 1);
-        const float tau = bound_of(t < parts ? v[t * top + r] : neg_inf(), j);
+        const float g = t < parts && ranks[t * top + r] != 0 ? key_value((uint32_t)(ranks[t * top + r] >> 32)) : neg_inf();
+        group[t] = g;
+        __builtin_amdgcn_wave_barrier();
+        const float tau = bound_of(group, g, j);
         if (t == 0) tau_s = tau;
     }
-    const Stat st = join_stats(a.stat + m * parts, parts, a.c2);
-    const float logs = log_of(st);
-    if (t == 0) put_scalars(a, m, st, logs, tok, x_tok);
+    const float logs = st.log();
+    if (t == 0) put_scalars(a, m, st, logs, tok, to_f(x_tok));
     if (!top) return;
     __syncthreads();
     const float tau = tau_s;
     for (int i = t; i < parts * top; i += 256) {
-        const float x = v[i];
-        const int k = c[i];
-        if (k >= 0 && x >= tau) {
-            const int at = atomicAdd(&n_s, 1);
-            val[at] = x;
-            col[at] = k;
-        }
+        const uint64_t rank = ranks[i];
+        if (rank != 0 && key_value((uint32_t)(rank >> 32)) >= tau) cand[lds_add(&n_s, 1)] = rank;
     }
     __syncthreads();
     const int n = n_s;
     for (int j = t; j < n; j += 256) {
-        const uint32_t key = order_key(val[j]);
-        const int mine = col[j];
+        const uint64_t mine = cand[j];
         int r = 0;
-        for (int i = 0; i < n; i++) {
-            const uint32_t k = order_key(val[i]);
-            r += k > key || (k == key && col[i] < mine) ? 1 : 0;
-        }
-        if (r < top) put_top(a, m, r, st, logs, val[j], mine);
+        for (int i = 0; i < n; i++) r += cand[i] > mine ? 1 : 0;
+        if (r < top) put_top(a, m, r, st, logs, mine);
     }
-    for (int r = n + t; r < top; r += 256) put_top(a, m, r, st, logs, quiet_nan(), -1);
+    for (int r = n + t; r < top; r += 256) put_top(a, m, r, st, logs, 0);
 }
 
 // ---------------------------------------------------------------- distillation
@@ -399,188 +522,183 @@ struct DistArgs {
     Stat* stat;
 };
 
-// Entry j of the teacher's list of a row: its logit, minus infinity for a column outside the row.
-struct Listed {
-    float t;
-    int col;
-};
-__device__ __forceinline__ Listed load_listed(const DistArgs& a, int64_t m, int j) {
-    Listed l;
-    l.col = a.t_idx[m * a.ldi + j];
-    float v[1];
-    load_typed(a.t_val, a.t_type, m * a.ldt + j, 1, v);
-    const bool in = (uint32_t)l.col < (uint64_t)a.V;
-    l.t = in ? v[0] : neg_inf();
-    l.col = in ? l.col : -1;
-    return l;
-}
-
-// Sum and maximum over a workgroup of NW waves; red: NW values that no one else uses.
-template <int NW>
-__device__ __forceinline__ float block_sum(float v, float* red) {
-    v = wave_sum_f32(v);
-    if (NW == 1) return v;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) v += red[i];
-    return v;
-}
-template <int NW>
-__device__ __forceinline__ float block_max(float v, float* red) {
-    v = wave_max_f32(v);
-    if (NW == 1) return v;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) v = fmaxf(v, red[i]);
-    return v;
-}
-
 // The teacher's distribution over its list: KPT entries a thread.
 template <int NW, int KPT>
 struct Teacher {
-    Listed l[KPT];
-    float p[KPT], logp[KPT];
-    bool any;     // whether the list has a probability
-    float unit;   // 1; NaN for a list with a NaN or an infinity
+    int col[KPT];     // -1: no entry, or a column outside the row
+    float t[KPT], p[KPT], logp[KPT];
+    bool any;         // whether the list has a probability
+    float unit;       // 1; NaN for a list with a NaN or an infinity
+    uint32_t wide[KPT];
+    uint16_t narrow[KPT];
+    // Of two places to load from, by the type, the other is a stand-in: no load is in a branch.
     __device__ __forceinline__ void load(const DistArgs& a, int64_t m) {
+        const bool f32 = a.t_type == NITI_F32;
 #pragma unroll
         for (int i = 0; i < KPT; i++) {
-            const int j = i * 64 * NW + threadIdx.x;
-            l[i] = j < a.top ? load_listed(a, m, j) : Listed{neg_inf(), -1};
+            const int j = min(i * 64 * NW + (int)threadIdx.x, a.top - 1);
+            col[i] = a.t_idx[m * a.ldi + j];
+            wide[i] = (f32 ? (const uint32_t*)a.t_val : (const uint32_t*)a.t_idx)[f32 ? m * a.ldt + j : m * a.ldi + j];
+            narrow[i] = (f32 ? (const uint16_t*)a.t_idx : (const uint16_t*)a.t_val)[f32 ? m * a.ldi + j : m * a.ldt + j];
         }
     }
-    __device__ __forceinline__ void form(const DistArgs& a, float* red0, float* red1) {
-        float mx = neg_inf(), s = 0.f;
-#pragma unroll
-        for (int i = 0; i < KPT; i++) mx = fmaxf(mx, l[i].t);
-        mx = block_max<NW>(mx, red0);
-        const float base = base_of(mx);
+    // The row's logits at the listed columns from c0 to c1 (any other: that of c0).
+    template <typename T>
+    __device__ __forceinline__ void gather(const DistArgs& a, const T* row, int c0, int c1, T (&z)[KPT]) {
 #pragma unroll
         for (int i = 0; i < KPT; i++) {
-            p[i] = __builtin_amdgcn_exp2f((l[i].t - base) * a.c2);
+            const bool in = i * 64 * NW + (int)threadIdx.x < a.top && (uint32_t)col[i] < (uint64_t)a.V;
+            col[i] = in ? col[i] : -1;
+            z[i] = row[col[i] >= c0 && col[i] < c1 ? col[i] : c0];
+        }
+    }
+    __device__ __forceinline__ float top(const DistArgs& a) {   // this thread's largest
+        float mx = neg_inf();
+#pragma unroll
+        for (int i = 0; i < KPT; i++) {
+            const uint16_t h = narrow[i];
+            const float half = a.t_type == NITI_F16 ? to_f(__builtin_bit_cast(f16, h)) : to_f(bf16{h});
+            t[i] = col[i] < 0 ? neg_inf() : (a.t_type == NITI_F32 ? __uint_as_float(wide[i]) : half);
+            mx = fmaxf(mx, t[i]);
+        }
+        return mx;
+    }
+    __device__ __forceinline__ float powers(const DistArgs& a, float mx) {   // this thread's sum
+        const float base = mx == neg_inf() ? 0.f : mx;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < KPT; i++) {
+            t[i] -= base;
+            p[i] = __builtin_amdgcn_exp2f(t[i] * a.c2);
             s += p[i];
         }
-        s = block_sum<NW>(s, red1);
+        return s;
+    }
+    __device__ __forceinline__ void form(const DistArgs& a, float s) {
         any = s != 0.f;
         unit = s / s;
         const float logs = logf(s);
 #pragma unroll
         for (int i = 0; i < KPT; i++) {
             p[i] = any ? p[i] / s : 0.f;
-            logp[i] = a.scale * (l[i].t - base) - logs;
+            logp[i] = a.scale * t[i] - logs;
+        }
+    }
+    // This thread's terms of the loss.
+    template <typename T>
+    __device__ __forceinline__ float loss(const DistArgs& a, const T (&z)[KPT], const Stat& st, float logs) const {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < KPT; i++) {
+            const float term = p[i] * (logp[i] - st.logp(a.scale, logs, to_f(z[i])));
+            s += p[i] == 0.f ? 0.f : term;
+        }
+        return s;
+    }
+    __device__ __forceinline__ void put(const DistArgs& a, int* cols, float* probs) const {   // for all threads; kListMax of each
+#pragma unroll
+        for (int i = 0; i < KPT; i++) {
+            const int j = i * 64 * NW + (int)threadIdx.x;
+            if (j < kListMax) cols[j] = j < a.top ? col[i] : -1, probs[j] = p[i];
+        }
+    }
+    // The listed columns' own gradients, from c0 to c1, after the whole row's: a column that is listed twice has both probabilities.
+    template <typename T>
+    __device__ __forceinline__ void store(const DistArgs& a, T* dx, const int* cols, const float* probs, const float (&q)[KPT], float g,
+                                          int c0, int c1) const {
+#pragma unroll
+        for (int i = 0; i < KPT; i++) {
+            const int mine = col[i];
+            if (mine < 0 || mine < c0 || mine >= c1) continue;
+            float s = 0.f;
+            for (int j = 0; j < a.top; j += 4) {   // (entries past the list: column -1)
+                const v4i c = *(const v4i*)(cols + j);
+                const v4f x = *(const v4f*)(probs + j);
+#pragma unroll
+                for (int e = 0; e < 4; e++) s += c[e] == mine ? x[e] : 0.f;
+            }
+            dx[mine] = from_f<T>(g * (q[i] - s));
         }
     }
 };
 
-// A row's loss from its statistics: the threads' terms, to be summed.  z: the row's logits at the listed columns.
-template <int NW, int KPT>
-__device__ __forceinline__ float loss_terms(const DistArgs& a, const Teacher<NW, KPT>& t, const float (&z)[KPT], const Stat& st, float logs) {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < KPT; i++) {
-        const float term = t.p[i] * (t.logp[i] - logp_of(st, a.scale, logs, z[i]));
-        s += t.p[i] == 0.f ? 0.f : term;
-    }
-    return s;
-}
-
-template <int KPT>
-__device__ __forceinline__ void put_list(int* col, float* p, const Listed (&l)[KPT], const float (&q)[KPT], int n) {
-#pragma unroll
-    for (int i = 0; i < KPT; i++) {
-        const int j = i * (int)blockDim.x + threadIdx.x;
-        if (j < n) col[j] = l[i].col, p[j] = q[i];
-    }
-}
-// The listed columns' own gradients, from c0 to c1, after the whole row's: a column that is listed twice has both probabilities.
-template <typename T, int KPT>
-__device__ __forceinline__ void put_listed(const DistArgs& a, T* dx, const int* col, const float* p, const Listed (&l)[KPT],
-                                           const float (&q)[KPT], float g, int c0, int c1) {
-#pragma unroll
-    for (int i = 0; i < KPT; i++) {
-        const int mine = l[i].col;
-        if (mine < c0 || mine >= c1 || mine < 0) continue;
-        float s = 0.f;
-        for (int j = 0; j < a.top; j++) s += col[j] == mine ? p[j] : 0.f;
-        dx[mine] = from_f<T>(g * (q[i] - s));
-    }
-}
-
 constexpr int list_per_thread(int nw) { return nw >= 4 ? 1 : 4; }
 
 // Loss of a row (GRAD: and its gradient) by one workgroup, or a part's statistics.
-template <typename T, int NW, int VPT, bool GRAD>
-__global__ __launch_bounds__(64 * NW) void distill_kernel(DistArgs a) {
+template <typename T, int NW, int VPT, bool TINY, bool GRAD>
+__global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(DistArgs a) {
     constexpr int NT = 64 * NW, LEN = NT * VPT * CH, KPT = list_per_thread(NW);
+    constexpr bool KEEP = GRAD && VPT <= 8;   // the powers of the sum serve the gradient: with more, they find no registers
     __shared__ float red_m[NW], red_s[NW], red_t[NW], red_u[NW], red_l[NW];
-    __shared__ int col[kListMax];
-    __shared__ float prob[kListMax];
-    const int t = threadIdx.x;
+    __shared__ __attribute__((aligned(16))) int cols[kListMax];
+    __shared__ __attribute__((aligned(16))) float probs[kListMax];
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t m = blockIdx.x / (uint32_t)a.parts;
     const int part = blockIdx.x % (uint32_t)a.parts, V = (int)a.V, c0 = part * LEN;
     const T* row = (const T*)a.x + m * a.ldx;
+    Teacher<NW, KPT> teach;
+    teach.load(a, m);
+    const float g1 = GRAD && a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
     Piece<T> p[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; i++) p[i] = load_logits(row, c0 + (i * NT + t) * CH, V);
-    Teacher<NW, KPT> teach;
-    float z[KPT];
-    if (a.parts == 1) {
-        teach.load(a, m);
+    for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
+    T z[KPT];
+    teach.gather(a, row, 0, V, z);
 #pragma unroll
-        for (int i = 0; i < KPT; i++) z[i] = to_f(row[max(teach.l[i].col, 0)]);
-    }
-    float mx = neg_inf();
-#pragma unroll
-    for (int i = 0; i < VPT; i++) {
-        end_logits(p[i], c0 + (i * NT + t) * CH, V);
-        float v[CH];
-        logit_values(p[i], v);
-#pragma unroll
-        for (int e = 0; e < CH; e++) mx = fmaxf(mx, v[e]);
-    }
+    for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
+    const float wm = wave_max(max_of(p)), wt = wave_max(teach.top(a));
+    if ((t & 63) == 0) red_m[wave] = wm, red_t[wave] = wt;
+    __syncthreads();
     Stat st;
-    st.m = block_max<NW>(mx, red_m);
-    const float base = base_of(st.m);
-    exp_sums<T, VPT>(p, base, a.c2, st.s, st.w);
-    st.s = block_sum<NW>(st.s, red_s);
+    st.m = join_max<NW>(red_m);
+    const float base = st.base();
+    float e[KEEP ? VPT : 1][CH];
+    row_sums<T, VPT, false, KEEP>(p, base, a.c2, st.s, st.w, e);
+    const float ws = wave_sum(st.s), wu = wave_sum(teach.powers(a, join_max<NW>(red_t)));
+    if ((t & 63) == 0) red_s[wave] = ws, red_u[wave] = wu;
+    __syncthreads();
+    st.s = join_sum<NW>(red_s);
+    st.w = 0.f;
     if (a.parts > 1) {
-        st.w = 0.f;
         if (t == 0) a.stat[m * a.parts + part] = st;
         return;
     }
-    const float logs = log_of(st);
-    teach.form(a, red_t, red_u);
-    if (GRAD) put_list(col, prob, teach.l, teach.p, a.top);
-    const float loss = block_sum<NW>(loss_terms(a, teach, z, st, logs), red_l);   // (its barrier is the list's too)
-    if (NW == 1) __syncthreads();
-    if (t == 0) {
-        a.loss[m] = loss;
-        if (a.lse) a.lse[m] = lse_of(st, a.scale, logs);
-    }
+    const float logs = st.log();
+    teach.form(a, join_sum<NW>(red_u));
+    const float wl = wave_sum(teach.loss(a, z, st, logs));
+    if ((t & 63) == 0) red_l[wave] = wl;
+    if (GRAD) teach.put(a, cols, probs);
     if constexpr (GRAD) {
-        const float g = (a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f) * a.scale * teach.unit;
-        T* dx = (T*)a.dx + m * a.lddx;
+        // Every load of the row has returned, here and, past the barriers above, in the other waves: dx may be x.
         const float inv = st.s == 0.f ? 0.f : 1.f / st.s;
-        float q[KPT];
-#pragma unroll
-        for (int i = 0; i < KPT; i++) q[i] = __builtin_amdgcn_exp2f((z[i] - base) * a.c2) * inv;
+        const float g = g1 * a.scale * teach.unit, f = g * inv;
+        T* dx = (T*)a.dx + m * a.lddx;
 #pragma unroll
         for (int i = 0; i < VPT; i++) {
-            const int c = (i * NT + t) * CH;
-            if (c >= V) continue;
             float v[CH];
-            logit_values(p[i], v);
+            if constexpr (!KEEP) logit_values(p[i], v);
 #pragma unroll
-            for (int e = 0; e < CH; e++) v[e] = teach.any ? g * (__builtin_amdgcn_exp2f((v[e] - base) * a.c2) * inv) : 0.f;
-            store_some(dx + c, V - c, v);
+            for (int k = 0; k < CH; k++) {
+                if constexpr (KEEP) v[k] = e[i][k] * f;
+                else v[k] = power_of(v[k], base, a.c2) * f;
+                if (!teach.any) v[k] = 0.f;
+            }
+            const int c = (i * NT + t) * CH;
+            if (c < V) store_logits<T, TINY>(dx, c, V, v);
         }
-        if (!teach.any) return;
         __syncthreads();   // the row's stores before the listed columns'
-        put_listed(a, dx, col, prob, teach.l, q, g, 0, V);
+        if (teach.any) {
+            float q[KPT];
+#pragma unroll
+            for (int i = 0; i < KPT; i++) q[i] = power_of(to_f(z[i]), base, a.c2) * inv;
+            teach.store(a, dx, cols, probs, q, g, 0, V);
+        }
+    } else {
+        __syncthreads();
+    }
+    if (t == 0) {
+        a.loss[m] = join_sum<NW>(red_l);
+        if (a.lse) a.lse[m] = st.lse(a.scale, logs);
     }
 }
 
@@ -588,72 +706,82 @@ __global__ __launch_bounds__(64 * NW) void distill_kernel(DistArgs a) {
 template <typename T>
 __global__ __launch_bounds__(256) void distill_join_kernel(DistArgs a) {
     __shared__ float red_t[4], red_u[4], red_l[4];
+    const int t = threadIdx.x, wave = t >> 6;
     const int64_t m = blockIdx.x;
     const T* row = (const T*)a.x + m * a.ldx;
     Teacher<4, 1> teach;
+    T z[1];
     teach.load(a, m);
-    const float z[1] = {to_f(row[max(teach.l[0].col, 0)])};
+    teach.gather(a, row, 0, (int)a.V, z);
     const Stat st = join_stats(a.stat + m * a.parts, a.parts, a.c2);
-    const float logs = log_of(st);
-    teach.form(a, red_t, red_u);
-    const float loss = block_sum<4>(loss_terms(a, teach, z, st, logs), red_l);
-    if (threadIdx.x == 0) {
-        a.loss[m] = loss;
-        if (a.lse) a.lse[m] = lse_of(st, a.scale, logs);
+    const float logs = st.log();
+    const float wt = wave_max(teach.top(a));
+    if ((t & 63) == 0) red_t[wave] = wt;
+    __syncthreads();
+    const float wu = wave_sum(teach.powers(a, join_max<4>(red_t)));
+    if ((t & 63) == 0) red_u[wave] = wu;
+    __syncthreads();
+    teach.form(a, join_sum<4>(red_u));
+    const float wl = wave_sum(teach.loss(a, z, st, logs));
+    if ((t & 63) == 0) red_l[wave] = wl;
+    __syncthreads();
+    if (t == 0) {
+        a.loss[m] = join_sum<4>(red_l);
+        if (a.lse) a.lse[m] = st.lse(a.scale, logs);
     }
 }
 
 // The gradient from lse: a part of a row each.  The whole part is loaded before any of it is stored, and so are its
-// listed columns: dx may be x.  (What a row's last piece reads of the part before is moved out of it.)
-template <typename T, int NW, int VPT>
+// listed columns: dx may be x.  (What a row's last piece reads of the part before counts for nothing.)
+template <typename T, int NW, int VPT, bool TINY>
 __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     constexpr int NT = 64 * NW, LEN = NT * VPT * CH, KPT = list_per_thread(NW);
     __shared__ float red_t[NW], red_u[NW];
-    __shared__ int col[kListMax];
-    __shared__ float prob[kListMax];
-    const int t = threadIdx.x;
+    __shared__ __attribute__((aligned(16))) int cols[kListMax];
+    __shared__ __attribute__((aligned(16))) float probs[kListMax];
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int64_t m = blockIdx.x / (uint32_t)a.parts;
     const int part = blockIdx.x % (uint32_t)a.parts, V = (int)a.V, c0 = part * LEN, c1 = min(c0 + LEN, V);
     const T* row = (const T*)a.x + m * a.ldx;
-    Piece<T> p[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; i++) p[i] = load_logits(row, c0 + (i * NT + t) * CH, V);
     Teacher<NW, KPT> teach;
     teach.load(a, m);
-    float z[KPT], q[KPT];
+    const float lse = a.lse_in[m], g1 = a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
+    Piece<T> p[VPT];
 #pragma unroll
-    for (int i = 0; i < KPT; i++) {
-        const int k = teach.l[i].col;
-        z[i] = to_f(row[k >= c0 && k < c1 ? k : c0]);
-    }
-    const float lse = a.lse_in[m];
-    float g = (a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f) * a.scale;
-    teach.form(a, red_t, red_u);
-    g *= teach.unit;
-    put_list(col, prob, teach.l, teach.p, a.top);
+    for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
+    T z[KPT];
+    teach.gather(a, row, c0, c1, z);
+    const float wt = wave_max(teach.top(a));
+    if ((t & 63) == 0) red_t[wave] = wt;
+    __syncthreads();
+    const float wu = wave_sum(teach.powers(a, join_max<NW>(red_t)));
+    if ((t & 63) == 0) red_u[wave] = wu;
+    __syncthreads();
+    teach.form(a, join_sum<NW>(red_u));
+    teach.put(a, cols, probs);
+    const float g = g1 * a.scale * teach.unit;
+    const bool none = lse == neg_inf();   // a row of minus infinities: q = 0
     auto share = [&](float x) {
         const float d = __builtin_fmaf(x, a.scale, -lse);
-        return lse == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
+        return none ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
     };
-#pragma unroll
-    for (int i = 0; i < KPT; i++) q[i] = share(z[i]);
     T* dx = (T*)a.dx + m * a.lddx;
-#pragma unroll
-    for (int i = 0; i < VPT; i++) end_logits(p[i], c0 + (i * NT + t) * CH, V);
-    __syncthreads();   // every load of the part has returned
+    // (every wave's loads are done: each has passed the barriers with what it loaded after them)
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        const int c = c0 + (i * NT + t) * CH;
-        if (c >= V) continue;
         float v[CH];
         logit_values(p[i], v);
 #pragma unroll
         for (int e = 0; e < CH; e++) v[e] = teach.any ? g * share(v[e]) : 0.f;
-        store_some(dx + c, V - c, v);
+        const int c = c0 + (i * NT + t) * CH;
+        if (c < V) store_logits<T, TINY>(dx, c, V, v);
     }
-    if (!teach.any) return;
     __syncthreads();
-    put_listed(a, dx, col, prob, teach.l, q, g, c0, c1);
+    if (!teach.any) return;
+    float q[KPT];
+#pragma unroll
+    for (int i = 0; i < KPT; i++) q[i] = share(to_f(z[i]));
+    teach.store(a, dx, cols, probs, q, g, c0, c1);
 }
 
 // ---------------------------------------------------------------- choice
@@ -663,7 +791,6 @@ struct Shape {
     constexpr int cols() const { return 64 * nw * vpt * CH; }
 };
 constexpr Shape kShapes[] = {{1, 1}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}, {16, 8}, {16, 16}};
-constexpr int kShapeCount = 8;
 
 // Calls f with the shape's sizes as constants.
 template <typename F>
@@ -706,7 +833,7 @@ constexpr int64_t kSlab = (int64_t)1 << 21;
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 size_t log_space(int64_t M, int parts, int64_t top) {
-    return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) + 2 * up256((size_t)M * parts * (size_t)top * 4) : 0;
+    return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) + up256((size_t)M * parts * (size_t)top * 8) : 0;
 }
 
 template <typename T>
@@ -715,15 +842,19 @@ hipError_t run_logprobs(LogArgs a, const Plan& plan, char* ws, hipStream_t strea
     const int64_t M = a.M, slab = kSlab / plan.parts;
     if (plan.parts > 1) {
         a.stat = (Stat*)ws;
-        a.val = (float*)(ws + up256((size_t)M * a.parts * sizeof(Stat)));
-        a.col = (int32_t*)((char*)a.val + up256((size_t)M * a.parts * a.top * 4));
+        a.ranks = (uint64_t*)(ws + up256((size_t)M * a.parts * sizeof(Stat)));
     }
     for (int64_t m0 = 0; m0 < M; m0 += slab) {
         a.M = M - m0 < slab ? M - m0 : slab;
         hipError_t e = by_shape(plan.shape, [&](auto nw, auto vpt) {
             constexpr int NW = decltype(nw)::value, VPT = decltype(vpt)::value;
+            if constexpr (VPT == 1)
+                if (a.V < CH) {
+                    hipLaunchKernelGGL((logprobs_kernel<T, NW, VPT, true>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
+                    return hipGetLastError();
+                }
             if constexpr (sizeof(T) * VPT <= 32)
-                hipLaunchKernelGGL((logprobs_kernel<T, NW, VPT>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
+                hipLaunchKernelGGL((logprobs_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
             return hipGetLastError();
         });
         if (e == hipSuccess && a.parts > 1) {
@@ -765,8 +896,13 @@ hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
         a.M = M - m0 < slab ? M - m0 : slab;
         const hipError_t e = by_shape(shape, [&](auto nw, auto vpt) {
             constexpr int NW = decltype(nw)::value, VPT = decltype(vpt)::value;
+            if constexpr (VPT == 1)
+                if (a.V < CH) {
+                    hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, true>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
+                    return hipGetLastError();
+                }
             if constexpr (NW <= 4)
-                hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
+                hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
@@ -790,11 +926,16 @@ hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t strea
         a.M = M - m0 < slab ? M - m0 : slab;
         hipError_t e = by_shape(plan.shape, [&](auto nw, auto vpt) {
             constexpr int NW = decltype(nw)::value, VPT = decltype(vpt)::value;
+            const dim3 grid((unsigned)(a.M * a.parts)), block(64 * NW);
+            if constexpr (VPT == 1)
+                if (a.V < CH) {
+                    if (grad) hipLaunchKernelGGL((distill_kernel<T, NW, VPT, true, true>), grid, block, 0, stream, a);
+                    else hipLaunchKernelGGL((distill_kernel<T, NW, VPT, true, false>), grid, block, 0, stream, a);
+                    return hipGetLastError();
+                }
             if constexpr (sizeof(T) * VPT <= 32) {
-                if (grad)
-                    hipLaunchKernelGGL((distill_kernel<T, NW, VPT, true>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
-                else
-                    hipLaunchKernelGGL((distill_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
+                if (grad) hipLaunchKernelGGL((distill_kernel<T, NW, VPT, false, true>), grid, block, 0, stream, a);
+                else hipLaunchKernelGGL((distill_kernel<T, NW, VPT, false, false>), grid, block, 0, stream, a);
             }
             return hipGetLastError();
         });
