@@ -46,7 +46,7 @@ __device__ __forceinline__ uint64_t rank_of(float v, int col) { return (uint64_t
 __device__ __forceinline__ int rank_col(uint64_t r) { return (int)~(uint32_t)r; }
 
 // ---------------------------------------------------------------- reductions
-// Row-local steps of a wave: after the first two, four neighbouring lanes have the same, after four, sixteen.
+// Row-local steps of a wave: after the first two, four neighbouring lanes have the same, after three, eight, after four, sixteen.
 template <int CTRL>
 __device__ __forceinline__ float lane_step(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
@@ -56,9 +56,12 @@ __device__ __forceinline__ float max_of_4(float v) {
     v = fmaxf(v, lane_step<0xB1>(v));
     return fmaxf(v, lane_step<0x4E>(v));
 }
-__device__ __forceinline__ float max_of_16(float v) {
+__device__ __forceinline__ float max_of_8(float v) {
     v = max_of_4(v);
-    v = fmaxf(v, lane_step<0x141>(v));
+    return fmaxf(v, lane_step<0x141>(v));
+}
+__device__ __forceinline__ float max_of_16(float v) {
+    v = max_of_8(v);
     return fmaxf(v, lane_step<0x140>(v));
 }
 __device__ __forceinline__ float max_of_rows(float v) {   // sixteen lanes have the same
@@ -72,20 +75,25 @@ __device__ __forceinline__ float wave_sum(float v) {
     v += lane_step<0x140>(v);
     return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
-// Of the NW values that the waves left in LDS.
+// Of the NW values that the waves left in LDS, each lane reading one of them; uniform.  (As all lane steps: by whole waves.)
 template <int NW>
 __device__ __forceinline__ float join_max(const float* red) {
-    float v = red[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) v = fmaxf(v, red[i]);
-    return v;
+    const float v = red[threadIdx.x & (NW - 1)];
+    if constexpr (NW == 1) return lane_of(v, 0);
+    if constexpr (NW == 4) return lane_of(max_of_4(v), 0);
+    if constexpr (NW == 8) return lane_of(max_of_8(v), 0);
+    return lane_of(max_of_16(v), 0);
 }
 template <int NW>
 __device__ __forceinline__ float join_sum(const float* red) {
-    float v = red[0];
-#pragma unroll
-    for (int i = 1; i < NW; i++) v += red[i];
-    return v;
+    float v = red[threadIdx.x & (NW - 1)];
+    if constexpr (NW > 1) {
+        v += lane_step<0xB1>(v);
+        v += lane_step<0x4E>(v);
+    }
+    if constexpr (NW > 4) v += lane_step<0x141>(v);
+    if constexpr (NW > 8) v += lane_step<0x140>(v);
+    return lane_of(v, 0);
 }
 
 // ---------------------------------------------------------------- a row in registers
@@ -157,10 +165,24 @@ __device__ __forceinline__ Piece<T> pick(const Piece<T> (&p)[VPT], int want) {
     return x;
 }
 
-// What exponents of a row are taken from: the maximum, or 0 where there is none.  An element's power is 2^((x - m) c2),
-// c2 = scale log2 e.  (One multiply-add, x c2 - m c2, would do but for rows of a type's lowest value, whose m c2 is no 32-bit number.)
-__device__ __forceinline__ float base_of(float top) { return top == neg_inf() ? 0.f : top; }
-__device__ __forceinline__ float power_of(float x, float base, float c2) { return __builtin_amdgcn_exp2f((x - base) * c2); }
+// What exponents of a row are taken from.  With c2 = scale log2 e an element's power is 2^(x c2 - mc), one multiply-add,
+// with mc = m c2 rounded; all of a row's are 2^r times too large, r = m c2 - mc, which the sums are freed of once.  Where
+// |m c2| is above 2^30 (a row of a type's lowest value, say) that r could be large; but whatever is not equal to m is then 2^6 or more
+// below it (a step of 32 bits is 2^-24 of a value), its power nothing beside that of m.  A power of two in c2's place, with
+// which m c2 is exact and any other value 2^100 below it, keeps the equals and drops the others.
+struct Base {
+    float c2, mc, r;
+    __device__ __forceinline__ Base(float top, float c) {   // (a row without a maximum: 0 in its place)
+        const float m = top == neg_inf() ? 0.f : top;
+        const uint32_t expo = __float_as_uint(m) >> 23 & 255u;
+        const bool far = fabsf(m * c) > 0x1p30f && expo < 255u;
+        c2 = far ? __uint_as_float((min(380u - expo, 254u)) << 23) : c;   // 2^126 over m's power of two
+        mc = m * c2;
+        r = __builtin_fmaf(m, c2, -mc);
+    }
+    __device__ __forceinline__ float arg(float x) const { return __builtin_fmaf(x, c2, -mc); }
+    __device__ __forceinline__ float power(float x) const { return __builtin_amdgcn_exp2f(arg(x)); }
+};
 
 // A row's (or a part's) statistics: the maximum, S = sum 2^u and W = sum u 2^u of u = (x - m) c2.  A row
 // of minus infinities has -inf, 0 and 0; a NaN or an infinity in the row leaves a NaN in S.
@@ -168,7 +190,7 @@ struct Stat {
     float m, s, w;
     __device__ __forceinline__ bool empty() const { return m == neg_inf() && s == 0.f; }
     __device__ __forceinline__ float log() const { return logf(s); }
-    __device__ __forceinline__ float base() const { return base_of(m); }
+    __device__ __forceinline__ float base() const { return m == neg_inf() ? 0.f : m; }
     __device__ __forceinline__ float lse(float scale, float logs) const { return empty() ? neg_inf() : scale * base() + logs; }
     __device__ __forceinline__ float logp(float scale, float logs, float x) const { return empty() ? neg_inf() : scale * (x - base()) - logs; }
     __device__ __forceinline__ float entropy(float logs) const { return empty() ? 0.f : logs - kLn2 * (w / s); }
@@ -182,9 +204,10 @@ __device__ __forceinline__ void forget_values(Piece<T> (&p)[VPT]) {
 #pragma unroll
         for (int w = 0; w < (int)(sizeof(p[i].w) / 4); w++) asm volatile("" : "+v"(p[i].w[w]));
 }
-// S and W over a thread's pieces; KEEP: the powers stay in e.
-template <typename T, int VPT, bool WANT_W, bool KEEP>
-__device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], float base, float c2, float& s, float& w, float (&e)[KEEP ? VPT : 1][CH]) {
+// S and W over a thread's pieces, both as their powers are; KEEP: the powers stay in e.  GUARD: there may be minus
+// infinities, whose terms of W are 0; without it they leave W a NaN.
+template <typename T, int VPT, bool WANT_W, bool KEEP, bool GUARD>
+__device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], const Base& b, float& s, float& w, float (&e)[KEEP ? VPT : 1][CH]) {
     if (sizeof(T) == 2) forget_values(p);
     s = w = 0.f;
 #pragma unroll
@@ -193,23 +216,34 @@ __device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], float base, float c
         logit_values(p[i], v);
 #pragma unroll
         for (int k = 0; k < CH; k++) {
-            const float u = (v[k] - base) * c2, x = __builtin_amdgcn_exp2f(u);
+            const float u = b.arg(v[k]), x = __builtin_amdgcn_exp2f(u);
             s += x;
-            if (WANT_W) w = __builtin_fmaf(x, fmaxf(u, -0x1p100f), w);   // (minus infinity times 0)
+            if (WANT_W) w = __builtin_fmaf(x, GUARD ? fmaxf(u, -0x1p100f) : u, w);
             if (KEEP) e[i][k] = x;
         }
     }
     if (sizeof(T) == 2 && !KEEP) forget_values(p);
 }
+
+// The larger of three.  (fmaxf would first quiet signalling NaNs, one instruction for each; what one
+// does to a maximum does not matter: its row is NaN by its power.  The compiler does not know the
+// instruction's result for one that a lane step has to wait for: it goes through an operation of its own first.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// A thread's largest, and that of each piece.
 template <typename T, int VPT>
-__device__ __forceinline__ float max_of(const Piece<T> (&p)[VPT]) {
+__device__ __forceinline__ float max_of(const Piece<T> (&p)[VPT], float (&top)[VPT]) {
     float mx = neg_inf();
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         float v[CH];
         logit_values(p[i], v);
-#pragma unroll
-        for (int e = 0; e < CH; e++) mx = fmaxf(mx, v[e]);
+        top[i] = max3(max3(max3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]);
+        top[i] = fmaxf(top[i], v[7]);
+        mx = fmaxf(mx, top[i]);
     }
     return mx;
 }
@@ -271,8 +305,7 @@ struct Select {
 
     // hits(v, e, at): f gets a piece's hits as a mask, its values and its place
     template <typename Hit, typename F>
-    __device__ __forceinline__ void piece(const Piece<T> (&p)[VPT], int i, Hit hit, F f) {
-        const Piece<T> x = pick(p, i);
+    __device__ __forceinline__ void piece(const Piece<T>& x, int i, Hit hit, F f) {
         const Place<TINY> at(c0 + (i * NT + (int)threadIdx.x) * CH, V);
         float v[CH];
         logit_values(x, v);
@@ -281,21 +314,21 @@ struct Select {
         for (int e = 0; e < CH; e++) mask |= (hit(v[e]) && at.own(e) ? 1u : 0u) << e;
         f(mask, v, at.from);
     }
-    // All that hit, in any order; what is past kCand is only counted.
-    template <typename Hit>
-    __device__ __forceinline__ void collect(const Piece<T> (&p)[VPT], Hit hit) {
-#pragma unroll 1
-        for (int i = 0; i < VPT; i++)
-            piece(p, i, hit, [&](uint32_t mask, const float (&v)[CH], int from) {
-                if (!mask) return;
-                int at = lds_add(n, __popc(mask));
+    // All above tau (or: equal to it as well), in any order; what is past kCand is only counted.
+    __device__ __forceinline__ void collect(const Piece<T> (&p)[VPT], const float (&tops)[VPT], float tau, bool equal) {
 #pragma unroll
-                for (int e = 0; e < CH; e++)
-                    if (mask >> e & 1) {
-                        if (at < kCand) cand[at] = rank_of(v[e], from + e);
-                        at++;
-                    }
-            });
+        for (int i = 0; i < VPT; i++)
+            if (tops[i] > tau || (equal && tops[i] == tau))
+                piece(p[i], i, [&](float v) { return v > tau || (equal && v == tau); },
+                      [&](uint32_t mask, const float (&v)[CH], int from) {
+                          int at = lds_add(n, __popc(mask));
+#pragma unroll
+                          for (int e = 0; e < CH; e++)
+                              if (mask >> e & 1) {
+                                  if (at < kCand) cand[at] = rank_of(v[e], from + e);
+                                  at++;
+                              }
+                      });
     }
     // The `need` equals of tau with the lowest columns, behind the first n0.
     __device__ __forceinline__ int equals(const Piece<T> (&p)[VPT], float tau, int n0, int need) {
@@ -303,7 +336,7 @@ struct Select {
         int got = 0;
 #pragma unroll 1
         for (int i = 0; i < VPT && got < need; i++)   // (the same for all threads)
-            piece(p, i, [&](float v) { return v == tau; }, [&](uint32_t mask, const float (&v)[CH], int from) {
+            piece(pick(p, i), i, [&](float v) { return v == tau; }, [&](uint32_t mask, const float (&v)[CH], int from) {
                 int incl = __popc(mask);
 #pragma unroll
                 for (int o = 1; o < 64; o *= 2) {
@@ -338,7 +371,7 @@ struct Select {
             int c = 0;
 #pragma unroll 1
             for (int i = 0; i < VPT; i++)
-                piece(p, i, [&](float v) { return v == v && order_key(v) >= want; },
+                piece(pick(p, i), i, [&](float v) { return v == v && order_key(v) >= want; },
                       [&](uint32_t mask, const float (&)[CH], int) { c += __popc(mask); });
 #pragma unroll
             for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o, kWave);
@@ -352,28 +385,21 @@ struct Select {
         }
         return key;
     }
-    __device__ __forceinline__ int restart() {
-        __syncthreads();
-        if (threadIdx.x == 0) *n = 0;
-        __syncthreads();
-        return 0;
-    }
-    // Number of candidates, among them the top ones; mx: this thread's largest.
-    __device__ __forceinline__ int run(const Piece<T> (&p)[VPT], float mx, float tau, int top) {
-        if (mx >= tau) collect(p, [&](float v) { return v >= tau; });
-        __syncthreads();
-        int count = *n;
-        if (count <= kCand) return count;
-        restart();
-        if (mx > tau) collect(p, [&](float v) { return v > tau; });
-        __syncthreads();
-        count = *n;
-        if (count > kCand) {
-            tau = key_value(kth(p, top));
-            restart();
-            if (mx > tau) collect(p, [&](float v) { return v > tau; });
+    // Number of candidates, among them the top ones; tops: the pieces' largest.
+    __device__ __forceinline__ int run(Piece<T> (&p)[VPT], const float (&tops)[VPT], float tau, int top) {
+        int count;
+#pragma unroll 1
+        for (int pass = 0;; pass++) {   // all that reach the bound; if too many, those above it; if too many, those above the top-th
+            forget_values(p);                // (and nothing that every pass needs is formed, and kept, before the first)
+            asm volatile("" : "+s"(V));
+            collect(p, tops, tau, pass == 0);
             __syncthreads();
-            count = min(*n, kCand);
+            count = *n;
+            if (count <= kCand) break;
+            if (pass == 1) tau = key_value(kth(p, top));
+            __syncthreads();
+            if (threadIdx.x == 0) *n = 0;
+            __syncthreads();
         }
         if (count < top) {
             count += equals(p, tau, count, top - count);
@@ -385,10 +411,10 @@ struct Select {
 
 // Waves that a SIMD is to hold: two workgroups of sixteen a CU, one loading while the other computes, where 64 registers do.
 template <typename T>
-constexpr int two_a_cu(int nw, int vpt) { return nw == 16 && vpt <= 4 && vpt * (int)sizeof(T) <= 16 ? 8 : 1; }
+constexpr int two_a_cu(int nw, int vpt) { return nw == 16 && vpt <= 4 && vpt * (int)sizeof(T) <= 8 ? 8 : 1; }
 
 template <typename T, int NW, int VPT, bool TINY>
-__global__ __launch_bounds__(64 * NW) void logprobs_kernel(LogArgs a) {
+__global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void logprobs_kernel(LogArgs a) {
     constexpr int NT = 64 * NW, LEN = NT * VPT * CH;
     __shared__ float red_m[NW], red_s[NW], red_w[NW], tau_s;
     __shared__ __attribute__((aligned(16))) float group[64];
@@ -406,10 +432,11 @@ __global__ __launch_bounds__(64 * NW) void logprobs_kernel(LogArgs a) {
     if (t == 0) n_s = 0;
 #pragma unroll
     for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
-    const float mx = max_of(p);
+    float top[VPT];
+    const float mx = max_of(p, top);
     // 64 groups of NW neighbouring threads
-    const float m4 = max_of_4(mx), m16 = max_of_16(m4);
-    if (t % NW == 0) group[t / NW] = NW == 1 ? mx : (NW == 4 ? m4 : m16);
+    const float m16 = max_of_16(mx), of_group = NW == 1 ? mx : (NW == 4 ? max_of_4(mx) : (NW == 8 ? max_of_8(mx) : m16));
+    if (t % NW == 0) group[t / NW] = of_group;   // (lane steps take all lanes: none of them in a branch)
     const float wm = max_of_rows(m16);
     if ((t & 63) == 0) red_m[wave] = wm;
     __syncthreads();
@@ -419,14 +446,17 @@ __global__ __launch_bounds__(64 * NW) void logprobs_kernel(LogArgs a) {
         const float tau = bound_of(group, group[t], a.top);
         if (t == 0) tau_s = tau;
     }
+    const Base base(st.m, a.c2);
     float none[1][CH];
-    row_sums<T, VPT, true, false>(p, st.base(), a.c2, st.s, st.w, none);
+    row_sums<T, VPT, true, false, false>(p, base, st.s, st.w, none);
+    if (__any(st.w != st.w)) row_sums<T, VPT, true, false, true>(p, base, st.s, st.w, none);   // masks here, or past the row's end
     st.s = wave_sum(st.s);
     st.w = wave_sum(st.w);
     if ((t & 63) == 0) red_s[wave] = st.s, red_w[wave] = st.w;
     __syncthreads();
-    st.s = join_sum<NW>(red_s);
-    st.w = join_sum<NW>(red_w);
+    const float back = __builtin_amdgcn_exp2f(-base.r);
+    st.s = join_sum<NW>(red_s) * back;
+    st.w = join_sum<NW>(red_w) * back - base.r * st.s;
     const float logs = st.log();
     if (t == 0) {
         if (a.parts == 1) put_scalars(a, m, st, logs, tok, to_f(x_tok));
@@ -434,7 +464,7 @@ __global__ __launch_bounds__(64 * NW) void logprobs_kernel(LogArgs a) {
     }
     if (!a.top) return;
     Select<T, NW, VPT, TINY> sel{cand, &n_s, red_c, c0, V};
-    const int n = sel.run(p, mx, tau_s, a.top);
+    const int n = sel.run(p, top, tau_s, a.top);
     auto put = [&](int r, uint64_t rank) {
         if (a.parts == 1) put_top(a, m, r, st, logs, rank);
         else a.ranks[(m * a.parts + part) * a.top + r] = rank;
@@ -575,7 +605,7 @@ struct Teacher {
         return s;
     }
     __device__ __forceinline__ void form(const DistArgs& a, float s) {
-        any = s != 0.f;
+        any = __builtin_amdgcn_readfirstlane(s != 0.f);
         unit = s / s;
         const float logs = logf(s);
 #pragma unroll
@@ -646,18 +676,20 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
     teach.gather(a, row, 0, V, z);
 #pragma unroll
     for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
-    const float wm = wave_max(max_of(p)), wt = wave_max(teach.top(a));
+    float tops[VPT];
+    const float wm = wave_max(max_of(p, tops)), wt = wave_max(teach.top(a));
     if ((t & 63) == 0) red_m[wave] = wm, red_t[wave] = wt;
     __syncthreads();
     Stat st;
     st.m = join_max<NW>(red_m);
-    const float base = st.base();
+    const Base base(st.m, a.c2);
     float e[KEEP ? VPT : 1][CH];
-    row_sums<T, VPT, false, KEEP>(p, base, a.c2, st.s, st.w, e);
+    row_sums<T, VPT, false, KEEP, false>(p, base, st.s, st.w, e);
     const float ws = wave_sum(st.s), wu = wave_sum(teach.powers(a, join_max<NW>(red_t)));
     if ((t & 63) == 0) red_s[wave] = ws, red_u[wave] = wu;
     __syncthreads();
-    st.s = join_sum<NW>(red_s);
+    const float sum = join_sum<NW>(red_s);   // as the powers are
+    st.s = sum * __builtin_amdgcn_exp2f(-base.r);
     st.w = 0.f;
     if (a.parts > 1) {
         if (t == 0) a.stat[m * a.parts + part] = st;
@@ -670,18 +702,18 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
     if (GRAD) teach.put(a, cols, probs);
     if constexpr (GRAD) {
         // Every load of the row has returned, here and, past the barriers above, in the other waves: dx may be x.
-        const float inv = st.s == 0.f ? 0.f : 1.f / st.s;
-        const float g = g1 * a.scale * teach.unit, f = g * inv;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum, g = g1 * a.scale * teach.unit, f = g * inv;
         T* dx = (T*)a.dx + m * a.lddx;
 #pragma unroll
         for (int i = 0; i < VPT; i++) {
             float v[CH];
             if constexpr (!KEEP) logit_values(p[i], v);
+            if (teach.any) {   // (uniform)
 #pragma unroll
-            for (int k = 0; k < CH; k++) {
-                if constexpr (KEEP) v[k] = e[i][k] * f;
-                else v[k] = power_of(v[k], base, a.c2) * f;
-                if (!teach.any) v[k] = 0.f;
+                for (int k = 0; k < CH; k++) v[k] = (KEEP ? e[KEEP ? i : 0][k] : base.power(v[k])) * f;
+            } else {
+#pragma unroll
+                for (int k = 0; k < CH; k++) v[k] = 0.f;
             }
             const int c = (i * NT + t) * CH;
             if (c < V) store_logits<T, TINY>(dx, c, V, v);
@@ -690,14 +722,15 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
         if (teach.any) {
             float q[KPT];
 #pragma unroll
-            for (int i = 0; i < KPT; i++) q[i] = power_of(to_f(z[i]), base, a.c2) * inv;
+            for (int i = 0; i < KPT; i++) q[i] = base.power(to_f(z[i])) * inv;
             teach.store(a, dx, cols, probs, q, g, 0, V);
         }
     } else {
         __syncthreads();
     }
+    const float loss = join_sum<NW>(red_l);
     if (t == 0) {
-        a.loss[m] = join_sum<NW>(red_l);
+        a.loss[m] = loss;
         if (a.lse) a.lse[m] = st.lse(a.scale, logs);
     }
 }
@@ -725,8 +758,9 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistArgs a) {
     const float wl = wave_sum(teach.loss(a, z, st, logs));
     if ((t & 63) == 0) red_l[wave] = wl;
     __syncthreads();
+    const float loss = join_sum<4>(red_l);
     if (t == 0) {
-        a.loss[m] = join_sum<4>(red_l);
+        a.loss[m] = loss;
         if (a.lse) a.lse[m] = st.lse(a.scale, logs);
     }
 }
