@@ -20,6 +20,7 @@
 
 #include <math.h>
 
+#include <initializer_list>
 #include <type_traits>
 
 namespace niti {
@@ -144,9 +145,18 @@ __device__ __forceinline__ void mask_logits(Piece<T>& p, int c, int V) {
     __builtin_memcpy(p.w, t, sizeof(t));
 }
 template <typename T, bool TINY>
-__device__ __forceinline__ void store_logits(T* row, int c, int V, const float (&v)[CH]) {
+__device__ __forceinline__ void store_logits(T* row, int c, int V, const float (&v)[CH], bool stream) {
     const Place<TINY> at(c, V);
-    if (at.whole()) {
+    if (at.whole() && stream) {
+        typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+        T t[CH];
+        any4 w[sizeof(t) / 16];
+#pragma unroll
+        for (int e = 0; e < CH; e++) t[e] = from_f<T>(v[e]);
+        __builtin_memcpy(w, t, sizeof(t));
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(t) / 16); i++) __builtin_nontemporal_store(w[i], (any4*)(row + c) + i);
+    } else if (at.whole()) {
         store_n(row + c, v);
     } else {
 #pragma unroll
@@ -547,7 +557,7 @@ struct DistArgs {
     const float* dloss;
     void* dx;
     int64_t ldx, ldt, ldi, lddx, M, V;
-    int32_t top, t_type, parts, g_step;
+    int32_t top, t_type, parts, g_step, stream;
     float scale, c2;
     Stat* stat;
 };
@@ -716,7 +726,7 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
                 for (int k = 0; k < CH; k++) v[k] = 0.f;
             }
             const int c = (i * NT + t) * CH;
-            if (c < V) store_logits<T, TINY>(dx, c, V, v);
+            if (c < V) store_logits<T, TINY>(dx, c, V, v, a.stream);
         }
         __syncthreads();   // the row's stores before the listed columns'
         if (teach.any) {
@@ -808,7 +818,7 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
 #pragma unroll
         for (int e = 0; e < CH; e++) v[e] = teach.any ? g * share(v[e]) : 0.f;
         const int c = c0 + (i * NT + t) * CH;
-        if (c < V) store_logits<T, TINY>(dx, c, V, v);
+        if (c < V) store_logits<T, TINY>(dx, c, V, v, a.stream);
     }
     __syncthreads();
     if (!teach.any) return;
@@ -819,24 +829,26 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
 }
 
 // ---------------------------------------------------------------- choice
-// Kernels by the columns that a workgroup holds.
+// Kernels by the waves of a workgroup and the pieces of a thread, in the order of the columns that they hold.
 struct Shape {
     int nw, vpt;
     constexpr int cols() const { return 64 * nw * vpt * CH; }
 };
-constexpr Shape kShapes[] = {{1, 1}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}, {16, 8}, {16, 16}};
+enum { k512, k2048, k4096, k8192, k16384, k32768, k32768w, k65536, k131072 };   // (w: of twice the waves)
+constexpr Shape kShapes[] = {{1, 1}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 4}, {16, 8}, {16, 16}};
 
 // Calls f with the shape's sizes as constants.
 template <typename F>
 hipError_t by_shape(int shape, F f) {
     switch (shape) {
-        case 0: return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
-        case 1: return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
-        case 2: return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
-        case 3: return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
-        case 4: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
-        case 5: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
-        case 6: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
+        case k512: return f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+        case k2048: return f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+        case k4096: return f(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+        case k8192: return f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+        case k16384: return f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+        case k32768: return f(std::integral_constant<int, 8>(), std::integral_constant<int, 8>());
+        case k32768w: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+        case k65536: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
         default: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 16>());
     }
 }
@@ -844,21 +856,46 @@ hipError_t by_shape(int shape, F f) {
 struct Plan {
     int shape, parts;
 };
-// The smallest shape that holds a whole row; a longer row in parts of the largest.
-Plan whole_rows(int64_t V, int type) {
-    const int most = type == NITI_F32 ? 6 : 7;   // (16 pieces of 32 bits a thread are all the registers there are)
-    for (int i = 0; i <= most; i++)
-        if (V <= kShapes[i].cols()) return Plan{i, 1};
-    return Plan{most, (int)((V + kShapes[most].cols() - 1) / kShapes[most].cols())};
-}
-// Few long rows: parts for all CUs.
-Plan split_rows(int64_t M, int64_t V, int type) {
-    Plan p = whole_rows(V, type);
-    while (p.shape > 2 && M * p.parts < 128 && (V + kShapes[p.shape].cols() / 2 - 1) / (kShapes[p.shape].cols() / 2) <= kPartsMax && V > 32768) {
-        p.shape--;
-        p.parts = (int)((V + kShapes[p.shape].cols() - 1) / kShapes[p.shape].cols());
+inline Plan in_parts(int64_t V, int shape) { return Plan{shape, (int)((V + kShapes[shape].cols() - 1) / kShapes[shape].cols())}; }
+// Parts of the first of the given shapes that makes no more than kPartsMax of them.
+inline Plan in_parts(int64_t V, std::initializer_list<int> shapes) {
+    Plan p{};
+    for (int s : shapes) {
+        p = in_parts(V, s);
+        if (p.parts <= kPartsMax) break;
     }
     return p;
+}
+// The smallest shape for a whole row of up to 16384 columns.
+inline Plan short_row(int64_t V) {
+    int s = k512;
+    while (V > kShapes[s].cols()) s++;
+    return Plan{s, 1};
+}
+
+// Whole rows need no second launch (3 us); parts of few registers leave more of them on a CU.  Both ways (us; whole, in parts),
+// 16 bits: 32000 columns, 1 row 8.7, 10.6, 1000 21.5, 26.0, 4096 62, 79; 60000 columns, 256 rows 14.3, 18.1, 1000 50.1, 44.1;
+// in 32 bits: 32000 columns, 256 rows 10.7, 14.2, 1000 36.9, 32.0, 2000 67, 56; 60000 columns, 64 rows 13.1, 12.4.  Parts of
+// 32768 (16 bits) where there are 1024 of them: 1000 x 128000 69 for 87 in parts of 8192, 300 x 50000 23 for 18.
+Plan logprobs_plan(int64_t M, int64_t V, int type) {
+    if (V <= 16384) return short_row(V);
+    const bool half = type != NITI_F32;
+    if (V <= 32768 && (half || M <= 512)) return Plan{k32768w, 1};
+    if (half && V <= 65536 && M <= 512) return Plan{k65536, 1};
+    if (!half) return in_parts(V, {k4096, k8192, k16384, k32768w, k65536});
+    const Plan wide = in_parts(V, k32768w);
+    return M * wide.parts >= 1024 ? in_parts(V, {k32768w, k65536}) : in_parts(V, {k8192, k16384, k32768w, k65536});
+}
+
+// With the gradient a second reading costs more than the registers of a whole row: parts only where those do not hold it (77 x
+// 128001 in 32 bits: parts of 8192 30 us, of 65536 37), or for few rows of more than 65536 (1 x 128000 in 16 bits 14.7 for 20; 1000 of them
+// 127 for 102).  32768 columns by eight waves: 4096 x 32000 in 16 bits 102 us, by sixteen 106.
+Plan distill_plan(int64_t M, int64_t V, int type) {
+    if (V <= 16384) return short_row(V);
+    if (V <= 32768) return Plan{k32768, 1};
+    if (V <= 65536) return Plan{k65536, 1};
+    if (V <= 131072 && type != NITI_F32 && M >= 64) return Plan{k131072, 1};
+    return in_parts(V, {k8192, k16384, k32768, k65536});
 }
 
 // A launch holds fewer than 2^32 threads: very many rows go in slabs.
@@ -887,7 +924,7 @@ hipError_t run_logprobs(LogArgs a, const Plan& plan, char* ws, hipStream_t strea
                     hipLaunchKernelGGL((logprobs_kernel<T, NW, VPT, true>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
                     return hipGetLastError();
                 }
-            if constexpr (sizeof(T) * VPT <= 32)
+            if constexpr (!(NW == 8 && VPT == 8) && VPT <= 8)
                 hipLaunchKernelGGL((logprobs_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
             return hipGetLastError();
         });
@@ -919,12 +956,16 @@ void next_slab(DistArgs& a, int64_t slab) {
     if (a.dx) a.dx = (T*)a.dx + slab * a.lddx;
 }
 
+// Whether a gradient goes past the caches: more than the eight L2 hold would only push out what is still to be read (4096 x 32000 in
+// 16 bits, with the loss 119 -> 102 us, alone 112 -> 89).
+inline int32_t streams(int64_t M, int64_t V, size_t size) { return M * V * (int64_t)size > ((int64_t)32 << 20); }
+
 template <typename T>
 hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
-    // 8192 columns a workgroup where rows are longer than that
-    int shape = 0;
-    while (shape < 3 && a.V > kShapes[shape].cols()) shape++;
-    a.parts = (int)((a.V + kShapes[shape].cols() - 1) / kShapes[shape].cols());
+    // 4096 columns a workgroup where rows are longer than 512
+    const int shape = a.V <= 512 ? k512 : k4096;
+    a.parts = in_parts(a.V, shape).parts;
+    a.stream = streams(a.M, a.V, sizeof(T));
     const int64_t M = a.M, slab = kSlab / a.parts;
     for (int64_t m0 = 0; m0 < M; m0 += slab) {
         a.M = M - m0 < slab ? M - m0 : slab;
@@ -935,7 +976,7 @@ hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
                     hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, true>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
                     return hipGetLastError();
                 }
-            if constexpr (NW <= 4)
+            if constexpr ((NW == 1 && VPT == 1) || (NW == 4 && VPT == 2))
                 hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
             return hipGetLastError();
         });
@@ -948,6 +989,7 @@ hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
 template <typename T>
 hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t stream) {
     a.parts = plan.parts;
+    a.stream = streams(a.M, a.V, sizeof(T));
     const DistArgs whole = a;
     const int64_t M = a.M, slab = kSlab / plan.parts;
     const bool grad = a.dx && plan.parts == 1;
@@ -967,7 +1009,7 @@ hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t strea
                     else hipLaunchKernelGGL((distill_kernel<T, NW, VPT, true, false>), grid, block, 0, stream, a);
                     return hipGetLastError();
                 }
-            if constexpr (sizeof(T) * VPT <= 32) {
+            if constexpr (!(NW == 16 && VPT == 4) && sizeof(T) * VPT <= 32) {
                 if (grad) hipLaunchKernelGGL((distill_kernel<T, NW, VPT, false, true>), grid, block, 0, stream, a);
                 else hipLaunchKernelGGL((distill_kernel<T, NW, VPT, false, false>), grid, block, 0, stream, a);
             }
@@ -993,12 +1035,12 @@ inline bool fine_scale(float s) { return s > 0.f && s < INFINITY; }
 // For either type's plan: the caller's sizes do not say which.
 size_t logprobs_workspace(int64_t M, int64_t V, int64_t top) {
     if (M < 1 || V < 1 || top < 0 || top > kTopMax || top > V || M >= kMaxDim || V >= kMaxLd) return 0;
-    const size_t wide = log_space(M, split_rows(M, V, NITI_F32).parts, top), half = log_space(M, split_rows(M, V, NITI_BF16).parts, top);
+    const size_t wide = log_space(M, logprobs_plan(M, V, NITI_F32).parts, top), half = log_space(M, logprobs_plan(M, V, NITI_BF16).parts, top);
     return wide > half ? wide : half;
 }
 size_t distill_workspace(int64_t M, int64_t V) {
     if (M < 1 || V < 1 || M >= kMaxDim || V >= kMaxLd) return 0;
-    const int wide = whole_rows(V, NITI_F32).parts, half = whole_rows(V, NITI_BF16).parts;
+    const int wide = distill_plan(M, V, NITI_F32).parts, half = distill_plan(M, V, NITI_BF16).parts;
     const int parts = wide > half ? wide : half;
     return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) + up256((size_t)M * 4) : 0;
 }
@@ -1018,7 +1060,7 @@ niti_status niti_token_logprobs(const void* x, int64_t ldx, const int32_t* token
     if (M == 0) return NITI_OK;
     if (!x || (logp != nullptr) != (tokens != nullptr) || ((top_logp || top_idx) != (top > 0))) return NITI_ERR_NULL;
     if (bad_ld(M > 1 ? ldx : V, V, false)) return NITI_ERR_SHAPE;
-    const Plan plan = split_rows(M, V, type);
+    const Plan plan = logprobs_plan(M, V, type);
     if (plan.parts > 1) {
         if (!ws || ws_bytes < log_space(M, plan.parts, top)) return NITI_ERR_WORKSPACE;
         if ((uintptr_t)ws & 15) return NITI_ERR_ARG;
@@ -1042,7 +1084,7 @@ niti_status niti_distill_fwd(const void* x, int64_t ldx, const void* t_val, int6
     if (bad_ld(M > 1 ? ldx : V, V, false) || bad_ld(M > 1 ? ldt : top, top, false) || bad_ld(M > 1 ? ldi : top, top, false) ||
         (dx && bad_ld(M > 1 ? lddx : V, V, true)) || (dloss && dloss_n != 1 && dloss_n != M))
         return NITI_ERR_SHAPE;
-    const Plan plan = whole_rows(V, type);
+    const Plan plan = distill_plan(M, V, type);
     if (plan.parts > 1) {
         if (!ws || ws_bytes < distill_workspace(M, V)) return NITI_ERR_WORKSPACE;
         if ((uintptr_t)ws & 15) return NITI_ERR_ARG;
