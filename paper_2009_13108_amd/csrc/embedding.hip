@@ -22,7 +22,7 @@ namespace {
 constexpr int kSortMax = 16384;   // tokens that one workgroup sorts
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kRounds = kSortMax / kSortThreads;
 constexpr int kBins = 256;
-constexpr int kRun = 16;          // sorted rows of a stretch
+constexpr int kRunMin = 8;        // sorted rows of a stretch: 8 or 16
 constexpr int64_t kMaxTokens = (int64_t)1 << 22;
 
 // ---------------------------------------------------------------- forward
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(EmbArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < CH; e++) v[e] = in ? v[e] * f : 0.f;
-    store_some((T*)a.out + m * a.ldo + c, D - c, v);
+    store_first((T*)a.out + m * a.ldo + c, D - c, v);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -84,22 +84,33 @@ struct EmbBwdArgs {
     int64_t lddy, ldt, M, V, D;
     float alpha;
     int32_t accumulate, passes;   // passes of the sort
+    int32_t run;                  // sorted rows of a stretch
     int32_t sorters;              // workgroups that sort, ahead of those that write zeros
     int32_t *order, *key;         // [M]: rows by token, and their tokens (V for those outside the table)
     int32_t *order1, *key1;       // the same of each chunk, where there are several
     float* part;                  // [stretches][2][D]
 };
 
-// (1) LDS: the chunk's tokens, two lists of places, the waves' counters.
+// (1) LDS: the chunk's tokens, two lists of places, a counter for each digit and wave.
 template <typename TG>
 __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int t = threadIdx.x;
-    if ((int)blockIdx.x >= a.sorters) {   // zeros of every n-th row
+    if ((int)blockIdx.x >= a.sorters) {   // zeros: of a whole table in one go, of spaced rows row by row
+        const int64_t first = (int64_t)blockIdx.x - a.sorters, step = (int64_t)gridDim.x - a.sorters;
         const float zero[CH] = {};
-        for (int64_t r = (int64_t)blockIdx.x - a.sorters; r < a.V; r += (int64_t)gridDim.x - a.sorters) {
-            TG* row = (TG*)a.dtable + r * a.ldt;
-            for (int c = t * CH; c < a.D; c += kSortThreads * CH) store_some(row + c, (int)(a.D - c), zero);
+        if (a.ldt == a.D) {
+            constexpr int64_t BLOCK = (int64_t)kSortThreads * CH;
+            const int64_t n = a.V * a.D;
+            for (int64_t i = first * BLOCK + t * CH; i < n; i += step * BLOCK) {
+                if (i + CH <= n) store_whole<true>((TG*)a.dtable + i, zero);
+                else store_first((TG*)a.dtable + i, (int)(n - i), zero);
+            }
+        } else {
+            for (int64_t r = first; r < a.V; r += step) {
+                TG* row = (TG*)a.dtable + r * a.ldt;
+                for (int c = t * CH; c < a.D; c += kSortThreads * CH) store_first(row + c, (int)(a.D - c), zero);
+            }
         }
         return;
     }
@@ -109,8 +120,8 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
     uint32_t* key = (uint32_t*)lds;
     uint16_t* src = (uint16_t*)(key + room);
     uint16_t* dst = src + room;
-    volatile uint32_t* bins = (volatile uint32_t*)(dst + room);   // [wave][bin]
-    volatile uint32_t* totals = bins + kSortWaves * kBins;        // of the four waves that scan
+    uint16_t* bins = dst + room;                                  // [digit][wave]
+    uint32_t* totals = (uint32_t*)(bins + kSortWaves * kBins);    // of the four waves that scan
     for (int i = t; i < n; i += kSortThreads) {
         const int tok = a.tokens[base + i];
         key[i] = (uint32_t)tok < (uint64_t)a.V ? (uint32_t)tok : (uint32_t)a.V;
@@ -120,38 +131,51 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     for (int pass = 0; pass < a.passes; pass++) {
         const int shift = 8 * pass;
-        for (int i = t; i < kSortWaves * kBins; i += kSortThreads) bins[i] = 0;
+        if (t < 2 * kBins) ((uint4*)bins)[t] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        // A wave's places are consecutive: each counts those of its digit before it, in this wave.
-        uint32_t rank[kRounds];
+        // A wave's places are consecutive.  All of a thread's are read before the first is counted.
+        uint16_t place[kRounds], rank[kRounds];
+        uint8_t digit[kRounds];
 #pragma unroll
         for (int r = 0; r < kRounds; r++) {
-            if (r >= rounds) break;
-            const int i = (wave * rounds + r) * 64 + lane;
-            const bool in = i < n;
-            const uint32_t d = in ? key[src[i]] >> shift & (kBins - 1) : 0u;
-            uint64_t peers = __ballot(in);
+            if (r < rounds) place[r] = src[min((wave * rounds + r) * 64 + lane, n - 1)];
+        }
+#pragma unroll
+        for (int r = 0; r < kRounds; r++) {
+            if (r < rounds) digit[r] = (uint8_t)(key[place[r]] >> shift);
+        }
+        // Each counts those of its digit before it, in this wave.
+#pragma unroll
+        for (int r = 0; r < kRounds; r++) {
+            if (r >= rounds) continue;
+            const bool in = (wave * rounds + r) * 64 + lane < n;
+            const uint32_t d = digit[r];
+            uint32_t lo = 0, hi = 0;   // lanes that differ in a bit
 #pragma unroll
             for (int b = 0; b < 8; b++) {
                 const uint64_t ones = __ballot(d >> b & 1);
-                peers &= d >> b & 1 ? ones : ~ones;
+                const uint32_t mine = (uint32_t)((int32_t)(d << (31 - b)) >> 31);
+                lo |= (uint32_t)ones ^ mine;
+                hi |= (uint32_t)(ones >> 32) ^ mine;
             }
-            volatile uint32_t* bin = bins + wave * kBins + d;
-            const uint32_t old = *bin;
-            rank[r] = old + (uint32_t)__popcll(peers & below);
+            const uint64_t peers = __ballot(in) & ~((uint64_t)hi << 32 | lo);
+            volatile uint16_t* bin = bins + d * kSortWaves + wave;
+            const uint32_t old = *bin, before = (uint32_t)__popcll(peers & below);
+            rank[r] = (uint16_t)(old + before);
             __builtin_amdgcn_wave_barrier();
-            if (in && (peers & below) == 0) *bin = old + (uint32_t)__popcll(peers);
+            if (in && before == 0) *bin = (uint16_t)(old + (uint32_t)__popcll(peers));
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
-        // bins[wave][d] = places of smaller digits, and of this one in the waves before
-        uint32_t sum = 0, incl = 0;
+        // bins[d][wave] = places of smaller digits, and of this one in the waves before: below 2^14
+        uint32_t count[kSortWaves], sum = 0, incl = 0;
         if (t < kBins) {
+            uint16_t c[kSortWaves];
+            __builtin_memcpy(c, __builtin_assume_aligned(bins + t * kSortWaves, 16), sizeof(c));
 #pragma unroll
             for (int w = 0; w < kSortWaves; w++) {
-                const uint32_t c = bins[w * kBins + t];
-                bins[w * kBins + t] = sum;
-                sum += c;
+                count[w] = sum;
+                sum += c[w];
             }
             incl = sum;
 #pragma unroll
@@ -164,25 +188,22 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
         __syncthreads();
         if (t < kBins) {
             uint32_t before = incl - sum;
-            for (int w = 0; w < wave; w++) before += totals[w];
 #pragma unroll
-            for (int w = 0; w < kSortWaves; w++) bins[w * kBins + t] = bins[w * kBins + t] + before;
+            for (int w = 0; w < 3; w++) before += w < wave ? totals[w] : 0u;
+            uint16_t c[kSortWaves];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; w++) c[w] = (uint16_t)(count[w] + before);
+            __builtin_memcpy(__builtin_assume_aligned(bins + t * kSortWaves, 16), c, sizeof(c));
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kRounds; r++) {
-            if (r >= rounds) break;
-            const int i = (wave * rounds + r) * 64 + lane;
-            if (i < n) {
-                const uint16_t p = src[i];
-                dst[bins[wave * kBins + (key[p] >> shift & (kBins - 1))] + rank[r]] = p;
-            }
+            if (r < rounds && (wave * rounds + r) * 64 + lane < n) dst[bins[(int)digit[r] * kSortWaves + wave] + rank[r]] = place[r];
         }
         __syncthreads();
         uint16_t* x = src;
         src = dst, dst = x;
     }
-    __syncthreads();   // (of no pass)
     int32_t *order = a.order1 ? a.order1 : a.order, *keys = a.key1 ? a.key1 : a.key;
     for (int i = t; i < n; i += kSortThreads) {
         const int p = src[i];
@@ -219,51 +240,73 @@ __global__ __launch_bounds__(256) void token_merge_kernel(EmbBwdArgs a) {
 
 constexpr int kSumThreads = 256, kSumCols = kSumThreads * CH;
 
-// (2) A stretch of sorted rows, 2048 columns.  KIND: the number of columns is at least 8 (1), or not (0).
-template <typename T, typename TG, int KIND>
+// A sum into the table's row of token k, on top of old where there is something to add to.
+template <typename TG, int N>
+__device__ __forceinline__ void put_sum(const EmbBwdArgs& a, int64_t k, int c, const float (&sum)[N], float (&old)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; e++) old[e] = a.accumulate ? __builtin_fmaf(a.alpha, sum[e], old[e]) : a.alpha * sum[e];
+    store_first((TG*)a.dtable + k * a.ldt + c, (int)(a.D - c), old);
+}
+
+// (2) A stretch of sorted rows, 2048 columns.  KIND: the number of columns is a multiple of 8 (2), is at least 8 (1), or neither (0).
+// ADD: with each row goes what its token's row in the table holds (read for every row: tokens' last rows are known later than the
+// loads are to go out, and the others hit a cache).
+template <typename T, typename TG, int KIND, bool ADD, int RUN>
 __global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, int slices) {
-    constexpr int AHEAD = sizeof(T) == 4 ? 8 : 16;   // rows in flight
+    constexpr int AHEAD = sizeof(T) == 4 && RUN > 8 ? 8 : RUN;   // rows in flight
     const int64_t s = blockIdx.x / (uint32_t)slices;
     const int D = (int)a.D, c = (int)(blockIdx.x % (uint32_t)slices) * kSumCols + (int)threadIdx.x * CH;
-    const int64_t i0 = s * kRun;
-    const int n = (int)min((int64_t)kRun, a.M - i0);
-    const int32_t* key = a.key + i0;
-    const int32_t* order = a.order + i0;
-    const int32_t before = i0 > 0 ? key[-1] : -1, after = i0 + n < a.M ? key[n] : -1;
+    const int64_t i0 = s * RUN;
+    const int n = (int)min((int64_t)RUN, a.M - i0);
+    // tokens and rows of the stretch, and its neighbours' tokens (-1: none): one load each, lane by lane
+    const int lane = threadIdx.x & 63;
+    const int64_t at = i0 + lane - 1;
+    int32_t keys = a.key[min(max(at, (int64_t)0), a.M - 1)];
+    const int32_t rows = a.order[min(i0 + min(lane, RUN - 1), a.M - 1)];
+    keys = at >= 0 && at < a.M ? keys : -1;
+    auto key_of = [&](int i) { return __builtin_amdgcn_readlane(keys, i + 1); };   // -1 .. RUN
     float sum[CH] = {};
     bool first = true;    // no row of this stretch has ended a token yet
-    int32_t k = key[0];
-#pragma unroll 1
-    for (int j0 = 0; j0 < n; j0 += AHEAD) {
-        Piece<T> p[AHEAD];
+    int32_t k = key_of(0);
+    const int32_t before = key_of(-1);
 #pragma unroll
-        for (int j = 0; j < AHEAD; j++) {
-            const T* row = (const T*)a.dy + (int64_t)order[min(j0 + j, n - 1)] * a.lddy;
-            if constexpr (KIND) p[j] = load_piece<T, false>(row, c, D);
+    for (int j0 = 0; j0 < RUN; j0 += AHEAD) {
+        if (j0 >= n) break;
+        Piece<T> p[AHEAD];
+        Piece<TG> o[ADD ? AHEAD : 1];
+        if constexpr (KIND > 0) {
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++)
+                p[j] = load_piece<T, KIND == 2>((const T*)a.dy + (int64_t)__builtin_amdgcn_readlane(rows, j0 + j) * a.lddy, c, D);
+            if constexpr (ADD) {
+#pragma unroll
+                for (int j = 0; j < AHEAD; j++) {
+                    const int32_t t = key_of(j0 + j);   // (past the end -1)
+                    o[j] = load_piece<TG, KIND == 2>((const TG*)a.dtable + ((uint32_t)t < (uint64_t)a.V ? t : 0) * a.ldt, c, D);
+                }
+            }
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; j++) {
-            const int at = j0 + j;
-            if (at >= n) break;
+            const int i = j0 + j;
+            if (i >= n) break;
             float v[CH];
-            if constexpr (KIND) piece_values<T, false>(p[j], c, D, v);
-            else load_some((const T*)a.dy + (int64_t)order[at] * a.lddy + c, D - c, v);
+            if constexpr (KIND > 0) piece_values<T, KIND == 2>(p[j], c, D, v);
+            else load_some((const T*)a.dy + (int64_t)__builtin_amdgcn_readlane(rows, i) * a.lddy + c, D - c, v);
 #pragma unroll
             for (int e = 0; e < CH; e++) sum[e] += v[e];
-            const int32_t next = at + 1 < n ? key[at + 1] : after;
-            if (next == k && at + 1 < n) continue;
+            const int32_t next = key_of(i + 1);
+            if (next == k && i + 1 < n) continue;
             // the last row of token k here
-            const bool from = first && before == k, on = at + 1 == n && next == k;
+            const bool from = first && before == k, on = i + 1 == n && next == k;
             if (c < D && k < a.V) {
                 if (from || on) {
-                    store_some(a.part + (2 * s + (from ? 0 : 1)) * a.D + c, D - c, sum);
+                    store_first(a.part + (2 * s + (from ? 0 : 1)) * a.D + c, D - c, sum);
                 } else {
-                    TG* row = (TG*)a.dtable + k * a.ldt + c;
-                    float old[CH];
-                    load_some(row, a.accumulate ? D - c : 0, old);
-#pragma unroll
-                    for (int e = 0; e < CH; e++) old[e] = __builtin_fmaf(a.alpha, sum[e], old[e]);
-                    store_some(row, D - c, old);
+                    float old[CH] = {};
+                    if constexpr (ADD && KIND > 0) piece_values<TG, KIND == 2>(o[j], c, D, old);
+                    else if (ADD) load_some((const TG*)a.dtable + k * a.ldt + c, D - c, old);
+                    put_sum<TG>(a, k, c, sum, old);
                 }
             }
 #pragma unroll
@@ -275,34 +318,42 @@ __global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, in
 }
 
 // (3) The token that crosses the end of a stretch that it begins in: its partial sums in order.
+constexpr int kJoinCols = 1024;
 template <typename TG>
 __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slices) {
     const int64_t s = blockIdx.x / (uint32_t)slices;
-    const int c = (int)(blockIdx.x % (uint32_t)slices) * 1024 + (int)threadIdx.x * 4;
-    const int64_t i0 = s * kRun, end = i0 + kRun;   // (the last stretch crosses nothing)
+    const int c = (int)(blockIdx.x % (uint32_t)slices) * kJoinCols + (int)threadIdx.x * 4;
+    const int64_t i0 = s * a.run, end = i0 + a.run;   // (the last stretch crosses nothing)
     if (end >= a.M) return;
-    const int32_t k = a.key[end];
-    if (a.key[end - 1] != k || k >= a.V || (i0 > 0 && a.key[i0 - 1] == k)) return;
-    const int64_t last = (end + count_below(a.key + end, a.M - end, k, true) - 1) / kRun;
+    const int lane = threadIdx.x & 63;
+    // stretches after this one that the token fills to their ends, 64 at a time: the next stretch's first token, and the one before it
+    auto ends = [&](int64_t at, int i) { return a.key[min((at + lane + 1) * a.run - 1 + i, a.M - 1)]; };
+    int32_t x = ends(s + 1, 0), y = ends(s + 1, 1);
+    const int32_t k = a.key[end], own = a.key[end - 1], left_of = a.key[max(i0 - 1, (int64_t)0)];
+    if (own != k || k >= a.V || (i0 > 0 && left_of == k)) return;   // (the same for all threads)
+    int64_t last = s + 1;
+    for (;;) {
+        const uint64_t on = __ballot((last + lane + 1) * a.run < a.M && x == k && y == k);
+        const int n = __ffsll((long long)~on);   // (0: all 64)
+        last += n ? n - 1 : 64;
+        if (n) break;
+        x = ends(last, 0), y = ends(last, 1);
+    }
     if (c >= a.D) return;
     const int left = (int)(a.D - c);
-    float sum[4];
+    float sum[4], old[4] = {};
     load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
-    for (int64_t p = s + 1; p <= last; p += 8) {
-        float v[8][4];
+    if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
+    for (int64_t p = s + 1; p <= last; p += 16) {
+        float v[16][4];
 #pragma unroll
-        for (int i = 0; i < 8; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
+        for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
 #pragma unroll
-        for (int i = 0; i < 8; i++)
+        for (int i = 0; i < 16; i++)
 #pragma unroll
             for (int e = 0; e < 4; e++) sum[e] += p + i <= last ? v[i][e] : 0.f;
     }
-    TG* row = (TG*)a.dtable + k * a.ldt + c;
-    float old[4];
-    load_some(row, a.accumulate ? left : 0, old);
-#pragma unroll
-    for (int e = 0; e < 4; e++) old[e] = __builtin_fmaf(a.alpha, sum[e], old[e]);
-    store_some(row, left, old);
+    put_sum<TG>(a, k, c, sum, old);
 }
 
 // ---------------------------------------------------------------- launches
@@ -320,9 +371,12 @@ EmbSpace emb_space(int64_t M, int64_t D) {
     s.order1 = s.key + up256(M * 4);
     s.key1 = s.order1 + (chunks ? up256(M * 4) : 0);
     s.part = s.key1 + (chunks ? up256(M * 4) : 0);
-    s.total = s.part + up256(ceil_div(M, kRun) * 2 * D * 4);
+    s.total = s.part + up256(ceil_div(M, kRunMin) * 2 * D * 4);
     return s;
 }
+
+// Short stretches where long ones leave CUs without work.
+int run_of(int64_t M, int64_t D) { return ceil_div(M, 16) * ceil_div(D, kSumCols) < 1024 ? 8 : 16; }
 
 int sort_passes(int64_t V) {   // bytes of the largest key, V
     int p = 1;
@@ -330,7 +384,7 @@ int sort_passes(int64_t V) {   // bytes of the largest key, V
     return p;
 }
 
-constexpr int kSortLds = kSortMax * 8 + kSortWaves * kBins * 4 + 64;
+constexpr int kSortLds = kSortMax * 8 + kSortWaves * kBins * 2 + 64;
 
 // Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
 template <auto kernel, int LDS>
@@ -352,28 +406,40 @@ hipError_t run_sort(EmbBwdArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     a.sorters = (int32_t)ceil_div(a.M, kSortMax);
     const int64_t n = a.M < kSortMax ? a.M : kSortMax;
-    const unsigned lds = (unsigned)(ceil_div(n, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 4 + 64);
-    const int64_t zeros = a.accumulate ? 0 : (a.V < 512 ? a.V : 512);
+    const unsigned lds = (unsigned)(ceil_div(n, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 2 + 64);
+    // zeros: many workgroups with a store each (262 MB 43 us; by 1024 that go on 52)
+    const int64_t stores = a.ldt == a.D ? ceil_div(a.V * a.D, (int64_t)kSortThreads * CH) : a.V;
+    const int64_t zeros = a.accumulate ? 0 : (stores < (1 << 20) ? stores : 1 << 20);
     hipLaunchKernelGGL((token_sort_kernel<TG>), dim3((unsigned)(a.sorters + zeros)), dim3(kSortThreads), lds, stream, a);
     return hipGetLastError();
 }
 
 template <typename T, typename TG>
 hipError_t run_sums(const EmbBwdArgs& a, hipStream_t stream) {
-    const int64_t runs = ceil_div(a.M, kRun);
+    const int64_t runs = ceil_div(a.M, a.run);
     const int slices = (int)ceil_div(a.D, kSumCols);
-    if (a.D >= CH)
-        hipLaunchKernelGGL((token_sum_kernel<T, TG, 1>), dim3((unsigned)(runs * slices)), dim3(kSumThreads), 0, stream, a, slices);
-    else
-        hipLaunchKernelGGL((token_sum_kernel<T, TG, 0>), dim3((unsigned)(runs * slices)), dim3(kSumThreads), 0, stream, a, slices);
+    const dim3 grid((unsigned)(runs * slices)), block(kSumThreads);
+    auto launch = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        auto by_run = [&](auto run) {
+            constexpr int RUN = decltype(run)::value;
+            if (a.accumulate) hipLaunchKernelGGL((token_sum_kernel<T, TG, KIND, true, RUN>), grid, block, 0, stream, a, slices);
+            else hipLaunchKernelGGL((token_sum_kernel<T, TG, KIND, false, RUN>), grid, block, 0, stream, a, slices);
+        };
+        if (a.run == 8) by_run(std::integral_constant<int, 8>());
+        else by_run(std::integral_constant<int, 16>());
+    };
+    if (a.D % CH == 0) launch(std::integral_constant<int, 2>());
+    else if (a.D > CH) launch(std::integral_constant<int, 1>());
+    else launch(std::integral_constant<int, 0>());
     return hipGetLastError();
 }
 
 template <typename TG>
 hipError_t run_join(const EmbBwdArgs& a, hipStream_t stream) {
-    const int64_t runs = ceil_div(a.M, kRun);
+    const int64_t runs = ceil_div(a.M, a.run);
     if (runs < 2) return hipSuccess;
-    const int slices = (int)ceil_div(a.D, 1024);
+    const int slices = (int)ceil_div(a.D, kJoinCols);
     hipLaunchKernelGGL((token_join_kernel<TG>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices);
     return hipGetLastError();
 }
@@ -437,7 +503,7 @@ niti_status niti_embedding_bwd(const void* dy, int64_t lddy, int type, const int
     char* base = (char*)ws;
     const bool chunks = M > kSortMax;
     hipStream_t s = (hipStream_t)stream;
-    EmbBwdArgs a{dy, tokens, dtable, M > 1 ? lddy : D, V > 1 ? ldt : D, M, V, D, alpha, accumulate != 0, sort_passes(V), 0,
+    EmbBwdArgs a{dy, tokens, dtable, M > 1 ? lddy : D, V > 1 ? ldt : D, M, V, D, alpha, accumulate != 0, sort_passes(V), run_of(M, D), 0,
                  (int32_t*)(base + w.order), (int32_t*)(base + w.key), chunks ? (int32_t*)(base + w.order1) : nullptr,
                  chunks ? (int32_t*)(base + w.key1) : nullptr, (float*)(base + w.part)};
     hipError_t e = by_type(dtable_type, [&](auto g) { return run_sort<decltype(g)>(a, s); });

@@ -445,13 +445,13 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinArgs A, int tiles_n)
             up[e] = (float)sums[r * PITCH + 32 + c + e] * par[32 + c + e] * sa + par[GT + 32 + c + e];
         }
         if (A.z) {
-            store_some((T*)A.z + m * A.ldz + n, left, gate);
-            store_some((T*)A.z + m * A.ldz + A.N + n, left, up);
+            store_first((T*)A.z + m * A.ldz + n, left, gate);
+            store_first((T*)A.z + m * A.ldz + A.N + n, left, up);
         }
         act_values(A.act, gate);
 #pragma unroll
         for (int e = 0; e < 8; e++) gate[e] *= up[e];
-        store_some((T*)A.out + m * A.ldout + n, left, gate);
+        store_first((T*)A.out + m * A.ldout + n, left, gate);
     } else {
         epilogue<T, GT, GT, 2, 2, sizeof(lds)>(A, acc, lds[0], par, m0, n0);
     }

@@ -148,16 +148,9 @@ template <typename T, bool TINY>
 __device__ __forceinline__ void store_logits(T* row, int c, int V, const float (&v)[CH], bool stream) {
     const Place<TINY> at(c, V);
     if (at.whole() && stream) {
-        typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
-        T t[CH];
-        any4 w[sizeof(t) / 16];
-#pragma unroll
-        for (int e = 0; e < CH; e++) t[e] = from_f<T>(v[e]);
-        __builtin_memcpy(w, t, sizeof(t));
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(t) / 16); i++) __builtin_nontemporal_store(w[i], (any4*)(row + c) + i);
+        store_whole<true>(row + c, v);
     } else if (at.whole()) {
-        store_n(row + c, v);
+        store_whole(row + c, v);
     } else {
 #pragma unroll
         for (int e = 0; e < CH; e++)

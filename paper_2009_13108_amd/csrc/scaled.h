@@ -74,6 +74,42 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&v)[N]) {
         if (i < n) p[i] = from_f<T>(v[i]);
 }
 
+// The same, the whole ones as vectors of 32-bit words: beside a branch for some of them the compiler takes an array's store apart
+// (two bytes, two bytes and twelve for eight 16-bit elements).  STREAM: past the caches.
+typedef uint32_t any_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+template <bool STREAM = false, typename T, int N>
+__device__ __forceinline__ void store_whole(T* p, const float (&v)[N]) {
+    static_assert(N * sizeof(T) % 16 == 0 || N * sizeof(T) == 8, "whole vectors");
+    T t[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) t[i] = from_f<T>(v[i]);
+    if constexpr (N * sizeof(T) == 8) {
+        any_u32x2 w;
+        __builtin_memcpy(&w, t, sizeof(w));
+        if (STREAM) __builtin_nontemporal_store(w, (any_u32x2*)p);
+        else *(any_u32x2*)p = w;
+    } else {
+        any_u32x4 w[N * sizeof(T) / 16];
+        __builtin_memcpy(w, t, sizeof(w));
+#pragma unroll
+        for (int i = 0; i < (int)(N * sizeof(T) / 16); i++) {
+            if (STREAM) __builtin_nontemporal_store(w[i], (any_u32x4*)p + i);
+            else *((any_u32x4*)p + i) = w[i];
+        }
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_first(T* p, int n, const float (&v)[N]) {
+    if (n >= N) {
+        store_whole(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        if (i < n) p[i] = from_f<T>(v[i]);
+}
+
 // Eight elements as they are loaded.  A load inside a branch is waited for where the
 // branch ends, so a kernel that is to have many in flight has none of them in a
 // branch: a piece past the row's end is loaded from inside it and set to zeros,
