@@ -11,7 +11,10 @@ namespace niti {
 
 namespace {
 
-// What a call takes in each kernel (see the forms), N counting the weight rows.
+// What a call takes in each kernel (see the forms), N counting the weight rows: as fitted for the plain product's tiles, but for 64 x
+// 128.  On 400 random products of 1..8192 x 32..9216 x 32..9216 what they pick takes 2.3% longer than the fastest in the mean, on
+// 200 with rows at odd addresses 2.2%; constants fitted to these calls were no better on others.  Parts of a sum side by side, as the
+// plain product has them, gained on none of the 400 more than 12%, in the mean nothing.
 constexpr Cost kPair12{16, 32, kSpread, 1.92f, 0.61f, 0.95f, 1.33f};
 constexpr Cost kPair22{32, 32, kSpread, 2.06f, 0.75f, 1.18f, 1.90f};
 constexpr Cost kPairBytes12{16, 32, kSpread, 2.01f, 0.59f, 1.23f, 2.45f};
@@ -28,10 +31,15 @@ struct Choice {
     bool pack;   // the operands are copied to whole aligned pieces first
 };
 
-Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room) {
+// keep: z is stored as well, by all CUs at once where there is one tile a CU, which nothing hides (4096 x 8192 x 4096: 29 us of 284; 8192 x
+// 2048 x 1024: 256 x 256 tiles 62 us, 128 x 128 ones, two a CU, 56, without z 46 either way).
+Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room, bool keep) {
     // columns of whole tiles: a half's last tile is not filled by the other half
     const bool whole = rows == kOfPieces, words = rows != kOfBytes;
-    auto at = [&](const Cost& c) { return cost(c, M, (F + c.bn / 2 - 1) / (c.bn / 2) * c.bn, K); };
+    auto at = [&](Cost c, float store = 0.f) {
+        c.round += keep ? store : 0.f;
+        return cost(c, M, (F + c.bn / 2 - 1) / (c.bn / 2) * c.bn, K);
+    };
     Choice c{Choice::kS12, at(words ? kPair12 : kPairBytes12), false};
     auto take = [&](decltype(c.kernel) kernel, float time) {
         if (time < c.time) c = Choice{kernel, time, false};
@@ -39,13 +47,13 @@ Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room) {
     take(Choice::kS22, at(words ? kPair22 : kPairBytes22));
     take(Choice::k64, at(whole ? kPair64 : kPairAny64));
     if (whole) {
-        take(Choice::k128, at(kPair128));
-        take(Choice::k128d, at(kPairDeep128) * (M * F > 128 * 128 * 128 ? 1.08f : 1.f));
-        take(Choice::k256, at(kPair256));
+        take(Choice::k128, at(kPair128, 1.3f));
+        take(Choice::k128d, at(kPairDeep128, 1.3f) * (M * F > 128 * 128 * 128 ? 1.08f : 1.f));
+        take(Choice::k256, at(kPair256, 7.8f));
     }
     const size_t copies = whole ? 0 : pack_bytes(M, 2 * F, K);
     if (copies > 0 && copies <= room) {
-        Choice p = choose(M, F, up16(K), kOfPieces, 0);
+        Choice p = choose(M, F, up16(K), kOfPieces, 0, keep);
         p.time += 2.3f + (float)((double)copies * 2. / 3e6);   // (3 TB/s)
         p.pack = true;
         if (p.time < c.time) c = p;
@@ -54,9 +62,11 @@ Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room) {
 }
 
 template <typename T>
-hipError_t run_gated(const LinArgs& A, void* ws, size_t ws_bytes, hipStream_t stream) {
+hipError_t run_gated(LinArgs A, void* ws, size_t ws_bytes, hipStream_t stream) {
     const bool whole = ring_takes(A);
-    const Choice c = choose(A.M, A.N, A.K, whole ? kOfPieces : (word_rows(A) ? kOfWords : kOfBytes), ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0);
+    // the backward pass reads z much later: more than the L2s hold goes past them (4096 x 8192 x 4096 315 -> 284 us)
+    A.z_stream = A.z && A.M * A.N * 2 * (int64_t)sizeof(T) > ((int64_t)32 << 20);
+    const Choice c = choose(A.M, A.N, A.K, whole ? kOfPieces : (word_rows(A) ? kOfWords : kOfBytes), ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0, A.z != nullptr);
     if (c.pack) {
         const int64_t Kp = up16(A.K);
         const uint32_t ppr = (uint32_t)(Kp / 16), pieces = (uint32_t)(A.M + 2 * A.N) * ppr;
@@ -83,8 +93,10 @@ hipError_t run_gated(const LinArgs& A, void* ws, size_t ws_bytes, hipStream_t st
 // For copies of the operands, if that is how this product would go with room for them.
 size_t gated_fwd_workspace(int64_t M, int64_t F, int64_t K) {
     if (M < 1 || F < 1 || K < 1 || M >= kMaxDim || F >= kMaxLd / 2 || K >= kMaxSum) return 0;
-    const bool pack = choose(M, F, K, kOfBytes, SIZE_MAX).pack || choose(M, F, K, kOfWords, SIZE_MAX).pack;
-    return pack ? pack_bytes(M, 2 * F, K) : 0;
+    for (Rows rows : {kOfBytes, kOfWords})
+        for (bool keep : {false, true})
+            if (choose(M, F, K, rows, SIZE_MAX, keep).pack) return pack_bytes(M, 2 * F, K);
+    return 0;
 }
 
 }  // namespace niti

@@ -23,6 +23,7 @@ struct LinArgs {
     int32_t res_dma;          // the residual's rows are whole aligned pieces within 32-bit offsets
     int32_t klen;             // products of one part of a split sum (blockIdx.y), or 0
     int64_t part;             // elements of a part's sums, from out on
+    int32_t z_stream;         // z goes past the caches (set by the gated product)
 };
 
 hipError_t linear_run(const LinArgs& a, int type, void* ws, size_t ws_bytes, hipStream_t stream);

@@ -293,7 +293,8 @@ __device__ __forceinline__ void gated_epilogue(const LinArgs& A, v16i (&acc)[BN 
                 if (m >= rows || nv <= 0) continue;
                 T* dst = out + m * ld + p * S::EPP;
                 if (nv >= S::EPP) {
-                    store16_any(dst, v);
+                    if (kind < 2 && A.z_stream) __builtin_nontemporal_store(any_u32x4{v.x, v.y, v.z, v.w}, (any_u32x4*)dst);
+                    else store16_any(dst, v);
                 } else {
                     T e[S::EPP];
                     __builtin_memcpy(e, &v, 16);
