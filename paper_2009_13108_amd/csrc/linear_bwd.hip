@@ -81,30 +81,42 @@ struct DzRows {
             }
         }
     }
+    // What was formed of the loads is formed anew from here on, in place of being kept.
+    __device__ __forceinline__ void forget_values() {
+        if constexpr (KIND > 0) {
+#pragma unroll
+            for (int i = 0; i < ROWS; i++)
+#pragma unroll
+                for (int w = 0; w < (int)(sizeof(y[i].w) / 4); w++) asm volatile("" : "+v"(y[i].w[w]), "+v"(z[i].w[w]));
+        }
+    }
+    // half HALF's values, the only one's or (-1) both
+    template <int HALF>
     __device__ __forceinline__ void get(const DzArgs& a, int i, int64_t m, int c, float (&d)[H][CH]) {
         const int W = (int)a.W;
         float s[CH], v[CH];
         if constexpr (KIND > 0) {
             piece_values<T, KIND == 2>(y[i], c, W, d[0]);
             piece_values<T, KIND == 2>(z[i], c, W, s);
-            if constexpr (G) piece_values<T, KIND == 2>(u[i], c, W, v);
+            if constexpr (G && HALF != 1) piece_values<T, KIND == 2>(u[i], c, W, v);
         } else {
             const int64_t r = min(m, a.M - 1);
             load_some((const T*)a.dy + r * a.lddy + c, W - c, d[0]);
             if (G || a.act != NITI_ACT_NONE) load_some((const T*)a.z + r * a.ldz + c, W - c, s);
-            if constexpr (G) load_some((const T*)a.z + r * a.ldz + a.W + c, W - c, v);
+            if constexpr (G && HALF != 1) load_some((const T*)a.z + r * a.ldz + a.W + c, W - c, v);
         }
-        if constexpr (G) {
+        if constexpr (G && HALF != 0) {
 #pragma unroll
             for (int e = 0; e < CH; e++) d[1][e] = s[e];
             act_values(a.act, d[1]);
 #pragma unroll
-            for (int e = 0; e < CH; e++) {
-                d[1][e] *= d[0][e];
-                d[0][e] *= v[e];
-            }
+            for (int e = 0; e < CH; e++) d[1][e] *= d[0][e];
         }
-        if (a.act != NITI_ACT_NONE) {
+        if constexpr (G && HALF != 1) {
+#pragma unroll
+            for (int e = 0; e < CH; e++) d[0][e] *= v[e];
+        }
+        if (HALF != 1 && a.act != NITI_ACT_NONE) {
             act_slopes(a.act, s);
 #pragma unroll
             for (int e = 0; e < CH; e++) d[0][e] *= s[e];
@@ -155,7 +167,7 @@ __global__ __launch_bounds__(256) void dz_stats_kernel(DzArgs a) {
     for (int i = 0; i < SR / 8; i++) {
         const int64_t m = tm * SR + i * 8 + grp;
         float d[H][CH];
-        rows.get(a, i, m, c, d);
+        rows.template get<G ? -1 : 0>(a, i, m, c, d);
         uint32_t top = 0;
 #pragma unroll
         for (int h = 0; h < H; h++)
@@ -315,10 +327,10 @@ __device__ __forceinline__ void turn_tile(const Turn& a, int block, int8_t (*til
 
 // Step 3: a CT x CT tile of codes, or one of a's or b's transposed copies.
 template <typename T, int KIND, bool G>
-__global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int codes, int tiles_c) {
+__global__ __launch_bounds__(CTH, G ? 4 : 1) void dz_codes_kernel(DzArgs a, Turn ta, Turn tb, int codes, int tiles_c) {
     constexpr int H = G ? 2 : 1;
     __shared__ __attribute__((aligned(16))) int8_t tile[H][CT][CP];
-    __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[H * CT];
+    __shared__ __attribute__((aligned(16))) float rinv[CT], cinv[H * CT], scale[H * CT];
     int block = blockIdx.x;
     if (block >= codes) {   // the codes' tiles, which take longest, are first
         block -= codes;
@@ -329,13 +341,11 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
     const int64_t m0 = (int64_t)((uint32_t)block / (uint32_t)tiles_c) * CT, n0 = (int64_t)((uint32_t)block % (uint32_t)tiles_c) * CT;
     const int col = (threadIdx.x & 15) * CH, row0 = (threadIdx.x >> 4) * 4;   // 8 columns of 4 rows a thread
     const int c = (int)(n0 + col);
-    float sb[H][CH], ci[H][CH], sa[4];
+    float sa[4];
     DzRows<T, KIND, 4, G> rows;
     rows.load(a, m0 + row0, 1, c);
 #pragma unroll
     for (int i = 0; i < 4; i++) sa[i] = a.s_a[a.a_step ? min(m0 + row0 + i, a.M - 1) : 0];
-#pragma unroll
-    for (int h = 0; h < H; h++) load_cols<KIND>(a.s_b + (a.b_step ? h * a.W : 0), a.b_step, c, (int)a.W, sb[h]);
     {   // the tile's factors: 128 threads a row each, 128 a column (of each half)
         const int i = threadIdx.x & (CT - 1), half = G ? (int)threadIdx.x / CT - 1 : 0;
         const int64_t m = min(m0 + i, a.M - 1), n = half * a.W + min(n0 + i, a.W - 1);
@@ -373,41 +383,42 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
                 inv = a.c[a.N + n];
             }
             cinv[half * CT + i] = n0 + i < a.W ? inv : 0.f;
+            scale[half * CT + i] = a.s_b[a.b_step ? n : 0];
         }
     }
     __syncthreads();
-    uint32_t cmask[H][2] = {};
-#pragma unroll
-    for (int h = 0; h < H; h++)
+    // (a gated product's halves one after the other: both at once take more registers than two workgroups a CU leave)
+    auto half_codes = [&](auto half) {
+        constexpr int h = decltype(half)::value;
+        float sb[CH], ci[CH];
+        uint32_t cmask[2] = {0, 0}, qc[4][2];   // codes of the columns: four rows of eight bytes
 #pragma unroll
         for (int e = 0; e < CH; e++) {
-            ci[h][e] = cinv[h * CT + col + e];
-            cmask[h][e >> 2] |= (code_mask(ci[h][e]) & 0xFFu) << (8 * (e & 3));
+            sb[e] = scale[h * CT + col + e];
+            ci[e] = cinv[h * CT + col + e];
+            cmask[e >> 2] |= (code_mask(ci[e]) & 0xFFu) << (8 * (e & 3));
         }
-    uint32_t qc[H][4][2];   // codes of the columns: four rows of eight bytes
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int64_t m = m0 + row0 + i;
-        const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
-        float d[H][CH];
-        rows.get(a, i, m, c, d);
-        const float ri = rinv[row0 + i];
-#pragma unroll
-        for (int h = 0; h < H; h++) {
-            float pc[CH], cc[CH];
+        for (int i = 0; i < 4; i++) {
+            const int64_t m = m0 + row0 + i;
+            const bool in = m < a.M;   // rows past M are zeros, which pad the sums over m
+            float both[H][CH], pc[CH], cc[CH];
+            rows.template get<h>(a, i, m, c, both);
+            const float(&d)[CH] = both[h];
+            const float ri = rinv[row0 + i];
             if (a.sr) {
                 DrawStream r(a.seed, a.call, (uint64_t)(m * a.N + h * a.W + c));
 #pragma unroll
                 for (int e = 0; e < CH; e++) {
                     const uint64_t u = r.next();
-                    pc[e] = code_sr(d[h][e] * sb[h][e], ri, draw_hi(u));
-                    cc[e] = code_sr(d[h][e] * sa[i], ci[h][e], draw_lo(u));
+                    pc[e] = code_sr(d[e] * sb[e], ri, draw_hi(u));
+                    cc[e] = code_sr(d[e] * sa[i], ci[e], draw_lo(u));
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < CH; e++) {
-                    pc[e] = code_rtn(d[h][e] * sb[h][e], ri);
-                    cc[e] = code_rtn(d[h][e] * sa[i], ci[h][e]);
+                    pc[e] = code_rtn(d[e] * sb[e], ri);
+                    cc[e] = code_rtn(d[e] * sa[i], ci[e]);
                 }
             }
             // (past the edges dz is 0, and so are the codes: a draw is below 1)
@@ -425,19 +436,22 @@ __global__ __launch_bounds__(CTH) void dz_codes_kernel(DzArgs a, Turn ta, Turn t
                         if (c + e < end) dst[e] = (int8_t)(w[e >> 2] >> (8 * (e & 3)));
                 }
             }
-            qc[h][i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[h][0];
-            qc[h][i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[h][1];
+            qc[i][0] = pack4(cc[0], cc[1], cc[2], cc[3]) & cmask[0];
+            qc[i][1] = pack4(cc[4], cc[5], cc[6], cc[7]) & cmask[1];
         }
-    }
-#pragma unroll
-    for (int h = 0; h < H; h++)
 #pragma unroll
         for (int g = 0; g < 2; g++) {
-            uint32_t w[4] = {qc[h][0][g], qc[h][1][g], qc[h][2][g], qc[h][3][g]};
+            uint32_t w[4] = {qc[0][g], qc[1][g], qc[2][g], qc[3][g]};
             turn4(w);
 #pragma unroll
             for (int i = 0; i < 4; i++) *(uint32_t*)&tile[h][col + 4 * g + i][row0] = w[i];
         }
+    };
+    half_codes(std::integral_constant<int, 0>());
+    if constexpr (G) {
+        rows.forget_values();
+        half_codes(std::integral_constant<int, 1>());
+    }
     if (!a.q) return;
     __syncthreads();
 #pragma unroll
@@ -474,7 +488,7 @@ struct BwdSpace {
     int64_t p, q, at, bt, r, c, rmax, cmax, csum, sums, sums_bytes, total;
 };
 
-// W: columns of dy.
+// W: columns of dy, N or half of that.
 BwdSpace space(int64_t M, int64_t N, int64_t W, int64_t K) {
     BwdSpace s;
     s.Mp = up(M, kPad);
