@@ -4,9 +4,9 @@
 // Gradient:  dtable[v] = alpha sum over the m with token v of dy[m]  (+ dtable[v]).
 //
 // The gradient goes by sorted tokens, so that every sum has a fixed order and no
-// atomics.  (1) A workgroup sorts up to 16384 tokens in its LDS (radix sort, stable; longer
-// batches are sorted in such chunks and placed by binary searches in the other chunks); meanwhile the other
-// workgroups of the launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
+// atomics.  (1) Workgroups sort 2048 tokens each in their LDS (radix sort, stable; 16384 in batches of more than 32768), and
+// a second launch places a chunk's tokens by binary searches in the other chunks; meanwhile the other
+// workgroups of the first launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
 // read and added up: a token whose rows lie inside such a stretch gets its row
 // at once, one that crosses its ends leaves partial sums in the workspace, and (3) those are joined
 // in order.  However often a token occurs, the work is split evenly.
@@ -19,7 +19,9 @@ namespace niti {
 
 namespace {
 
-constexpr int kSortMax = 16384;   // tokens that one workgroup sorts
+constexpr int kSortMax = 16384;   // tokens that one workgroup sorts at most
+constexpr int kSortFew = 2048;    // and where the whole batch is no more than
+constexpr int kMergeMax = 32768;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kRounds = kSortMax / kSortThreads;
 constexpr int kBins = 256;
 constexpr int kRunMin = 8;        // sorted rows of a stretch: 8 or 16
@@ -88,6 +90,7 @@ struct EmbBwdArgs {
     int32_t sorters;              // workgroups that sort, ahead of those that write zeros
     int32_t *order, *key;         // [M]: rows by token, and their tokens (V for those outside the table)
     int32_t *order1, *key1;       // the same of each chunk, where there are several
+    int32_t chunk;                // tokens of one
     float* part;                  // [stretches][2][D]
 };
 
@@ -114,8 +117,8 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
         }
         return;
     }
-    const int64_t base = (int64_t)blockIdx.x * kSortMax;
-    const int n = (int)min((int64_t)kSortMax, a.M - base);
+    const int64_t base = (int64_t)blockIdx.x * a.chunk;
+    const int n = (int)min((int64_t)a.chunk, a.M - base);
     const int rounds = (n + kSortThreads - 1) / kSortThreads, room = rounds * kSortThreads;
     uint32_t* key = (uint32_t*)lds;
     uint16_t* src = (uint16_t*)(key + room);
@@ -235,6 +238,39 @@ __global__ __launch_bounds__(256) void token_merge_kernel(EmbBwdArgs a) {
     for (int64_t c = 0; c * kSortMax < a.M; c++)
         if (c != mine) at += count_below(a.key1 + c * kSortMax, min((int64_t)kSortMax, a.M - c * kSortMax), k, c < mine);
     a.order[at] = a.order1[i];
+    a.key[at] = k;
+}
+
+// The same for chunks of 2048 that all fit in LDS: four searches of twelve steps at a time.
+__global__ __launch_bounds__(1024) void token_merge_few_kernel(EmbBwdArgs a) {
+    extern __shared__ __attribute__((aligned(16))) int32_t keys[];
+    const int M = (int)a.M, chunks = (M + kSortFew - 1) / kSortFew;
+    const int i = (int)blockIdx.x * 1024 + (int)threadIdx.x, mine = (int)blockIdx.x * 1024 / kSortFew;
+    const int32_t place = a.order1[min(i, M - 1)];
+#pragma unroll 4
+    for (int j = (int)threadIdx.x * 4; j < M; j += 4096) {   // (whole fours: the workspace holds more than the last)
+        const v4i x = *(const v4i*)(a.key1 + j);
+        *(v4i*)(keys + j) = x;
+    }
+    __syncthreads();
+    if (i >= M) return;
+    const int32_t k = keys[i];
+    int at = i - mine * kSortFew;
+    for (int c0 = 0; c0 < chunks; c0 += 4) {
+        int pos[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int step = kSortFew; step >= 1; step /= 2)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int c = c0 + j, n = min(kSortFew, M - c * kSortFew);   // (of a chunk past the last: none)
+                const int32_t v = keys[min(c * kSortFew + pos[j] + step, M) - 1];
+                const bool before = v < k || (v == k && c < mine);
+                pos[j] += pos[j] + step <= n && before ? step : 0;
+            }
+#pragma unroll
+        for (int j = 0; j < 4; j++) at += c0 + j == mine ? 0 : pos[j];
+    }
+    a.order[at] = place;
     a.key[at] = k;
 }
 
@@ -365,7 +401,7 @@ struct EmbSpace {
 };
 EmbSpace emb_space(int64_t M, int64_t D) {
     EmbSpace s{};
-    const bool chunks = M > kSortMax;
+    const bool chunks = M > kSortFew;
     s.order = 0;
     s.key = s.order + up256(M * 4);
     s.order1 = s.key + up256(M * 4);
@@ -404,13 +440,24 @@ template <typename TG>
 hipError_t run_sort(EmbBwdArgs& a, hipStream_t stream) {
     const hipError_t e = allow_lds<token_sort_kernel<TG>, kSortLds>();
     if (e != hipSuccess) return e;
-    a.sorters = (int32_t)ceil_div(a.M, kSortMax);
-    const int64_t n = a.M < kSortMax ? a.M : kSortMax;
+    a.sorters = (int32_t)ceil_div(a.M, a.chunk);
+    const int64_t n = a.M < a.chunk ? a.M : a.chunk;
     const unsigned lds = (unsigned)(ceil_div(n, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 2 + 64);
     // zeros: many workgroups with a store each (262 MB 43 us; by 1024 that go on 52)
     const int64_t stores = a.ldt == a.D ? ceil_div(a.V * a.D, (int64_t)kSortThreads * CH) : a.V;
     const int64_t zeros = a.accumulate ? 0 : (stores < (1 << 20) ? stores : 1 << 20);
     hipLaunchKernelGGL((token_sort_kernel<TG>), dim3((unsigned)(a.sorters + zeros)), dim3(kSortThreads), lds, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t run_merge(const EmbBwdArgs& a, hipStream_t stream) {
+    if (a.M <= kMergeMax) {
+        const hipError_t e = allow_lds<token_merge_few_kernel, kMergeMax * 4>();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(token_merge_few_kernel, dim3((unsigned)ceil_div(a.M, 1024)), dim3(1024), (unsigned)(ceil_div(a.M, 4) * 16), stream, a);
+    } else {
+        hipLaunchKernelGGL(token_merge_kernel, dim3((unsigned)ceil_div(a.M, 256)), dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 
@@ -501,15 +548,14 @@ niti_status niti_embedding_bwd(const void* dy, int64_t lddy, int type, const int
     if (M > 0 && (!ws || ws_bytes < (size_t)w.total)) return NITI_ERR_WORKSPACE;
     if (M > 0 && ((uintptr_t)ws & 15)) return NITI_ERR_ARG;
     char* base = (char*)ws;
-    const bool chunks = M > kSortMax;
+    const bool chunks = M > kSortFew;
     hipStream_t s = (hipStream_t)stream;
     EmbBwdArgs a{dy, tokens, dtable, M > 1 ? lddy : D, V > 1 ? ldt : D, M, V, D, alpha, accumulate != 0, sort_passes(V), run_of(M, D), 0,
                  (int32_t*)(base + w.order), (int32_t*)(base + w.key), chunks ? (int32_t*)(base + w.order1) : nullptr,
-                 chunks ? (int32_t*)(base + w.key1) : nullptr, (float*)(base + w.part)};
+                 chunks ? (int32_t*)(base + w.key1) : nullptr, M <= kMergeMax ? kSortFew : kSortMax, (float*)(base + w.part)};
     hipError_t e = by_type(dtable_type, [&](auto g) { return run_sort<decltype(g)>(a, s); });
     if (e == hipSuccess && chunks) {
-        hipLaunchKernelGGL(token_merge_kernel, dim3((unsigned)ceil_div(M, 256)), dim3(256), 0, s, a);
-        e = hipGetLastError();
+        e = run_merge(a, s);
     }
     if (e == hipSuccess && M > 0)
         e = by_type(dtable_type, [&](auto g) {
