@@ -4,9 +4,9 @@
 // Gradient:  dtable[v] = alpha sum over the m with token v of dy[m]  (+ dtable[v]).
 //
 // The gradient goes by sorted tokens, so that every sum has a fixed order and no
-// atomics.  (1) Workgroups sort 2048 tokens each in their LDS (radix sort, stable; 16384 in batches of more than 32768), and
-// a second launch places a chunk's tokens by binary searches in the other chunks; meanwhile the other
-// workgroups of the first launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
+// atomics.  (1) Up to 8192 tokens are placed by comparing all with all; of more, workgroups sort 2048 each in their LDS (radix sort,
+// stable; 16384 in batches of more than 32768), and a second launch places a chunk's tokens by binary searches in the other
+// chunks; meanwhile the other workgroups of the first launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
 // read and added up: a token whose rows lie inside such a stretch gets its row
 // at once, one that crosses its ends leaves partial sums in the workspace, and (3) those are joined
 // in order.  However often a token occurs, the work is split evenly.
@@ -22,6 +22,7 @@ namespace {
 constexpr int kSortMax = 16384;   // tokens that one workgroup sorts at most
 constexpr int kSortFew = 2048;    // and where the whole batch is no more than
 constexpr int kMergeMax = 32768;
+constexpr int kRankMax = 8192;    // tokens that are compared all with all
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kRounds = kSortMax / kSortThreads;
 constexpr int kBins = 256;
 constexpr int kRunMin = 8;        // sorted rows of a stretch: 8 or 16
@@ -94,27 +95,79 @@ struct EmbBwdArgs {
     float* part;                  // [stretches][2][D]
 };
 
-// (1) LDS: the chunk's tokens, two lists of places, a counter for each digit and wave.
+// A token's place in the order: tokens outside the table after all others.
+__device__ __forceinline__ int32_t sort_key(const EmbBwdArgs& a, int64_t i) {
+    const int tok = a.tokens[i];
+    return (uint32_t)tok < (uint64_t)a.V ? tok : (int32_t)a.V;
+}
+
+// The workgroups past those that sort write the zeros: of a whole table in one go, of spaced rows row by row.
+template <typename TG>
+__device__ __forceinline__ void write_zeros(const EmbBwdArgs& a) {
+    const int t = threadIdx.x;
+    const int64_t first = (int64_t)blockIdx.x - a.sorters, step = (int64_t)gridDim.x - a.sorters;
+    const float zero[CH] = {};
+    if (a.ldt == a.D) {
+        constexpr int64_t BLOCK = (int64_t)kSortThreads * CH;
+        const int64_t n = a.V * a.D;
+        for (int64_t i = first * BLOCK + t * CH; i < n; i += step * BLOCK) {
+            if (i + CH <= n) store_whole<true>((TG*)a.dtable + i, zero);
+            else store_first((TG*)a.dtable + i, (int)(n - i), zero);
+        }
+    } else {
+        for (int64_t r = first; r < a.V; r += step) {
+            TG* row = (TG*)a.dtable + r * a.ldt;
+            for (int c = t * CH; c < a.D; c += kSortThreads * CH) store_first(row + c, (int)(a.D - c), zero);
+        }
+    }
+}
+
+// (1) Few tokens: a token's place is the number of those before it, smaller ones and equal ones with a smaller index, counted by
+// comparing all with all (two instructions a pair, on all CUs; 4096 tokens in 7 us where sorting and placing took 16).  A workgroup
+// places 64, its sixteen waves count in a sixteenth of the batch each.
+template <typename TG>
+__global__ __launch_bounds__(kSortThreads) void token_rank_kernel(EmbBwdArgs a) {
+    extern __shared__ __attribute__((aligned(16))) int32_t keys[];   // [M to a multiple of 64], and [16][64] counts
+    if ((int)blockIdx.x >= a.sorters) {
+        write_zeros<TG>(a);
+        return;
+    }
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int M = (int)a.M, room = (M + 63) / 64 * 64, i0 = (int)blockIdx.x * 64, i = i0 + lane;
+    for (int j = t; j < room; j += kSortThreads) keys[j] = j < M ? sort_key(a, j) : 0x7FFFFFFF;   // (before none)
+    __syncthreads();
+    const int32_t k = keys[i];
+    const int per = room / 64 * 4, from = wave * per, to = from + per;   // (multiples of 4, as i0 is)
+    int n = 0;
+    auto count = [&](int lo, int hi, auto before) {
+#pragma unroll 4
+        for (int j = max(from, lo); j < min(to, hi); j += 4) {
+            const v4i x = *(const v4i*)(keys + j);
+#pragma unroll
+            for (int e = 0; e < 4; e++) n += before(x[e], j + e) ? 1 : 0;
+        }
+    };
+    count(0, i0, [&](int32_t x, int) { return x <= k; });
+    count(i0, i0 + 64, [&](int32_t x, int j) { return x < k || (x == k && j < i); });
+    count(i0 + 64, room, [&](int32_t x, int) { return x < k; });
+    int* counts = keys + room;
+    counts[wave * 64 + lane] = n;
+    __syncthreads();
+    if (wave != 0 || i >= M) return;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; w++) n += counts[w * 64 + lane];
+    a.order[n] = i;
+    a.key[n] = k;
+}
+
+// LDS: the chunk's tokens, two lists of places, a counter for each digit and wave.
 template <typename TG>
 __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int t = threadIdx.x;
-    if ((int)blockIdx.x >= a.sorters) {   // zeros: of a whole table in one go, of spaced rows row by row
-        const int64_t first = (int64_t)blockIdx.x - a.sorters, step = (int64_t)gridDim.x - a.sorters;
-        const float zero[CH] = {};
-        if (a.ldt == a.D) {
-            constexpr int64_t BLOCK = (int64_t)kSortThreads * CH;
-            const int64_t n = a.V * a.D;
-            for (int64_t i = first * BLOCK + t * CH; i < n; i += step * BLOCK) {
-                if (i + CH <= n) store_whole<true>((TG*)a.dtable + i, zero);
-                else store_first((TG*)a.dtable + i, (int)(n - i), zero);
-            }
-        } else {
-            for (int64_t r = first; r < a.V; r += step) {
-                TG* row = (TG*)a.dtable + r * a.ldt;
-                for (int c = t * CH; c < a.D; c += kSortThreads * CH) store_first(row + c, (int)(a.D - c), zero);
-            }
-        }
+    if ((int)blockIdx.x >= a.sorters) {
+        write_zeros<TG>(a);
         return;
     }
     const int64_t base = (int64_t)blockIdx.x * a.chunk;
@@ -126,8 +179,7 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
     uint16_t* bins = dst + room;                                  // [digit][wave]
     uint32_t* totals = (uint32_t*)(bins + kSortWaves * kBins);    // of the four waves that scan
     for (int i = t; i < n; i += kSortThreads) {
-        const int tok = a.tokens[base + i];
-        key[i] = (uint32_t)tok < (uint64_t)a.V ? (uint32_t)tok : (uint32_t)a.V;
+        key[i] = (uint32_t)sort_key(a, base + i);
         src[i] = (uint16_t)i;
     }
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
@@ -353,12 +405,16 @@ __global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, in
     }
 }
 
-// (3) The token that crosses the end of a stretch that it begins in: its partial sums in order.
+// (3) The token that crosses the end of a stretch that it begins in: its partial sums in order.  Threads that rows of fewer than 1024
+// columns leave over take every `groups`-th partial sum, and the groups' sums are added in order.
 constexpr int kJoinCols = 1024;
-template <typename TG>
-__global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slices) {
+template <typename TG, bool GROUPS>
+__global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slices, int of_groups) {
+    __shared__ float sums[GROUPS ? 256 : 1][4];
+    const int groups = GROUPS ? of_groups : 1;
     const int64_t s = blockIdx.x / (uint32_t)slices;
-    const int c = (int)(blockIdx.x % (uint32_t)slices) * kJoinCols + (int)threadIdx.x * 4;
+    const int per = 256 / groups, group = GROUPS ? (int)threadIdx.x / per : 0;
+    const int c = (int)(blockIdx.x % (uint32_t)slices) * kJoinCols + (int)threadIdx.x % per * 4;
     const int64_t i0 = s * a.run, end = i0 + a.run;   // (the last stretch crosses nothing)
     if (end >= a.M) return;
     const int lane = threadIdx.x & 63;
@@ -375,21 +431,50 @@ __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slice
         if (n) break;
         x = ends(last, 0), y = ends(last, 1);
     }
-    if (c >= a.D) return;
-    const int left = (int)(a.D - c);
-    float sum[4], old[4] = {};
-    load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
-    if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
-    for (int64_t p = s + 1; p <= last; p += 16) {
-        float v[16][4];
+    if constexpr (!GROUPS) {
+        if (c >= a.D) return;
+        const int left = (int)(a.D - c);
+        float sum[4], old[4] = {};
+        load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
+        if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
+        for (int64_t p = s + 1; p <= last; p += 16) {
+            float v[16][4];
 #pragma unroll
-        for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
+            for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
 #pragma unroll
-        for (int i = 0; i < 16; i++)
+            for (int i = 0; i < 16; i++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) sum[e] += p + i <= last ? v[i][e] : 0.f;
+                for (int e = 0; e < 4; e++) sum[e] += p + i <= last ? v[i][e] : 0.f;
+        }
+        put_sum<TG>(a, k, c, sum, old);
+        return;
     }
-    put_sum<TG>(a, k, c, sum, old);
+    const int left = (int)(a.D - c);
+    float sum[4] = {}, old[4] = {};
+    if (left > 0) {
+        if (group == 0) {
+            load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
+            if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
+        }
+        for (int64_t p = s + 1 + group; p <= last; p += 16 * groups) {
+            float v[16][4];
+#pragma unroll
+            for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i * groups, last) * a.D + c, left, v[i]);
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) sum[e] += p + i * groups <= last ? v[i][e] : 0.f;
+        }
+    }
+    if constexpr (GROUPS) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) sums[threadIdx.x][e] = sum[e];
+        __syncthreads();
+        for (int g = 1; g < groups && group == 0; g++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) sum[e] += sums[g * per + threadIdx.x][e];
+    }
+    if (left > 0 && group == 0) put_sum<TG>(a, k, c, sum, old);
 }
 
 // ---------------------------------------------------------------- launches
@@ -401,7 +486,7 @@ struct EmbSpace {
 };
 EmbSpace emb_space(int64_t M, int64_t D) {
     EmbSpace s{};
-    const bool chunks = M > kSortFew;
+    const bool chunks = M > kRankMax;
     s.order = 0;
     s.key = s.order + up256(M * 4);
     s.order1 = s.key + up256(M * 4);
@@ -438,14 +523,20 @@ hipError_t allow_lds() {
 
 template <typename TG>
 hipError_t run_sort(EmbBwdArgs& a, hipStream_t stream) {
-    const hipError_t e = allow_lds<token_sort_kernel<TG>, kSortLds>();
-    if (e != hipSuccess) return e;
-    a.sorters = (int32_t)ceil_div(a.M, a.chunk);
-    const int64_t n = a.M < a.chunk ? a.M : a.chunk;
-    const unsigned lds = (unsigned)(ceil_div(n, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 2 + 64);
     // zeros: many workgroups with a store each (262 MB 43 us; by 1024 that go on 52)
     const int64_t stores = a.ldt == a.D ? ceil_div(a.V * a.D, (int64_t)kSortThreads * CH) : a.V;
     const int64_t zeros = a.accumulate ? 0 : (stores < (1 << 20) ? stores : 1 << 20);
+    if (a.M <= kRankMax) {
+        a.sorters = (int32_t)ceil_div(a.M, 64);
+        if (a.sorters + zeros == 0) return hipSuccess;
+        hipLaunchKernelGGL((token_rank_kernel<TG>), dim3((unsigned)(a.sorters + zeros)), dim3(kSortThreads),
+                           (unsigned)(a.sorters * 256 + kSortWaves * 256), stream, a);
+        return hipGetLastError();
+    }
+    const hipError_t e = allow_lds<token_sort_kernel<TG>, kSortLds>();
+    if (e != hipSuccess) return e;
+    a.sorters = (int32_t)ceil_div(a.M, a.chunk);
+    const unsigned lds = (unsigned)(ceil_div(a.chunk, kSortThreads) * kSortThreads * 8 + kSortWaves * kBins * 2 + 64);
     hipLaunchKernelGGL((token_sort_kernel<TG>), dim3((unsigned)(a.sorters + zeros)), dim3(kSortThreads), lds, stream, a);
     return hipGetLastError();
 }
@@ -465,7 +556,7 @@ template <typename T, typename TG>
 hipError_t run_sums(const EmbBwdArgs& a, hipStream_t stream) {
     const int64_t runs = ceil_div(a.M, a.run);
     const int slices = (int)ceil_div(a.D, kSumCols);
-    const dim3 grid((unsigned)(runs * slices)), block(kSumThreads);
+    const dim3 grid((unsigned)(runs * slices)), block(a.D <= 64 * CH ? 64 : kSumThreads);
     auto launch = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
         auto by_run = [&](auto run) {
@@ -487,7 +578,12 @@ hipError_t run_join(const EmbBwdArgs& a, hipStream_t stream) {
     const int64_t runs = ceil_div(a.M, a.run);
     if (runs < 2) return hipSuccess;
     const int slices = (int)ceil_div(a.D, kJoinCols);
-    hipLaunchKernelGGL((token_join_kernel<TG>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices);
+    int groups = 1;
+    while (groups < 16 && a.D * 2 * groups <= kJoinCols) groups *= 2;
+    if (groups > 1)
+        hipLaunchKernelGGL((token_join_kernel<TG, true>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices, groups);
+    else
+        hipLaunchKernelGGL((token_join_kernel<TG, false>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices, 1);
     return hipGetLastError();
 }
 
@@ -548,7 +644,7 @@ niti_status niti_embedding_bwd(const void* dy, int64_t lddy, int type, const int
     if (M > 0 && (!ws || ws_bytes < (size_t)w.total)) return NITI_ERR_WORKSPACE;
     if (M > 0 && ((uintptr_t)ws & 15)) return NITI_ERR_ARG;
     char* base = (char*)ws;
-    const bool chunks = M > kSortFew;
+    const bool chunks = M > kRankMax;
     hipStream_t s = (hipStream_t)stream;
     EmbBwdArgs a{dy, tokens, dtable, M > 1 ? lddy : D, V > 1 ? ldt : D, M, V, D, alpha, accumulate != 0, sort_passes(V), run_of(M, D), 0,
                  (int32_t*)(base + w.order), (int32_t*)(base + w.key), chunks ? (int32_t*)(base + w.order1) : nullptr,
