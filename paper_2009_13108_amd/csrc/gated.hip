@@ -11,19 +11,24 @@ namespace niti {
 
 namespace {
 
-// What a call takes in each kernel (see the forms), N counting the weight rows: as fitted for the plain product's tiles, but for 64 x
-// 128.  On 400 random products of 1..8192 x 32..9216 x 32..9216 what they pick takes 2.3% longer than the fastest in the mean, on
-// 200 with rows at odd addresses 2.2%; constants fitted to these calls were no better on others.  Parts of a sum side by side, as the
-// plain product has them, gained on none of the 400 more than 12%, in the mean nothing.
-constexpr Cost kPair12{16, 32, kSpread, 1.92f, 0.61f, 0.95f, 1.33f};
-constexpr Cost kPair22{32, 32, kSpread, 2.06f, 0.75f, 1.18f, 1.90f};
-constexpr Cost kPairBytes12{16, 32, kSpread, 2.01f, 0.59f, 1.23f, 2.45f};
-constexpr Cost kPairBytes22{32, 32, kSpread, 2.02f, 0.86f, 1.39f, 3.48f};
-constexpr Cost kPair64{64, 128, kTwo, 2.09f, 1.8f, 1.6f, 2.6f};
-constexpr Cost kPairAny64{64, 64, kSpread, 2.84f, 1.02f, 3.38f, 4.07f};
-constexpr Cost kPair128{128, 128, kTwo, 0.96f, 3.17f, 3.79f, 3.45f};
-constexpr Cost kPairDeep128{128, 128, kRounds, 0.12f, 4.49f, 3.72f, 2.33f};
-constexpr Cost kPair256{256, 256, kRounds, 0.41f, 11.1f, 9.31f, 5.98f};
+// What a call takes in each kernel (see the forms), N counting the weight rows; store: what z adds to a round.  Found for the least
+// time lost on half of 500 random calls of 1..8192 x 32..9216 x 32..9216 with whole pieces: on the other half what they pick takes
+// 0.8% longer than the fastest kernel in the mean, with z 1.9% (with the plain product's constants 1.4% and 2.9%).  Rows at odd addresses
+// go by the plain product's, 2.2% from the fastest on 200 calls.  Parts of a sum side by side, as that has them, gained on none of 400 calls
+// more than 12%, in the mean nothing.
+struct PairCost {
+    Cost cost;
+    float store;
+};
+constexpr PairCost kPair12{{16, 32, kSpread, 2.39f, 1.22f, 0.99f, 3.07f}, 0.14f};
+constexpr PairCost kPair22{{32, 32, kSpread, 2.46f, 0.74f, 1.16f, 3.04f}, 1.09f};
+constexpr PairCost kPairBytes12{{16, 32, kSpread, 2.01f, 0.59f, 1.23f, 2.45f}, 0.f};
+constexpr PairCost kPairBytes22{{32, 32, kSpread, 2.02f, 0.86f, 1.39f, 3.48f}, 0.f};
+constexpr PairCost kPair64{{64, 128, kTwo, 1.15f, 3.70f, 1.35f, 2.86f}, 0.83f};
+constexpr PairCost kPairAny64{{64, 64, kSpread, 2.84f, 1.02f, 3.38f, 4.07f}, 0.f};
+constexpr PairCost kPair128{{128, 128, kTwo, 2.84f, 2.72f, 4.16f, 2.62f}, 0.17f};
+constexpr PairCost kPairDeep128{{128, 128, kRounds, 1.38f, 3.45f, 4.24f, 0.13f}, 1.91f};
+constexpr PairCost kPair256{{256, 256, kRounds, 4.69f, 11.87f, 5.12f, 0.30f}, 1.33f};
 
 struct Choice {
     enum { kS12, kS22, k64, k128, k128d, k256 } kernel;
@@ -31,13 +36,13 @@ struct Choice {
     bool pack;   // the operands are copied to whole aligned pieces first
 };
 
-// keep: z is stored as well, by all CUs at once where there is one tile a CU, which nothing hides (4096 x 8192 x 4096: 29 us of 284; 8192 x
-// 2048 x 1024: 256 x 256 tiles 62 us, 128 x 128 ones, two a CU, 56, without z 46 either way).
+// keep: z is stored as well.
 Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room, bool keep) {
     // columns of whole tiles: a half's last tile is not filled by the other half
     const bool whole = rows == kOfPieces, words = rows != kOfBytes;
-    auto at = [&](Cost c, float store = 0.f) {
-        c.round += keep ? store : 0.f;
+    auto at = [&](const PairCost& p) {
+        Cost c = p.cost;
+        c.round += keep ? p.store : 0.f;
         return cost(c, M, (F + c.bn / 2 - 1) / (c.bn / 2) * c.bn, K);
     };
     Choice c{Choice::kS12, at(words ? kPair12 : kPairBytes12), false};
@@ -47,9 +52,10 @@ Choice choose(int64_t M, int64_t F, int64_t K, Rows rows, size_t room, bool keep
     take(Choice::kS22, at(words ? kPair22 : kPairBytes22));
     take(Choice::k64, at(whole ? kPair64 : kPairAny64));
     if (whole) {
-        take(Choice::k128, at(kPair128, 1.3f));
-        take(Choice::k128d, at(kPairDeep128, 1.3f) * (M * F > 128 * 128 * 128 ? 1.08f : 1.f));
-        take(Choice::k256, at(kPair256, 7.8f));
+        take(Choice::k128, at(kPair128));
+        // (where tiles outnumber the CUs, two a CU come out a little better than the model has them)
+        take(Choice::k128d, at(kPairDeep128) * (M * F > 128 * 128 * 128 ? 1.08f : 1.f));
+        take(Choice::k256, at(kPair256));
     }
     const size_t copies = whole ? 0 : pack_bytes(M, 2 * F, K);
     if (copies > 0 && copies <= room) {

@@ -7,7 +7,7 @@ import scaled_ref as R
 from helpers import say
 from paper_2009_13108_amd import niti
 from test_gpu_linear import ACTS, BF16, F16, F32, codes, codes64, floats, row_scales
-from test_gpu_linear_kernels import launches
+from test_gpu_linear_kernels import NAMES, launches
 
 pytestmark = pytest.mark.gpu
 
@@ -89,6 +89,38 @@ def test_forward_epilogues(m, f, k, dtype, act):
 def test_forward_strides(m, f, k, pad):
     say("gated_fwd strides", m, f, k, pad)
     run_forward(m, f, k, BF16, pad=pad)
+
+
+RING64, RING128, DEEP128, RING256 = "64,128,3,2,2,128", "128,128,2,4,2,128", "128,128,4,4,2,128", "256,256,4,2,4,64"
+
+# rows, columns, sum, padding of the operands' rows, kernel without z, kernel with it (None: the same)
+CASES = [
+    (4001, 2001, 272, (0, 0), "ring:" + RING256, None), (3841, 2045, 2064, (0, 16), "ring:" + RING256, None),
+    (4001, 1999, 1003, (1, 2), "ring:" + RING256, None),                                                     # rows copied first
+    (4001, 2001, 16, (0, 0), "ring:" + RING128, None), (4001, 2001, 80, (16, 0), "ring:" + RING128, None),
+    (2100, 1051, 1040, (0, 0), "ring:" + RING128, None), (2100, 1051, 515, (3, 0), "ring:" + RING128, None),
+    (257, 10001, 160, (0, 48), "ring:" + RING128, None),
+    (2000, 751, 528, (0, 0), "ring:" + DEEP128, None), (1024, 1100, 2048, (16, 16), "ring:" + DEEP128, None),
+    (1500, 751, 304, (0, 0), "ring:" + DEEP128, "ring:" + RING64), (1000, 751, 16, (0, 0), "ring:" + DEEP128, "ring:" + RING64),
+    (999, 753, 400, (48, 0), "ring:" + RING64, None), (700, 700, 1024, (0, 0), "ring:" + RING64, None),
+    (1000, 751, 97, (2, 5), "any", None), (1000, 751, 100, (4, 8), "any", None), (1500, 751, 300, (1, 1), "any", None),
+    (1, 1001, 260, (4, 0), "small:2,2,0", "small:1,2,0"), (300, 500, 4100, (0, 0), "small:2,2,0", None),
+    (257, 257, 148, (0, 4), "small:2,2,0", "small:1,2,0"),
+    (1, 1001, 259, (1, 0), "small:1,2,1", None), (257, 257, 143, (0, 2), "small:1,2,1", None), (300, 500, 4096, (1, 0), "small:2,2,1", None),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("m,f,k,pad,without,with_z", CASES)
+def test_kernel(m, f, k, pad, without, with_z, dtype):
+    """Each kernel at ragged sizes that the choice gives it: the timing records say which ran."""
+    say("gated kernel", m, f, k, pad, without, with_z, dtype)
+
+    def label(kernel):
+        kind, _, args = kernel.partition(":")
+        return "linear_%s_kernel<%s,%spairs>" % (kind, NAMES[dtype], args + "," if args else "")
+    run_forward(m, f, k, dtype, act="silu", keep=False, pad=pad, kernel=label(without))
+    run_forward(m, f, k, dtype, act="gelu", keep=True, pad=pad, kernel=label(with_z or without))
 
 
 def test_forward_special_values():

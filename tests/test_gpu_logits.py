@@ -70,6 +70,18 @@ def test_logprobs(m, v, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,v", [(520, 34000), (513, 17001), (1, 800001), (1, 1200001), (1, 3000001), (70, 90000)])
+def test_many_or_very_long_rows(m, v, dtype):
+    """Rows in parts of each size, up to the widest rows; and whole rows of the widest kernel."""
+    say("logits", m, v, dtype)
+    x, tok = logits(m, v, dtype, 1), some_tokens(m, v, 2)
+    check_logprobs(x, tok, 20, 0.7)
+    if m < 100:
+        tv, ti = teacher_of(x, 20, 12, dtype)
+        check_distill(x, tv, ti, 0.7, torch.full((m,), 0.25, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("v", [40, 700, 5000, 33000, 140000])
 def test_equal_logits(v, dtype):
     """Ties go to the lowest column: all equal, few distinct values, rows in order, zeros of both signs."""
