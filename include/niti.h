@@ -348,6 +348,8 @@ niti_status niti_dropout_bwd(const int8_t *dy, const uint8_t *keep, int8_t *dx, 
  *   Aliasing    An output may be one of the call's own inputs (same address,
  *               type and stride) where that is said; otherwise they must not
  *               overlap.
+ *   Workspace   Nothing in it is kept from one call for the next.  Calls that
+ *               may run at once, captured graphs among them, take one each.
  */
 typedef enum niti_type {
     NITI_F32 = 0,

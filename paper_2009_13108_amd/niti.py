@@ -795,6 +795,16 @@ def linear_bwd(dy, a, b, s_a, s_b, ws, z=None, act=ACT_NONE, da=None, db=None, d
          _stream(stream))
 
 
+def _stream_on(dev, stream):
+    """Handle of the stream, the current one if none is given, for work on tensors of device dev: a launch goes to
+    the current device, which may not be able to read another's memory."""
+    here = _torch_mod._C._cuda_getDevice()
+    if here != dev or (stream is not None and stream.device_index != dev):
+        raise ValueError("tensors are on device %d, the call's stream on device %d, the current device is %d" % (
+            dev, here if stream is None else stream.device_index, here))
+    return _stream(stream)
+
+
 def gated_fwd(a, b, out, s_a, s_b, act=ACT_SILU, bias=None, z=None, ws=None, stream=None):
     """out = act(gate) * up, where b [2F][K] holds the rows of both projections, the gates' first:
     [gate up] = z = s_a[m] s_b[n] sum_k a[m][k] b[n][k] + bias[n]; ws as
@@ -811,7 +821,7 @@ def gated_fwd(a, b, out, s_a, s_b, act=ACT_SILU, bias=None, z=None, ws=None, str
     psb, nsb = _scales(s_b, dev, 2 * F, "s_b")
     pws, nws = _ws_args(ws, dev)
     _run("niti_gated_fwd", pa, lda, psa, nsa, pb, ldb, psb, nsb, _vec(bias, dev, 2 * F, "bias"),
-         F32 if bias is None else _type_of(bias.dtype, "bias"), act, pz, ldz, po, ldo, M, F, K, kind, pws, nws, _stream(stream))
+         F32 if bias is None else _type_of(bias.dtype, "bias"), act, pz, ldz, po, ldo, M, F, K, kind, pws, nws, _stream_on(dev, stream))
 
 
 def gated_bwd(dy, z, a, b, s_a, s_b, ws, act=ACT_SILU, da=None, db=None, dbias=None, mode=RTN, seed=0, call=0, stream=None):
@@ -832,7 +842,7 @@ def gated_bwd(dy, z, a, b, s_a, s_b, ws, act=ACT_SILU, da=None, db=None, dbias=N
     pws, nws = _ws_args(ws, dev)
     _run("niti_gated_bwd", pdy, lddy, pz, ldz, act, pa, lda, psa, nsa, pb, ldb, psb, nsb, pda, ldda, pdb, lddb,
          _vec(dbias, dev, 2 * F, "dbias", f32), M, F, K, mode, seed & 0xFFFFFFFFFFFFFFFF, call & 0xFFFFFFFF, kind, pws, nws,
-         _stream(stream))
+         _stream_on(dev, stream))
 
 
 # ------------------------------------------------------------------ tokens and logits
@@ -857,7 +867,7 @@ def embedding_fwd(table, tokens, out, table_scale=None, alpha=1.0, stream=None):
     pt, ldt = _mat(table, dev, table.dtype, (V, D), "table")
     po, ldo = _mat(out, dev, dt, (M, D), "out", True)
     _run("niti_embedding_fwd", pt, ldt, t_type, _vec(table_scale, dev, V, "table_scale", _torch_mod.float32),
-         _vec(tokens, dev, M, "tokens", _torch_mod.int32), po, ldo, M, V, D, alpha, kind, _stream(stream))
+         _vec(tokens, dev, M, "tokens", _torch_mod.int32), po, ldo, M, V, D, alpha, kind, _stream_on(dev, stream))
 
 
 def embedding_bwd(dy, tokens, dtable, ws, alpha=1.0, accumulate=False, stream=None):
@@ -872,7 +882,7 @@ def embedding_bwd(dy, tokens, dtable, ws, alpha=1.0, accumulate=False, stream=No
     pg, ldg = _mat(dtable, dev, gt, (V, D), "dtable", True)
     pws, nws = _ws_args(ws, dev)
     _run("niti_embedding_bwd", pdy, lddy, kind, _vec(_given(tokens, "tokens"), dev, M, "tokens", _torch_mod.int32), pg, ldg, gkind,
-         M, V, D, alpha, 1 if accumulate else 0, pws, nws, _stream(stream))
+         M, V, D, alpha, 1 if accumulate else 0, pws, nws, _stream_on(dev, stream))
 
 
 def token_logprobs(logits, tokens=None, logp=None, lse=None, entropy=None, top_logp=None, top_idx=None, scale=1.0, ws=None,
@@ -892,7 +902,7 @@ def token_logprobs(logits, tokens=None, logp=None, lse=None, entropy=None, top_l
     pws, nws = _ws_args(ws, dev)
     _run("niti_token_logprobs", px, ldx, _vec(tokens, dev, M, "tokens", i32), _vec(logp, dev, M, "logp", f32),
          _vec(lse, dev, M, "lse", f32), _vec(entropy, dev, M, "entropy", f32), pv, pi, M, V, top, scale, kind, pws, nws,
-         _stream(stream))
+         _stream_on(dev, stream))
 
 
 def _misshapen(t, shape, what):
@@ -920,7 +930,7 @@ def distill_fwd(logits, t_val, t_idx, loss, lse=None, dlogits=None, dloss=None, 
     f32 = _torch_mod.float32
     pws, nws = _ws_args(ws, dev)
     _run("niti_distill_fwd", *operands, _vec(_given(loss, "loss"), dev, M, "loss", f32), _vec(lse, dev, M, "lse", f32), *grad, M, V,
-         top, scale, kind, pws, nws, _stream(stream))
+         top, scale, kind, pws, nws, _stream_on(dev, stream))
 
 
 def distill_bwd(logits, t_val, t_idx, lse, dloss, dlogits, scale=1.0, stream=None):
@@ -928,7 +938,7 @@ def distill_bwd(logits, t_val, t_idx, lse, dloss, dlogits, scale=1.0, stream=Non
     logits (niti_distill_bwd)."""
     M, V, top, dev, kind, operands, grad = _distill_args(logits, t_val, t_idx, dloss, _given(dlogits, "dlogits"))
     _run("niti_distill_bwd", *operands, _vec(_given(lse, "lse"), dev, M, "lse", _torch_mod.float32), *grad, M, V, top, scale, kind,
-         _stream(stream))
+         _stream_on(dev, stream))
 
 
 ADAMW_BLOCK = 256   # consecutive elements that share a scale in an 8-bit state
