@@ -3,13 +3,15 @@
 // Forward:   out[m] = alpha table[token m], the table in a float type or as int8 rows with a scale each.
 // Gradient:  dtable[v] = alpha sum over the m with token v of dy[m]  (+ dtable[v]).
 //
-// The gradient goes by sorted tokens, so that every sum has a fixed order and no
-// atomics.  (1) Up to 8192 tokens are placed by comparing all with all; of more, workgroups sort 2048 each in their LDS (radix sort,
-// stable; 16384 in batches of more than 32768), and a second launch places a chunk's tokens by binary searches in the other
-// chunks; meanwhile the other workgroups of the first launch write the table's zeros.  (2) Sixteen consecutive sorted rows at a time are
-// read and added up: a token whose rows lie inside such a stretch gets its row
-// at once, one that crosses its ends leaves partial sums in the workspace, and (3) those are joined
-// in order.  However often a token occurs, the work is split evenly.
+// The gradient goes by sorted tokens, so that every sum has a fixed order and no atomics:
+//  (1) a launch that puts the tokens in order.  Up to 8192 are placed by comparing all with all (4111: 9 us, where sorting and placing
+//      took 16); of more, workgroups sort 2048 each in their LDS (radix sort, stable; 16384 each in batches of more than 32768), and a
+//      second launch places a chunk's tokens by binary searches in the other chunks.  Meanwhile the first launch's other workgroups
+//      write the table's zeros, which bound it where they are many (32000 x 4096 bf16, 262 MB: 44 us, 6.0 TB/s).
+//  (2) Eight or sixteen consecutive sorted rows at a time are read and added up (8192 x 4096 bf16: 18.6 us, 3.6 TB/s).  A token whose
+//      rows lie inside such a stretch gets its row at once; one that crosses its ends leaves partial sums in the workspace, and
+//  (3) those are joined in order (8.5 us, latency).  However often a token occurs, the work is split evenly.
+// Small batches are bound by the latency of the three launches.
 #include "linear.h"
 
 #include <atomic>
@@ -19,10 +21,11 @@ namespace niti {
 
 namespace {
 
-constexpr int kSortMax = 16384;   // tokens that one workgroup sorts at most
-constexpr int kSortFew = 2048;    // and where the whole batch is no more than
+// Tokens are compared all with all up to kRankMax (its time grows with their square: with 16384 of them sorting was faster).
+constexpr int kRankMax = 8192;
+constexpr int kSortFew = 2048;    // tokens that a workgroup sorts, in batches of up to kMergeMax, all of whose keys the next launch has in LDS
 constexpr int kMergeMax = 32768;
-constexpr int kRankMax = 8192;    // tokens that are compared all with all
+constexpr int kSortMax = 16384;   // and in larger ones
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kRounds = kSortMax / kSortThreads;
 constexpr int kBins = 256;
 constexpr int kRunMin = 8;        // sorted rows of a stretch: 8 or 16
@@ -123,8 +126,8 @@ __device__ __forceinline__ void write_zeros(const EmbBwdArgs& a) {
 }
 
 // (1) Few tokens: a token's place is the number of those before it, smaller ones and equal ones with a smaller index, counted by
-// comparing all with all (two instructions a pair, on all CUs; 4096 tokens in 7 us where sorting and placing took 16).  A workgroup
-// places 64, its sixteen waves count in a sixteenth of the batch each.
+// comparing all with all (two instructions a pair, on all CUs; bound by them and by each workgroup's reading of all tokens).  A
+// workgroup places 64, its sixteen waves count in a sixteenth of the batch each.
 template <typename TG>
 __global__ __launch_bounds__(kSortThreads) void token_rank_kernel(EmbBwdArgs a) {
     extern __shared__ __attribute__((aligned(16))) int32_t keys[];   // [M to a multiple of 64], and [16][64] counts

@@ -5,10 +5,14 @@
 // With u_v = x_v - max x:  S = sum exp(scale u_v), W = sum u_v exp(scale u_v),
 //   lse = scale max + ln S,  log p_v = scale u_v - ln S,  entropy = ln S - scale W / S,
 //   dx_v = dloss scale (exp(scale u_v) / S - sum of the p_j of v).
-// A row is read once: it stays in the registers of one workgroup (up to 64K columns in 32 bits, 128K
-// in 16) as it was loaded, the maximum is found first and the sums next, so
-// that every element costs one exponential; longer rows, and few of them, are split over
-// workgroups whose parts a second launch joins.  The fused gradient writes from the same registers.
+// A row is read once: it stays in the registers of one workgroup (up to 64K columns, in distillation 128K of 16 bits; the plans below) as it
+// was loaded, the maximum is found first and the sums next, so that every element costs one exponential; longer rows, and few of
+// them, are split over workgroups whose parts a second launch joins.  The fused gradient writes from the same registers.
+// What bounds them: distillation and its gradient memory (4096 x 32000 bf16 with the gradient, 524 MB, 99 us: 5.3 TB/s); log
+// probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 69 us, 3.8 TB/s: some ten instructions an element, of which the
+// exponential takes four issue slots) between the barriers of two workgroups a CU; of 32 bits memory, in parts (77 x 128001 14.5 us and
+// 5 for the join); one row latency (1 x 32000 7.5 us).  Workgroups that go on to another row, its loads out while the last one's results
+// are joined, spilled registers and took 101 us for 69.
 //
 // The k largest of a row: 64 groups of threads have a maximum each, and the k-th
 // largest of those is a bound that at least k logits reach.  Logits that reach it
@@ -437,6 +441,7 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void logprobs_kernel
     for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
     float top[VPT];
     const float mx = max_of(p, top);
+    const float x_of_tok = lane_of(to_f(x_tok), 0);   // (the same in all lanes, as some below: in a scalar register)
     // 64 groups of NW neighbouring threads
     const float m16 = max_of_16(mx), of_group = NW == 1 ? mx : (NW == 4 ? max_of_4(mx) : (NW == 8 ? max_of_8(mx) : m16));
     if (t % NW == 0) group[t / NW] = of_group;   // (lane steps take all lanes: none of them in a branch)
@@ -458,11 +463,11 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void logprobs_kernel
     if ((t & 63) == 0) red_s[wave] = st.s, red_w[wave] = st.w;
     __syncthreads();
     const float back = __builtin_amdgcn_exp2f(-base.r);
-    st.s = join_sum<NW>(red_s) * back;
-    st.w = join_sum<NW>(red_w) * back - base.r * st.s;
-    const float logs = st.log();
+    st.s = lane_of(join_sum<NW>(red_s) * back, 0);
+    st.w = lane_of(join_sum<NW>(red_w) * back - base.r * st.s, 0);
+    const float logs = lane_of(st.log(), 0);
     if (t == 0) {
-        if (a.parts == 1) put_scalars(a, m, st, logs, tok, to_f(x_tok));
+        if (a.parts == 1) put_scalars(a, m, st, logs, tok, x_of_tok);
         else a.stat[m * a.parts + part] = st;
     }
     if (!a.top) return;
@@ -803,7 +808,7 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
         return none ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
     };
     T* dx = (T*)a.dx + m * a.lddx;
-    // (every wave's loads are done: each has passed the barriers with what it loaded after them)
+    // (every wave's loads of the row come before the barriers above: dx may be x)
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
         float v[CH];
