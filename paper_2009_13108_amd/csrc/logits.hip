@@ -137,6 +137,19 @@ __device__ __forceinline__ void logit_values(const Piece<T>& p, float (&v)[CH]) 
 #pragma unroll
     for (int e = 0; e < CH; e++) v[e] = to_f(t[e]);
 }
+// A wave's pieces that are whole, and those that have any columns of the row: the others cost no arithmetic (10000 columns in a
+// workgroup's 16384: TIMES).  left: columns from the workgroup's first to the row's end.
+template <int NW, int VPT>
+struct Live {
+    int whole, all;
+    __device__ __forceinline__ Live(int left, int wave) {
+        constexpr int STEP = 64 * NW * CH;
+        const int mine = left - wave * 64 * CH;
+        whole = min(max(mine - 64 * CH + STEP, 0) / STEP, VPT);
+        all = min(max(mine + STEP - 1, 0) / STEP, VPT);
+    }
+};
+
 // Minus infinity in the place of the elements that are not the piece's own.
 template <typename T, bool TINY>
 __device__ __forceinline__ void mask_logits(Piece<T>& p, int c, int V) {
@@ -213,21 +226,27 @@ __device__ __forceinline__ void forget_values(Piece<T> (&p)[VPT]) {
 }
 // S and W over a thread's pieces, both as their powers are; KEEP: the powers stay in e.  GUARD: there may be minus
 // infinities, whose terms of W are 0; without it they leave W a NaN.
-template <typename T, int VPT, bool WANT_W, bool KEEP, bool GUARD>
-__device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], const Base& b, float& s, float& w, float (&e)[KEEP ? VPT : 1][CH]) {
+template <typename T, int NW, int VPT, bool WANT_W, bool KEEP, bool GUARD>
+__device__ __forceinline__ void row_sums(Piece<T> (&p)[VPT], const Live<NW, VPT>& live, const Base& b, float& s, float& w,
+                                         float (&e)[KEEP ? VPT : 1][CH]) {
     if (sizeof(T) == 2) forget_values(p);
     s = w = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
-        float v[CH];
-        logit_values(p[i], v);
+        auto add = [&](auto guard) {
+            float v[CH];
+            logit_values(p[i], v);
 #pragma unroll
-        for (int k = 0; k < CH; k++) {
-            const float u = b.arg(v[k]), x = __builtin_amdgcn_exp2f(u);
-            s += x;
-            if (WANT_W) w = __builtin_fmaf(x, GUARD ? fmaxf(u, -0x1p100f) : u, w);
-            if (KEEP) e[i][k] = x;
-        }
+            for (int k = 0; k < CH; k++) {
+                const float u = b.arg(v[k]), x = __builtin_amdgcn_exp2f(u);
+                s += x;
+                if (WANT_W) w = __builtin_fmaf(x, decltype(guard)::value ? fmaxf(u, -0x1p100f) : u, w);
+                if (KEEP) e[i][k] = x;
+            }
+        };
+        constexpr bool BOTH = WANT_W && !GUARD;   // (past the row's end there are minus infinities)
+        if (i < (BOTH ? live.whole : live.all)) add(std::integral_constant<bool, GUARD>());
+        else if (BOTH && i < live.all) add(std::true_type());
     }
     if (sizeof(T) == 2 && !KEEP) forget_values(p);
 }
@@ -241,11 +260,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 // A thread's largest, and that of each piece.
-template <typename T, int VPT>
-__device__ __forceinline__ float max_of(const Piece<T> (&p)[VPT], float (&top)[VPT]) {
+template <typename T, int NW, int VPT>
+__device__ __forceinline__ float max_of(const Piece<T> (&p)[VPT], const Live<NW, VPT>& live, float (&top)[VPT]) {
     float mx = neg_inf();
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
+        top[i] = neg_inf();
+        if (i >= live.all) continue;
         float v[CH];
         logit_values(p[i], v);
         top[i] = max3(max3(max3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]);
@@ -432,15 +453,17 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void logprobs_kernel
     const int part = blockIdx.x % (uint32_t)a.parts, V = (int)a.V, c0 = part * LEN;
     const T* row = (const T*)a.x + m * a.ldx;
     const int tok = a.parts == 1 && a.tokens ? a.tokens[m] : -1;
+    const Live<NW, VPT> live(V - c0, wave);
     Piece<T> p[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
     const T x_tok = row[(uint32_t)tok < (uint32_t)V ? tok : 0];
     if (t == 0) n_s = 0;
 #pragma unroll
-    for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
+    for (int i = 0; i < VPT; i++)
+        if (i >= live.whole && i < live.all) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
     float top[VPT];
-    const float mx = max_of(p, top);
+    const float mx = max_of(p, live, top);
     const float x_of_tok = lane_of(to_f(x_tok), 0);   // (the same in all lanes, as some below: in a scalar register)
     // 64 groups of NW neighbouring threads
     const float m16 = max_of_16(mx), of_group = NW == 1 ? mx : (NW == 4 ? max_of_4(mx) : (NW == 8 ? max_of_8(mx) : m16));
@@ -456,8 +479,8 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void logprobs_kernel
     }
     const Base base(st.m, a.c2);
     float none[1][CH];
-    row_sums<T, VPT, true, false, false>(p, base, st.s, st.w, none);
-    if (__any(st.w != st.w)) row_sums<T, VPT, true, false, true>(p, base, st.s, st.w, none);   // masks here, or past the row's end
+    row_sums<T, NW, VPT, true, false, false>(p, live, base, st.s, st.w, none);
+    if (__any(st.w != st.w)) row_sums<T, NW, VPT, true, false, true>(p, live, base, st.s, st.w, none);   // masks here
     st.s = wave_sum(st.s);
     st.w = wave_sum(st.w);
     if ((t & 63) == 0) red_s[wave] = st.s, red_w[wave] = st.w;
@@ -677,22 +700,24 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
     Teacher<NW, KPT> teach;
     teach.load(a, m);
     const float g1 = GRAD && a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
+    const Live<NW, VPT> live(V - c0, wave);
     Piece<T> p[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
     T z[KPT];
     teach.gather(a, row, 0, V, z);
 #pragma unroll
-    for (int i = 0; i < VPT; i++) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
+    for (int i = 0; i < VPT; i++)
+        if (i >= live.whole && i < live.all) mask_logits<T, TINY>(p[i], c0 + (i * NT + t) * CH, V);
     float tops[VPT];
-    const float wm = wave_max(max_of(p, tops)), wt = wave_max(teach.top(a));
+    const float wm = wave_max(max_of(p, live, tops)), wt = wave_max(teach.top(a));
     if ((t & 63) == 0) red_m[wave] = wm, red_t[wave] = wt;
     __syncthreads();
     Stat st;
     st.m = join_max<NW>(red_m);
     const Base base(st.m, a.c2);
     float e[KEEP ? VPT : 1][CH];
-    row_sums<T, VPT, false, KEEP, false>(p, base, st.s, st.w, e);
+    row_sums<T, NW, VPT, false, KEEP, false>(p, live, base, st.s, st.w, e);
     const float ws = wave_sum(st.s), wu = wave_sum(teach.powers(a, join_max<NW>(red_t)));
     if ((t & 63) == 0) red_s[wave] = ws, red_u[wave] = wu;
     __syncthreads();
@@ -714,6 +739,7 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
         T* dx = (T*)a.dx + m * a.lddx;
 #pragma unroll
         for (int i = 0; i < VPT; i++) {
+            if (i >= live.all) continue;
             float v[CH];
             if constexpr (!KEEP) logit_values(p[i], v);
             if (teach.any) {   // (uniform)
@@ -788,6 +814,7 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     Teacher<NW, KPT> teach;
     teach.load(a, m);
     const float lse = a.lse_in[m], g1 = a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
+    const Live<NW, VPT> live(V - c0, wave);
     Piece<T> p[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; i++) p[i] = load_logits<T, TINY>(row, c0 + (i * NT + t) * CH, V);
@@ -811,6 +838,7 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     // (every wave's loads of the row come before the barriers above: dx may be x)
 #pragma unroll
     for (int i = 0; i < VPT; i++) {
+        if (i >= live.all) continue;
         float v[CH];
         logit_values(p[i], v);
 #pragma unroll
