@@ -9,7 +9,7 @@
 // was loaded, the maximum is found first and the sums next, so that every element costs one exponential; longer rows, and few of
 // them, are split over workgroups whose parts a second launch joins.  The fused gradient writes from the same registers.
 // What bounds them: distillation and its gradient memory (4096 x 32000 bf16 with the gradient, 524 MB, 99 us: 5.3 TB/s); log
-// probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 69 us, 3.8 TB/s: some ten instructions an element, of which the
+// probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 62 us, 4.2 TB/s: some ten instructions an element, of which the
 // exponential takes four issue slots) between the barriers of two workgroups a CU; of 32 bits memory, in parts (77 x 128001 14.5 us and
 // 5 for the join); one row latency (1 x 32000 7.5 us).  Workgroups that go on to another row, its loads out while the last one's results
 // are joined, spilled registers and took 101 us for 69.
@@ -138,7 +138,7 @@ __device__ __forceinline__ void logit_values(const Piece<T>& p, float (&v)[CH]) 
     for (int e = 0; e < CH; e++) v[e] = to_f(t[e]);
 }
 // A wave's pieces that are whole, and those that have any columns of the row: the others cost no arithmetic (10000 columns in a
-// workgroup's 16384: TIMES).  left: columns from the workgroup's first to the row's end.
+// workgroup's 16384: log probabilities of 4096 rows of bf16 42.3 -> 27.3 us).  left: columns from the workgroup's first to the row's end.
 template <int NW, int VPT>
 struct Live {
     int whole, all;
@@ -899,18 +899,18 @@ inline Plan short_row(int64_t V) {
     return Plan{s, 1};
 }
 
-// Whole rows need no second launch (3 us); parts of few registers leave more of them on a CU.  Both ways (us; whole, in parts),
-// 16 bits: 32000 columns, 1 row 8.7, 10.6, 1000 21.5, 26.0, 4096 62, 79; 60000 columns, 256 rows 14.3, 18.1, 1000 50.1, 44.1;
-// in 32 bits: 32000 columns, 256 rows 10.7, 14.2, 1000 36.9, 32.0, 2000 67, 56; 60000 columns, 64 rows 13.1, 12.4.  Parts of
-// 32768 (16 bits) where there are 1024 of them: 1000 x 128000 69 for 87 in parts of 8192, 300 x 50000 23 for 18.
+// Whole rows need no second launch (3 us), parts of fewer registers leave more of them on a CU.  Both ways in us, whole and in parts
+// (of 16384 columns in 16 bits, of 8192 in 32):  16 bits, 32000 columns, 1000 rows 20.2, 23.7; 40000 columns, 60 rows 9.2, 11.2, 300
+// 17.0, 16.1, 1000 33.2, 28.5; 60000 columns, 300 rows 19.8, 18.4;  32 bits, 32000 columns, 300 rows 16.3, 16.9, 1000 33.2, 29.3, 4000 125,
+// 104; 60000 columns, 60 rows 10.3, 12.4, 300 23.7, 22.5.  Which parts, of 4096, 8192 and 16384: 100000 columns in 16 bits, 1 row
+// 9.4, 10.5, 10.5, 60 12.6, 12.6, 12.4, 1000 79, 56, 56; in 32 bits, 60 rows 14.0, 14.5, 14.2, 300 29.8, 27.4, 27.4, 1000 85, 74, 75.
 Plan logprobs_plan(int64_t M, int64_t V, int type) {
     if (V <= 16384) return short_row(V);
     const bool half = type != NITI_F32;
     if (V <= 32768 && (half || M <= 512)) return Plan{k32768w, 1};
-    if (half && V <= 65536 && M <= 512) return Plan{k65536, 1};
-    if (!half) return in_parts(V, {k4096, k8192, k16384, k32768w, k65536});
-    const Plan wide = in_parts(V, k32768w);
-    return M * wide.parts >= 1024 ? in_parts(V, {k32768w, k65536}) : in_parts(V, {k8192, k16384, k32768w, k65536});
+    if (V > 32768 && V <= 65536 && M <= 256) return Plan{k65536, 1};
+    if (M <= (half ? 48 : 96)) return in_parts(V, {k4096, k8192, k16384, k32768w, k65536});
+    return half ? in_parts(V, {k16384, k32768w, k65536}) : in_parts(V, {k8192, k16384, k32768w, k65536});
 }
 
 // With the gradient a second reading costs more than the registers of a whole row: parts only where those do not hold it (77 x

@@ -81,6 +81,22 @@ def test_many_or_very_long_rows(m, v, dtype):
         check_distill(x, tv, ti, 0.7, torch.full((m,), 0.25, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("m,v", [(5, 1023), (5, 1537), (4, 2560), (4, 2561), (3, 6151), (3, 10000), (3, 12287), (2, 24577), (3, 33281), (300, 40003),
+                                 (600, 20001)])
+def test_rows_that_end_between_waves(m, v, dtype):
+    """A row's end in the middle of a workgroup's columns: waves with fewer pieces than others, with one that is cut, or with none."""
+    say("logits", m, v, dtype)
+    x, tok = logits(m, v, dtype, 5), some_tokens(m, v, 6)
+    for top in (0, 9):
+        check_logprobs(x, tok, top, 1.3)
+    tv, ti = teacher_of(x, 30, 7, dtype)
+    check_distill(x, tv, ti, 1.3, torch.full((m,), 0.5, device="cuda"))
+    x[0, : v - 3] = NINF
+    x[1, 2:] = NINF
+    check_logprobs(x, tok, 9, 1.3)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("v", [40, 700, 5000, 33000, 140000])
 def test_equal_logits(v, dtype):
