@@ -132,10 +132,11 @@ __device__ __forceinline__ Piece<T> load_logits(const T* row, int c, int V) {
 }
 template <typename T>
 __device__ __forceinline__ void logit_values(const Piece<T>& p, float (&v)[CH]) {
-    T t[CH];
-    __builtin_memcpy(t, p.w, sizeof(t));
 #pragma unroll
-    for (int e = 0; e < CH; e++) v[e] = to_f(t[e]);
+    for (int e = 0; e < CH; e++) {   // (halves by shifts: taken from a copy as an array, fp16 stayed apart in two registers a word)
+        if constexpr (sizeof(T) == 2) v[e] = to_f(__builtin_bit_cast(T, (uint16_t)(p.w[e / 2] >> (e % 2 * 16))));
+        else v[e] = __uint_as_float(p.w[e]);
+    }
 }
 // A wave's pieces that are whole, and those that have any columns of the row: the others cost no arithmetic (10000 columns in a
 // workgroup's 16384: log probabilities of 4096 rows of bf16 42.3 -> 27.3 us).  left: columns from the workgroup's first to the row's end.
@@ -155,11 +156,13 @@ template <typename T, bool TINY>
 __device__ __forceinline__ void mask_logits(Piece<T>& p, int c, int V) {
     const Place<TINY> at(c, V);
     if (at.whole()) return;
-    T t[CH];
-    __builtin_memcpy(t, p.w, sizeof(t));
+    constexpr int BITS = 8 * sizeof(T), IN = 32 / BITS;   // elements in a word
+    const uint32_t mask = sizeof(T) == 4 ? kNegInf : (std::is_same_v<T, f16> ? 0xFC00u : 0xFF80u);
 #pragma unroll
-    for (int e = 0; e < CH; e++) t[e] = at.own(e) ? t[e] : from_f<T>(neg_inf());
-    __builtin_memcpy(p.w, t, sizeof(t));
+    for (int e = 0; e < CH; e++) {
+        const uint32_t mine = (uint32_t)(((uint64_t)1 << BITS) - 1) << (e % IN * BITS);
+        p.w[e / IN] = at.own(e) ? p.w[e / IN] : (p.w[e / IN] & ~mine) | mask << (e % IN * BITS);
+    }
 }
 template <typename T, bool TINY>
 __device__ __forceinline__ void store_logits(T* row, int c, int V, const float (&v)[CH], bool stream) {
