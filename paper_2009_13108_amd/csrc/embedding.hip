@@ -10,7 +10,7 @@
 //      write the table's zeros, which bound it where they are many (32000 x 4096 bf16, 262 MB: 44 us, 6.0 TB/s).
 //  (2) Eight or sixteen consecutive sorted rows at a time are read and added up (8192 x 4096 bf16: 18.6 us, 3.6 TB/s).  A token whose
 //      rows lie inside such a stretch gets its row at once; one that crosses its ends leaves partial sums in the workspace, and
-//  (3) those are joined in order (8.5 us, latency).  However often a token occurs, the work is split evenly.
+//  (3) those are joined in order (6.8 us, latency).  However often a token occurs, the work is split evenly.
 // Small batches are bound by the latency of the three launches.
 #include "linear.h"
 
@@ -21,7 +21,8 @@ namespace niti {
 
 namespace {
 
-// Tokens are compared all with all up to kRankMax (its time grows with their square: with 16384 of them sorting was faster).
+// Tokens are compared all with all up to kRankMax (the gradient of M x 256, added: 4096 18.1 us, by sorting 25.5; 8192 26.4 and 29.7;
+// 12000 31.6 and 33.9, 16384 38.8 and 35.7).
 constexpr int kRankMax = 8192;
 constexpr int kSortFew = 2048;    // tokens that a workgroup sorts, in batches of up to kMergeMax, all of whose keys the next launch has in LDS
 constexpr int kMergeMax = 32768;
@@ -331,12 +332,11 @@ __global__ __launch_bounds__(1024) void token_merge_few_kernel(EmbBwdArgs a) {
 
 constexpr int kSumThreads = 256, kSumCols = kSumThreads * CH;
 
-// A sum into the table's row of token k, on top of old where there is something to add to.
-template <typename TG, int N>
-__device__ __forceinline__ void put_sum(const EmbBwdArgs& a, int64_t k, int c, const float (&sum)[N], float (&old)[N]) {
+// A sum on top of old, where there is something to add to.
+template <int N>
+__device__ __forceinline__ void sum_on(const EmbBwdArgs& a, const float (&sum)[N], float (&old)[N]) {
 #pragma unroll
     for (int e = 0; e < N; e++) old[e] = a.accumulate ? __builtin_fmaf(a.alpha, sum[e], old[e]) : a.alpha * sum[e];
-    store_first((TG*)a.dtable + k * a.ldt + c, (int)(a.D - c), old);
 }
 
 // (2) A stretch of sorted rows, 2048 columns.  KIND: the number of columns is a multiple of 8 (2), is at least 8 (1), or neither (0).
@@ -397,7 +397,8 @@ __global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, in
                     float old[CH] = {};
                     if constexpr (ADD && KIND > 0) piece_values<TG, KIND == 2>(o[j], c, D, old);
                     else if (ADD) load_some((const TG*)a.dtable + k * a.ldt + c, D - c, old);
-                    put_sum<TG>(a, k, c, sum, old);
+                    sum_on(a, sum, old);
+                    store_first((TG*)a.dtable + k * a.ldt + c, D - c, old);
                 }
             }
 #pragma unroll
@@ -409,9 +410,12 @@ __global__ __launch_bounds__(kSumThreads) void token_sum_kernel(EmbBwdArgs a, in
 }
 
 // (3) The token that crosses the end of a stretch that it begins in: its partial sums in order.  Threads that rows of fewer than 1024
-// columns leave over take every `groups`-th partial sum, and the groups' sums are added in order.
+// columns leave over take every `groups`-th partial sum, and the groups' sums are added in order.  No load is in a branch that part of a
+// wave takes, where it would be waited for: the four columns at a row's end are read, and added up, from four before it on, and only
+// those of this thread are stored (NARROW: of fewer than four, one by one).  The first two partial sums, all that most tokens have,
+// are on their way with the tokens (8192 x 4096: 8.3 -> 6.8 us; the three launches for 4111 x 1111 added 25.7 -> 23.5).
 constexpr int kJoinCols = 1024;
-template <typename TG, bool GROUPS>
+template <typename TG, bool GROUPS, bool NARROW>
 __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slices, int of_groups) {
     __shared__ float sums[GROUPS ? 256 : 1][4];
     const int groups = GROUPS ? of_groups : 1;
@@ -420,12 +424,27 @@ __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slice
     const int c = (int)(blockIdx.x % (uint32_t)slices) * kJoinCols + (int)threadIdx.x % per * 4;
     const int64_t i0 = s * a.run, end = i0 + a.run;   // (the last stretch crosses nothing)
     if (end >= a.M) return;
+    const int D = (int)a.D, from = NARROW ? c : min(c, D - 4);
+    auto load = [&](const auto* row, float (&v)[4]) {
+        if constexpr (NARROW) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = to_f(row[min(c + e, D - 1)]);
+        } else {
+            load_n(row + from, v);
+        }
+    };
+    const int64_t stretches = (a.M + a.run - 1) / a.run;
+    float sum[4], next[4];
+    load(a.part + (2 * s + 1) * a.D, sum);
+    load(a.part + 2 * min(s + 1 + group, stretches - 1) * a.D, next);
     const int lane = threadIdx.x & 63;
     // stretches after this one that the token fills to their ends, 64 at a time: the next stretch's first token, and the one before it
     auto ends = [&](int64_t at, int i) { return a.key[min((at + lane + 1) * a.run - 1 + i, a.M - 1)]; };
     int32_t x = ends(s + 1, 0), y = ends(s + 1, 1);
     const int32_t k = a.key[end], own = a.key[end - 1], left_of = a.key[max(i0 - 1, (int64_t)0)];
     if (own != k || k >= a.V || (i0 > 0 && left_of == k)) return;   // (the same for all threads)
+    float old[4] = {};
+    if (a.accumulate) load((const TG*)a.dtable + k * a.ldt, old);
     int64_t last = s + 1;
     for (;;) {
         const uint64_t on = __ballot((last + lane + 1) * a.run < a.M && x == k && y == k);
@@ -434,40 +453,18 @@ __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slice
         if (n) break;
         x = ends(last, 0), y = ends(last, 1);
     }
-    if constexpr (!GROUPS) {
-        if (c >= a.D) return;
-        const int left = (int)(a.D - c);
-        float sum[4], old[4] = {};
-        load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
-        if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
-        for (int64_t p = s + 1; p <= last; p += 16) {
-            float v[16][4];
+    const bool mine = s + 1 + group <= last;
 #pragma unroll
-            for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i, last) * a.D + c, left, v[i]);
+    for (int e = 0; e < 4; e++) sum[e] = (group == 0 ? sum[e] : 0.f) + (mine ? next[e] : 0.f);
+    for (int64_t p0 = s + 1 + groups; p0 <= last; p0 += 16 * groups) {   // (the same for all threads)
+        const int64_t p = p0 + group;
+        float v[16][4];
 #pragma unroll
-            for (int i = 0; i < 16; i++)
+        for (int i = 0; i < 16; i++) load(a.part + 2 * min(p + i * groups, last) * a.D, v[i]);
 #pragma unroll
-                for (int e = 0; e < 4; e++) sum[e] += p + i <= last ? v[i][e] : 0.f;
-        }
-        put_sum<TG>(a, k, c, sum, old);
-        return;
-    }
-    const int left = (int)(a.D - c);
-    float sum[4] = {}, old[4] = {};
-    if (left > 0) {
-        if (group == 0) {
-            load_some(a.part + (2 * s + 1) * a.D + c, left, sum);
-            if (a.accumulate) load_some((const TG*)a.dtable + k * a.ldt + c, left, old);
-        }
-        for (int64_t p = s + 1 + group; p <= last; p += 16 * groups) {
-            float v[16][4];
+        for (int i = 0; i < 16; i++)
 #pragma unroll
-            for (int i = 0; i < 16; i++) load_some(a.part + 2 * min(p + i * groups, last) * a.D + c, left, v[i]);
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) sum[e] += p + i * groups <= last ? v[i][e] : 0.f;
-        }
+            for (int e = 0; e < 4; e++) sum[e] += p + i * groups <= last ? v[i][e] : 0.f;
     }
     if constexpr (GROUPS) {
 #pragma unroll
@@ -477,7 +474,16 @@ __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slice
 #pragma unroll
             for (int e = 0; e < 4; e++) sum[e] += sums[g * per + threadIdx.x][e];
     }
-    if (left > 0 && group == 0) put_sum<TG>(a, k, c, sum, old);
+    if (c >= D || group != 0) return;
+    sum_on(a, sum, old);
+    TG* row = (TG*)a.dtable + k * a.ldt + from;
+    if (!NARROW && from == c) {
+        store_whole(row, old);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (from + e >= c && from + e < D) row[e] = from_f<TG>(old[e]);
+    }
 }
 
 // ---------------------------------------------------------------- launches
@@ -499,7 +505,7 @@ EmbSpace emb_space(int64_t M, int64_t D) {
     return s;
 }
 
-// Short stretches where long ones leave CUs without work.
+// Short stretches where long ones leave CUs without work (1000 x 1024 13.4 us, with stretches of 16 16.6; 16384 x 4096 91, of 8 102).
 int run_of(int64_t M, int64_t D) { return ceil_div(M, 16) * ceil_div(D, kSumCols) < 1024 ? 8 : 16; }
 
 int sort_passes(int64_t V) {   // bytes of the largest key, V
@@ -583,10 +589,13 @@ hipError_t run_join(const EmbBwdArgs& a, hipStream_t stream) {
     const int slices = (int)ceil_div(a.D, kJoinCols);
     int groups = 1;
     while (groups < 16 && a.D * 2 * groups <= kJoinCols) groups *= 2;
-    if (groups > 1)
-        hipLaunchKernelGGL((token_join_kernel<TG, true>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices, groups);
-    else
-        hipLaunchKernelGGL((token_join_kernel<TG, false>), dim3((unsigned)(runs * slices)), dim3(256), 0, stream, a, slices, 1);
+    auto launch = [&](auto in_groups, auto narrow) {
+        hipLaunchKernelGGL((token_join_kernel<TG, decltype(in_groups)::value, decltype(narrow)::value>), dim3((unsigned)(runs * slices)),
+                           dim3(256), 0, stream, a, slices, groups);
+    };
+    if (a.D < 4) launch(std::true_type(), std::true_type());
+    else if (groups > 1) launch(std::true_type(), std::false_type());
+    else launch(std::false_type(), std::false_type());
     return hipGetLastError();
 }
 
