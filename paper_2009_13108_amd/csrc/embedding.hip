@@ -8,7 +8,7 @@
 //      took 16); of more, workgroups sort 2048 each in their LDS (radix sort, stable; 16384 each in batches of more than 32768), and a
 //      second launch places a chunk's tokens by binary searches in the other chunks.  Meanwhile the first launch's other workgroups
 //      write the table's zeros, which bound it where they are many (32000 x 4096 bf16, 262 MB: 44 us, 6.0 TB/s).
-//  (2) Eight or sixteen consecutive sorted rows at a time are read and added up (8192 x 4096 bf16: 18.6 us, 3.6 TB/s).  A token whose
+//  (2) Eight or sixteen consecutive sorted rows at a time are read and added up (8192 x 4096 bf16: 18.5 us, 3.6 TB/s).  A token whose
 //      rows lie inside such a stretch gets its row at once; one that crosses its ends leaves partial sums in the workspace, and
 //  (3) those are joined in order (6.8 us, latency).  However often a token occurs, the work is split evenly.
 // Small batches are bound by the latency of the three launches.

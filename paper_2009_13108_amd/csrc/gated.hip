@@ -6,8 +6,8 @@
 // The kernels are those of the plain product with weight rows paired (see linear_tiles.h): the sums are
 // exact in int32, a is read once for both projections, and z reaches memory only where it is asked for.
 //
-// Measured, bf16 with SiLU (F x K): 1 x 9216 x 4096 14.3 us, 5.3 TB/s of weights; 4096 x 8192 x 4096 with z 285 to 291 us, 1.9
-// POPS, bound by power and by the 200 MB that it stores (without z 254); 1000 x 1500 x 1111 in 32 bits 14.7, of which 3 go to
+// Measured, bf16 with SiLU (F x K): 1 x 9216 x 4096 14.3 us, 5.3 TB/s of weights; 4096 x 8192 x 4096 with z 280 to 293 us, 1.9
+// POPS, bound by power and by the 200 MB that it stores (without z 244, 2.25 POPS); 1000 x 1500 x 1111 in 32 bits 14.7, of which 3 to 5 go to
 // copying the rows to whole pieces.
 #include "linear_tiles.h"
 

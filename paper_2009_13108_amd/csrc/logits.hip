@@ -9,7 +9,7 @@
 // was loaded, the maximum is found first and the sums next, so that every element costs one exponential; longer rows, and few of
 // them, are split over workgroups whose parts a second launch joins.  The fused gradient writes from the same registers.
 // What bounds them: distillation and its gradient memory (4096 x 32000 bf16 with the gradient, 524 MB, 99 us: 5.3 TB/s); log
-// probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 62 us, 4.2 TB/s: some ten instructions an element, of which the
+// probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 62 us, 4.2 TB/s: fourteen instructions an element, of which the
 // exponential takes four issue slots) between the barriers of two workgroups a CU; of 32 bits memory, in parts (77 x 128001 14.5 us and
 // 5 for the join); one row latency (1 x 32000 7.5 us).  Workgroups that go on to another row, its loads out while the last one's results
 // are joined, spilled registers and took 101 us for 69.
