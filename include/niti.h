@@ -501,7 +501,8 @@ niti_status niti_embedding_bwd(const void *dy, int64_t lddy, int type, const int
  * log probability and lse minus infinity, entropy 0, and its first columns as
  * alternatives; a row with a NaN or plus infinity is NaN throughout, its
  * alternatives' columns -1.  Workspace: niti_workspace_bytes(
- * NITI_OP_TOKEN_LOGPROBS, NULL, M, V, top), 0 for most sizes. */
+ * NITI_OP_TOKEN_LOGPROBS, NULL, M, V, top), 0 for most sizes; it does for
+ * fewer rows as well. */
 niti_status niti_token_logprobs(const void *x, int64_t ldx, const int32_t *tokens, float *logp, float *lse,
                                 float *entropy, float *top_logp, int32_t *top_idx, int64_t M, int64_t V, int64_t top,
                                 float scale, int type, void *ws, size_t ws_bytes, void *stream);

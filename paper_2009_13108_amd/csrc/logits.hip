@@ -24,6 +24,7 @@
 
 #include <math.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <type_traits>
 
@@ -907,12 +908,13 @@ inline Plan short_row(int64_t V) {
 // 17.0, 16.1, 1000 33.2, 28.5; 60000 columns, 300 rows 19.8, 18.4;  32 bits, 32000 columns, 300 rows 16.3, 16.9, 1000 33.2, 29.3, 4000 125,
 // 104; 60000 columns, 60 rows 10.3, 12.4, 300 23.7, 22.5.  Which parts, of 4096, 8192 and 16384: 100000 columns in 16 bits, 1 row
 // 9.4, 10.5, 10.5, 60 12.6, 12.6, 12.4, 1000 79, 56, 56; in 32 bits, 60 rows 14.0, 14.5, 14.2, 300 29.8, 27.4, 27.4, 1000 85, 74, 75.
+constexpr int64_t few_rows(int type) { return type != NITI_F32 ? 48 : 96; }
 Plan logprobs_plan(int64_t M, int64_t V, int type) {
     if (V <= 16384) return short_row(V);
     const bool half = type != NITI_F32;
     if (V <= 32768 && (half || M <= 512)) return Plan{k32768w, 1};
     if (V > 32768 && V <= 65536 && M <= 256) return Plan{k65536, 1};
-    if (M <= (half ? 48 : 96)) return in_parts(V, {k4096, k8192, k16384, k32768w, k65536});
+    if (M <= few_rows(type)) return in_parts(V, {k4096, k8192, k16384, k32768w, k65536});
     return half ? in_parts(V, {k16384, k32768w, k65536}) : in_parts(V, {k8192, k16384, k32768w, k65536});
 }
 
@@ -1062,10 +1064,13 @@ inline bool fine_scale(float s) { return s > 0.f && s < INFINITY; }
 }  // namespace
 
 // For either type's plan: the caller's sizes do not say which.
+// (Few rows may be in more parts than many, and take more: there is room for any number of rows up to M.)
 size_t logprobs_workspace(int64_t M, int64_t V, int64_t top) {
     if (M < 1 || V < 1 || top < 0 || top > kTopMax || top > V || M >= kMaxDim || V >= kMaxLd) return 0;
-    const size_t wide = log_space(M, logprobs_plan(M, V, NITI_F32).parts, top), half = log_space(M, logprobs_plan(M, V, NITI_BF16).parts, top);
-    return wide > half ? wide : half;
+    size_t need = 0;
+    for (int type : {NITI_F32, NITI_BF16})
+        for (int64_t m : {M, std::min(M, few_rows(type))}) need = std::max(need, log_space(m, logprobs_plan(m, V, type).parts, top));
+    return need;
 }
 size_t distill_workspace(int64_t M, int64_t V) {
     if (M < 1 || V < 1 || M >= kMaxDim || V >= kMaxLd) return 0;

@@ -143,3 +143,18 @@ def test_binding_takes_device_tensors_only():
                  lambda: niti.distill_fwd(x, x, t.view(2, 1), s), lambda: niti.distill_bwd(x, x, t.view(2, 1), s, s, x)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("v", [30000, 40000, 65537, 100000, 131073, 262145, 1 << 20])
+def test_workspace_of_many_rows_does_for_fewer(v):
+    """A batch's workspace, sized once, serves the smaller last batch too."""
+    rows = sorted(set(range(1, 200)) | {255, 256, 257, 511, 512, 513, 1000, 4096})
+    for op, top in ((niti.OP_TOKEN_LOGPROBS, 0), (niti.OP_TOKEN_LOGPROBS, 20), (niti.OP_DISTILL_FWD, 0)):
+        need = [niti.workspace_bytes(op, None, m, v, top) for m in rows]
+        assert need == sorted(need)
+
+
+@pytest.mark.parametrize("d", [64, 1000, 4096])
+def test_workspace_of_many_tokens_does_for_fewer(d):
+    need = [niti.workspace_bytes(niti.OP_EMBEDDING_BWD, None, m, 32000, d) for m in (1, 100, 4096, 8191, 8192, 8193, 16384, 32768, 32769, 100000)]
+    assert need == sorted(need)
