@@ -419,9 +419,9 @@ struct Select {
     }
     // Number of candidates, among them the top ones; tops: the pieces' largest.
     __device__ __forceinline__ int run(Piece<T> (&p)[VPT], const float (&tops)[VPT], float tau, int top) {
-        int count;
+        int count, pass = 0;
 #pragma unroll 1
-        for (int pass = 0;; pass++) {   // all that reach the bound; if too many, those above it; if too many, those above the top-th
+        for (;; pass++) {   // all that reach the bound; if too many, those above it; if too many, those above the top-th
             forget_values(p);                // (and nothing that every pass needs is formed, and kept, before the first)
             asm volatile("" : "+s"(V));
             collect(p, tops, tau, pass == 0);
@@ -433,7 +433,8 @@ struct Select {
             if (threadIdx.x == 0) *n = 0;
             __syncthreads();
         }
-        if (count < top) {
+        // (the first pass has the bound's equals already: fewer than top are all the numbers that there are)
+        if (pass > 0 && count < top) {
             count += equals(p, tau, count, top - count);
             __syncthreads();
         }
