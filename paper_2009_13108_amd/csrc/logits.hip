@@ -585,7 +585,8 @@ struct DistArgs {
     int64_t ldx, ldt, ldi, lddx, M, V;
     int32_t top, t_type, parts, g_step, stream;
     float scale, c2;
-    Stat* stat;
+    Stat* stat;            // [M][stats] of split rows' parts; the first then the whole row's
+    int64_t stats;
 };
 
 // The teacher's distribution over its list: KPT entries a thread.
@@ -730,7 +731,7 @@ __global__ __launch_bounds__(64 * NW, two_a_cu<T>(NW, VPT)) void distill_kernel(
     st.s = sum * __builtin_amdgcn_exp2f(-base.r);
     st.w = 0.f;
     if (a.parts > 1) {
-        if (t == 0) a.stat[m * a.parts + part] = st;
+        if (t == 0) a.stat[m * a.stats + part] = st;
         return;
     }
     const float logs = st.log();
@@ -785,7 +786,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistArgs a) {
     T z[1];
     teach.load(a, m);
     teach.gather(a, row, 0, (int)a.V, z);
-    const Stat st = join_stats(a.stat + m * a.parts, a.parts, a.c2);
+    const Stat st = join_stats(a.stat + m * a.stats, a.parts, a.c2);
     const float logs = st.log();
     const float wt = wave_max(teach.top(a));
     if ((t & 63) == 0) red_t[wave] = wt;
@@ -799,14 +800,16 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistArgs a) {
     __syncthreads();
     const float loss = join_sum<4>(red_l);
     if (t == 0) {
+        a.stat[m * a.stats] = st;   // (all waves have joined the parts' before the barriers)
         a.loss[m] = loss;
         if (a.lse) a.lse[m] = st.lse(a.scale, logs);
     }
 }
 
-// The gradient from lse: a part of a row each.  The whole part is loaded before any of it is stored, and so are its
+// The gradient from lse, or from the maxima and sums that the loss has left (JOINED): an lse is off by |lse| 2^-24, and so
+// are shares of the row formed from it, relative, which those from the sum are not.  A part of a row each.  The whole part is loaded before any of it is stored, and so are its
 // listed columns: dx may be x.  (What a row's last piece reads of the part before counts for nothing.)
-template <typename T, int NW, int VPT, bool TINY>
+template <typename T, int NW, int VPT, bool TINY, bool JOINED>
 __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     constexpr int NT = 64 * NW, LEN = NT * VPT * CH, KPT = list_per_thread(NW);
     __shared__ float red_t[NW], red_u[NW];
@@ -818,7 +821,8 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     const T* row = (const T*)a.x + m * a.ldx;
     Teacher<NW, KPT> teach;
     teach.load(a, m);
-    const float lse = a.lse_in[m], g1 = a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
+    const Stat st = JOINED ? a.stat[m * a.stats] : Stat{0.f, 1.f, 0.f};
+    const float lse = JOINED ? 0.f : a.lse_in[m], g1 = a.dloss ? a.dloss[a.g_step ? m : 0] : 1.f;
     const Live<NW, VPT> live(V - c0, wave);
     Piece<T> p[VPT];
 #pragma unroll
@@ -835,7 +839,10 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     teach.put(a, cols, probs);
     const float g = g1 * a.scale * teach.unit;
     const bool none = lse == neg_inf();   // a row of minus infinities: q = 0
+    const Base base(st.m, a.c2);
+    const float inv = st.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(-base.r) / st.s;
     auto share = [&](float x) {
+        if constexpr (JOINED) return base.power(x) * inv;
         const float d = __builtin_fmaf(x, a.scale, -lse);
         return none ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
     };
@@ -986,13 +993,14 @@ void next_slab(DistArgs& a, int64_t slab) {
     if (a.lse_in) a.lse_in += slab;
     if (a.dloss && a.g_step) a.dloss += slab;
     if (a.dx) a.dx = (T*)a.dx + slab * a.lddx;
+    if (a.stat) a.stat += slab * a.stats;
 }
 
 // Whether a gradient goes past the caches: more than the eight L2 hold would only push out what is still to be read (4096 x 32000 in
 // 16 bits, with the loss 119 -> 102 us, alone 112 -> 89).
 inline int32_t streams(int64_t M, int64_t V, size_t size) { return M * V * (int64_t)size > ((int64_t)32 << 20); }
 
-template <typename T>
+template <typename T, bool JOINED>
 hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
     // 4096 columns a workgroup where rows are longer than 512
     const int shape = a.V <= 512 ? k512 : k4096;
@@ -1003,13 +1011,13 @@ hipError_t run_distill_bwd(DistArgs a, hipStream_t stream) {
         a.M = M - m0 < slab ? M - m0 : slab;
         const hipError_t e = by_shape(shape, [&](auto nw, auto vpt) {
             constexpr int NW = decltype(nw)::value, VPT = decltype(vpt)::value;
-            if constexpr (VPT == 1)
+            if constexpr (VPT == 1 && !JOINED)
                 if (a.V < CH) {
-                    hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, true>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
+                    hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, true, false>), dim3((unsigned)a.M), dim3(64 * NW), 0, stream, a);
                     return hipGetLastError();
                 }
-            if constexpr ((NW == 1 && VPT == 1) || (NW == 4 && VPT == 2))
-                hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, false>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
+            if constexpr ((NW == 1 && VPT == 1 && !JOINED) || (NW == 4 && VPT == 2))   // (split rows are long ones)
+                hipLaunchKernelGGL((distill_bwd_kernel<T, NW, VPT, false, JOINED>), dim3((unsigned)(a.M * a.parts)), dim3(64 * NW), 0, stream, a);
             return hipGetLastError();
         });
         if (e != hipSuccess) return e;
@@ -1022,14 +1030,11 @@ template <typename T>
 hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t stream) {
     a.parts = plan.parts;
     a.stream = streams(a.M, a.V, sizeof(T));
+    a.stats = plan.parts;
+    if (plan.parts > 1) a.stat = (Stat*)ws;
     const DistArgs whole = a;
     const int64_t M = a.M, slab = kSlab / plan.parts;
     const bool grad = a.dx && plan.parts == 1;
-    if (plan.parts > 1) {
-        a.stat = (Stat*)ws;
-        if (a.dx && !a.lse) a.lse = (float*)(ws + up256((size_t)M * a.parts * sizeof(Stat)));
-    }
-    const float* lse = a.lse;
     for (int64_t m0 = 0; m0 < M; m0 += slab) {
         a.M = M - m0 < slab ? M - m0 : slab;
         hipError_t e = by_shape(plan.shape, [&](auto nw, auto vpt) {
@@ -1055,9 +1060,7 @@ hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t strea
         next_slab<T>(a, slab);
     }
     if (!whole.dx || grad) return hipSuccess;
-    DistArgs b = whole;
-    b.lse_in = lse;
-    return run_distill_bwd<T>(b, stream);
+    return run_distill_bwd<T, true>(whole, stream);
 }
 
 inline bool fine_scale(float s) { return s > 0.f && s < INFINITY; }
@@ -1077,7 +1080,7 @@ size_t distill_workspace(int64_t M, int64_t V) {
     if (M < 1 || V < 1 || M >= kMaxDim || V >= kMaxLd) return 0;
     const int wide = distill_plan(M, V, NITI_F32).parts, half = distill_plan(M, V, NITI_BF16).parts;
     const int parts = wide > half ? wide : half;
-    return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) + up256((size_t)M * 4) : 0;
+    return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) : 0;
 }
 
 }  // namespace niti
@@ -1149,7 +1152,7 @@ niti_status niti_distill_bwd(const void* x, int64_t ldx, const void* t_val, int6
     a.ldi = M > 1 ? ldi : top, a.lse_in = lse, a.dloss = dloss, a.g_step = dloss_n == 1 ? 0 : 1;
     a.dx = dx, a.lddx = M > 1 ? lddx : V, a.M = M, a.V = V, a.top = (int32_t)top;
     a.scale = scale, a.c2 = (float)((double)scale * 1.44269504088896340736);
-    return by_type(type, [&](auto t) { return run_distill_bwd<decltype(t)>(a, (hipStream_t)stream); }) == hipSuccess
+    return by_type(type, [&](auto t) { return run_distill_bwd<decltype(t), false>(a, (hipStream_t)stream); }) == hipSuccess
                ? NITI_OK : NITI_ERR_HIP;
 }
 
