@@ -489,7 +489,7 @@ niti_status niti_embedding_bwd(const void *dy, int64_t lddy, int type, const int
                                int accumulate, void *ws, size_t ws_bytes, void *stream);
 
 /* Log probabilities of logits x [M][V] (softmax of scale * x along the rows,
- * 0 < scale < inf: the reciprocal of a temperature), each output optional:
+ * 0 < scale <= 2^127: the reciprocal of a temperature), each output optional:
  *   logp      [M] of tokens[m] (int32; given exactly where logp is); 0 for a
  *             token outside 0..V-1;
  *   lse       [M] log sum exp(scale * x);
@@ -508,7 +508,7 @@ niti_status niti_token_logprobs(const void *x, int64_t ldx, const int32_t *token
                                 float scale, int type, void *ws, size_t ws_bytes, void *stream);
 
 /* Divergence of a row's softmax q of scale * x [M][V] from a teacher's
- * distribution p, the softmax of scale * t_val over the row's list of `top`
+ * distribution p, the softmax of scale * t_val (0 < scale <= 2^127) over the row's list of `top`
  * columns t_idx (int32) with their logits t_val (t_type), both [M][top]:
  *     loss[m] = sum_j p_j (log p_j - log q[t_idx_j]).
  * top is 1..256.  A column outside 0..V-1 is no part of the list (lists of

@@ -1063,7 +1063,8 @@ hipError_t run_distill(DistArgs a, const Plan& plan, char* ws, hipStream_t strea
     return run_distill_bwd<T, true>(whole, stream);
 }
 
-inline bool fine_scale(float s) { return s > 0.f && s < INFINITY; }
+// (scale log2 e is finite up to here: an infinite one times a difference of 0 is a NaN)
+inline bool fine_scale(float s) { return s > 0.f && s <= 0x1p127f; }
 
 }  // namespace
 
