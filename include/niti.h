@@ -527,7 +527,10 @@ niti_status niti_distill_fwd(const void *x, int64_t ldx, const void *t_val, int6
                              int type, void *ws, size_t ws_bytes, void *stream);
 
 /* The gradient alone, from the forward call's lse, for a dloss that is known
- * later.  dx may be x. */
+ * later: q_v = exp(scale * x_v - lse) is off by |lse| 2^-24 of its value, which
+ * the gradient in the forward call is not.  Where lse has no digits left that tell
+ * (a row of the type's lowest value throughout), q is a number from 0 to 1, and 0
+ * where scale * x overflows.  dx may be x. */
 niti_status niti_distill_bwd(const void *x, int64_t ldx, const void *t_val, int64_t ldt, int t_type,
                              const int32_t *t_idx, int64_t ldi, const float *lse, const float *dloss, int64_t dloss_n,
                              void *dx, int64_t lddx, int64_t M, int64_t V, int64_t top, float scale, int type,

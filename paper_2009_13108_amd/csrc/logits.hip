@@ -843,8 +843,10 @@ __global__ __launch_bounds__(64 * NW) void distill_bwd_kernel(DistArgs a) {
     const float inv = st.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(-base.r) / st.s;
     auto share = [&](float x) {
         if constexpr (JOINED) return base.power(x) * inv;
+        // A share above 1 is lse's rounding: by little it goes as it is; where lse has no digits of that size (a row of the type's
+        // lowest value) the difference may be any number, and counts for 0.  (A NaN stays one.)
         const float d = __builtin_fmaf(x, a.scale, -lse);
-        return none ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
+        return none ? 0.f : __builtin_amdgcn_exp2f((d > 0x1p-7f ? 0.f : d) * kLog2e);
     };
     T* dx = (T*)a.dx + m * a.lddx;
     // (every wave's loads of the row come before the barriers above: dx may be x)
