@@ -14,7 +14,6 @@
 // Small batches are bound by the latency of the three launches.
 #include "linear.h"
 
-#include <atomic>
 #include <type_traits>
 
 namespace niti {
@@ -94,7 +93,7 @@ struct EmbBwdArgs {
     int32_t run;                  // sorted rows of a stretch
     int32_t sorters;              // workgroups that sort, ahead of those that write zeros
     int32_t *order, *key;         // [M]: rows by token, and their tokens (V for those outside the table)
-    int32_t *order1, *key1;       // the same of each chunk, where there are several
+    int32_t *order1, *key1;       // the same of each chunk that is sorted
     int32_t chunk;                // tokens of one
     float* part;                  // [stretches][2][D]
 };
@@ -263,11 +262,10 @@ __global__ __launch_bounds__(kSortThreads) void token_sort_kernel(EmbBwdArgs a) 
         uint16_t* x = src;
         src = dst, dst = x;
     }
-    int32_t *order = a.order1 ? a.order1 : a.order, *keys = a.key1 ? a.key1 : a.key;
     for (int i = t; i < n; i += kSortThreads) {
         const int p = src[i];
-        order[base + i] = (int32_t)(base + p);
-        keys[base + i] = (int32_t)key[p];
+        a.order1[base + i] = (int32_t)(base + p);
+        a.key1[base + i] = (int32_t)key[p];
     }
 }
 
@@ -488,7 +486,6 @@ __global__ __launch_bounds__(256) void token_join_kernel(EmbBwdArgs a, int slice
 
 // ---------------------------------------------------------------- launches
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 struct EmbSpace {
     int64_t order, key, order1, key1, part, total;
@@ -515,20 +512,6 @@ int sort_passes(int64_t V) {   // bytes of the largest key, V
 }
 
 constexpr int kSortLds = kSortMax * 8 + kSortWaves * kBins * 2 + 64;
-
-// Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
-template <auto kernel, int LDS>
-hipError_t allow_lds() {
-    static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
-    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-    return e;
-}
 
 template <typename TG>
 hipError_t run_sort(EmbBwdArgs& a, hipStream_t stream) {

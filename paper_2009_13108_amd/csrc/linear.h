@@ -4,6 +4,8 @@
 
 #include "scaled.h"
 
+#include <atomic>
+
 namespace niti {
 
 struct LinArgs {
@@ -37,5 +39,22 @@ size_t gated_bwd_workspace(int64_t M, int64_t F, int64_t K);
 size_t embedding_bwd_workspace(int64_t M, int64_t V, int64_t D);
 size_t logprobs_workspace(int64_t M, int64_t V, int64_t top);
 size_t distill_workspace(int64_t M, int64_t V);
+
+// Arrays of a workspace begin at multiples of 256 bytes.
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
+template <auto kernel, int LDS>
+inline hipError_t allow_lds() {
+    static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 }  // namespace niti

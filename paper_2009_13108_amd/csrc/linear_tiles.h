@@ -12,7 +12,6 @@
 
 #include <math.h>
 
-#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -871,20 +870,6 @@ template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS>
 __global__ __launch_bounds__(64 * WGM * WGN, BM * BN / (WGM * WGN) <= 8192 ? 2 : 1) void linear_ring_pair_kernel(LinPair P) {
     const int i = (int)blockIdx.x < P.blocks ? 0 : 1;
     ring_tile<T, BM, BN, NS, WGM, WGN, KS>(P.a[i], P.tiles_n[i], (int)blockIdx.x - i * P.blocks);
-}
-
-// Once for each kernel and device, from any thread: it may have more than 64 KiB of LDS.
-template <auto kernel, int LDS>
-hipError_t allow_lds() {
-    static std::atomic<uint64_t> done{0};   // a bit for each of the first 64 devices
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
-    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-    return e;
 }
 
 template <typename T, int BM, int BN, int NS, int WGM, int WGN, int KS, bool G = false>

@@ -942,8 +942,6 @@ Plan distill_plan(int64_t M, int64_t V, int type) {
 // A launch holds fewer than 2^32 threads: very many rows go in slabs.
 constexpr int64_t kSlab = (int64_t)1 << 21;
 
-inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-
 size_t log_space(int64_t M, int parts, int64_t top) {
     return parts > 1 ? up256((size_t)M * parts * sizeof(Stat)) + up256((size_t)M * parts * (size_t)top * 8) : 0;
 }
