@@ -848,6 +848,8 @@ def gated_bwd(dy, z, a, b, s_a, s_b, ws, act=ACT_SILU, da=None, db=None, dbias=N
 # ------------------------------------------------------------------ tokens and logits
 def _given(t, what):
     """An operand that a call cannot go without."""
+    if _Tensor is None:
+        _torch()
     if not isinstance(t, _Tensor):
         raise TypeError("%s must be a device tensor" % what)
     return t
