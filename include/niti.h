@@ -508,13 +508,15 @@ niti_status niti_token_logprobs(const void *x, int64_t ldx, const int32_t *token
                                 float scale, int type, void *ws, size_t ws_bytes, void *stream);
 
 /* Divergence of a row's softmax q of scale * x [M][V] from a teacher's
- * distribution p, the softmax of scale * t_val (0 < scale <= 2^127) over the row's list of `top`
- * columns t_idx (int32) with their logits t_val (t_type), both [M][top]:
+ * distribution p, the softmax of scale * t_val (0 < scale <= 2^127) over the
+ * row's list of `top` columns t_idx (int32) with their logits t_val (t_type),
+ * both [M][top]:
  *     loss[m] = sum_j p_j (log p_j - log q[t_idx_j]).
  * top is 1..256.  A column outside 0..V-1 is no part of the list (lists of
  * different lengths are filled up with -1); one that is listed twice counts
- * twice.  An empty list, or one of minus infinities, has loss 0 and gradient 0.  lse [M],
- * optional, is kept for the backward pass.  dx, optional, receives the
+ * twice; one whose exponential is below 2^-126 of the list's largest counts as
+ * none.  An empty list, or one of minus infinities, has loss 0 and gradient 0.
+ * lse [M], optional, is kept for the backward pass.  dx, optional, receives the
  * gradient in the same pass,
  *     dx[m][v] = dloss[m] * scale * (q_v - sum of the p_j with t_idx_j = v),
  * with dloss float [M], or one for all (dloss_n = 1), or NULL for 1; dx may be

@@ -23,8 +23,9 @@
 // Measured, 2048 x 4096 x 4096 bf16 with SiLU: 13.7, 5.0, 24.8 (96 MB, 3.9 TB/s), 40.9 and
 // 37.9 us (1.7 and 1.8 POPS), 109 to 117 together: the products' tiles make one and two rounds of the
 // CUs, steps 1 and 3 are bound by memory with the activation's slope on top.  Gated, 2048 x 4096 (F) x 4096: 19 to 21, 5, 39, 74
-// and 70 us, 210 together (step 1 by the vector units: an activation, its slope and two products an element; step 3 stores 76 MB of
-// codes and transposes, and 17 of registers that two workgroups a CU do not hold; one workgroup a CU with all of them took 56).
+// and 70 us, 205 to 210 together (step 1 by the vector units: an activation, its slope and two products an element; step 3 stores 76 MB of
+// codes and transposes, and 17 of registers that two workgroups a CU do not hold; one workgroup a CU with all of them took 56); fp16
+// 207; 32 bits 261, of which the codes 62 to 70.  Spilled are 16 registers in bf16, 21 in fp16 and 82 in 32 bits, where one workgroup a CU was not timed.
 #include <type_traits>
 
 #include "linear.h"

@@ -7,10 +7,12 @@
 //   dx_v = dloss scale (exp(scale u_v) / S - sum of the p_j of v).
 // A row is read once: it stays in the registers of one workgroup (up to 64K columns, in distillation 128K of 16 bits; the plans below) as it
 // was loaded, the maximum is found first and the sums next, so that every element costs one exponential; longer rows, and few of
-// them, are split over workgroups whose parts a second launch joins.  The fused gradient writes from the same registers.
+// them, are split over workgroups whose parts a second launch joins.  The fused gradient writes from the same registers; that of split rows reads
+// them again, and takes the joined maximum and sum.  Powers below 2^-126 are 0, as the hardware gives them.
 // What bounds them: distillation and its gradient memory (4096 x 32000 bf16 with the gradient, 524 MB, 99 us: 5.3 TB/s); log
 // probabilities of 16 bits the vector units (4096 x 32000, 262 MB, 62 us, 4.2 TB/s: fourteen instructions an element, of which the
-// exponential takes four issue slots) between the barriers of two workgroups a CU; of 32 bits memory, in parts (77 x 128001 14.5 us and
+// exponential takes four issue slots) between the barriers of two workgroups a CU, which is what narrower rows from 16385 columns on have too
+// (4000 x 20000 54 us for 30 of memory; 4096 x 10000, eight waves, 27 for 15.5); of 32 bits memory, in parts (77 x 128001 14.5 us and
 // 5 for the join); one row latency (1 x 32000 7.5 us).  Workgroups that go on to another row, its loads out while the last one's results
 // are joined, spilled registers and took 101 us for 69.
 //
@@ -19,7 +21,7 @@
 // (some 25 where k is 20) are collected in any order and placed by counting,
 // for each, those before it: larger, or equal with a lower column.  Where more than kCand reach the bound
 // (masked rows whose bound is minus infinity, many equal ones) the k-th value is found by bisection on its bits, and
-// the last column of its equals by bisection on the column.
+// its equals are taken in the order of their columns.
 #include "linear.h"
 
 #include <math.h>
@@ -930,7 +932,8 @@ Plan logprobs_plan(int64_t M, int64_t V, int type) {
 
 // With the gradient a second reading costs more than the registers of a whole row: parts only where those do not hold it (77 x
 // 128001 in 32 bits: parts of 8192 30 us, of 65536 37), or for few rows of more than 65536 (1 x 128000 in 16 bits 14.7 for 20; 1000 of them
-// 127 for 102).  32768 columns by eight waves: 4096 x 32000 in 16 bits 102 us, by sixteen 106.
+// 127 for 102).  32768 columns by eight waves: 4096 x 32000 in 16 bits 102 us, by sixteen 106; in 32 bits 1000 x 32000 56 us, by sixteen 66, but
+// 4000 x 32000 240 and 222.
 Plan distill_plan(int64_t M, int64_t V, int type) {
     if (V <= 16384) return short_row(V);
     if (V <= 32768) return Plan{k32768, 1};
